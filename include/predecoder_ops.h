@@ -1,0 +1,192 @@
+/*
+ * predecoder_ops.h -- C ABI of the token operators (MI355X, gfx950).
+ *
+ * The pre-decoder of predecoder.h is local: an output sees its receptive field
+ * only.  A layer that looks at a whole volume is a block of attention over its
+ * sites, one token for each site of each round (the activations that
+ * predecoder_activations gives, [batch][T][H][H][channels], are such tokens).
+ * These are the operators of such a block, for inference:
+ *
+ *   predecoder_rms_norm    root-mean-square norm with the residual's addition,
+ *                          its output as it is or in 8 bits with a scale a token
+ *   predecoder_matmul8     product of 8-bit codes with scales for each token and
+ *                          channel, bias and activation
+ *   predecoder_rope        rotary positions with three axes (round, row, column)
+ *   predecoder_attention   grouped-head attention with capped scores, a distance
+ *                          bias and masks by volume, round and prefix
+ *
+ * Types.  bf16 (PD_DTYPE_BF16) and fp32 (PD_DTYPE_FP32) values; 8-bit codes are
+ * OCP E4M3 (the library's 8-bit format) or signed integers.  Sums, norms and
+ * softmax statistics are fp32 (sums of int8 products: exact int32); every
+ * output is rounded once, to nearest even.  Results are bit-reproducible: no
+ * operator uses atomics, and a call's order of sums depends on its sizes,
+ * types and alignment alone.
+ *
+ * Layout.  The last axis of a matrix is contiguous; strides of the other axes
+ * are in elements and may be any (rows of a wider tensor, a joint projection, a
+ * cache).  Rows at 16-byte aligned addresses with lengths a multiple of 16 bytes take
+ * the wide loads; others are right, and slower.
+ *
+ * Errors, streams.  As in predecoder.h: every function is nothrow and never
+ * aborts; misuse that the host can see gives PD_ERR_INVALID_ARG (sizes or
+ * strides it has no form for: PD_ERR_UNSUPPORTED) before any device call; a
+ * failed launch gives PD_ERR_DEVICE.  All buffers are the caller's device
+ * memory, work is enqueued on hip_stream, the host never waits, nothing is
+ * allocated (calls may be recorded into HIP graphs).  The operators keep no
+ * state: calls on different streams may overlap if their buffers do not.
+ * Calls with no token do nothing.
+ */
+#ifndef PREDECODER_OPS_H
+#define PREDECODER_OPS_H
+
+#include "predecoder.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Where a token sits: its round, its row and column on the grid, and the
+ * volume (logical qubit, document) that it belongs to.  volume < 0: no token
+ * (padding; the unused rest of a cache). */
+typedef struct pd_site {
+  int32_t t, i, j, volume;
+} pd_site;
+
+typedef enum pd_codes { PD_CODES_NONE = 0, PD_CODES_E4M3 = 1, PD_CODES_INT8 = 2 } pd_codes;
+
+/* ---- Root-mean-square norm ----
+ *
+ *   s = x + residual                      (residual NULL: s = x)
+ *   y = s / sqrt(mean(s^2) + eps) * gain  (gain NULL: 1; mean over the row)
+ * Each of these outputs may be NULL (one at least must be given):
+ *   sum     s rounded to dtype (the next residual); may be x or residual
+ *   out     y rounded to dtype; may be x or residual
+ *   codes   y / scale rounded to codes_type, and scales (given with codes, fp32,
+ *           one a row): scale = max |y| / 448 (E4M3) or / 127 (int8).  A row of
+ *           zeros has scale 0 and codes 0; a row whose sum of squares or whose
+ *           s gain is not finite in fp32 has scale NaN and codes 0.
+ * y is computed from the unrounded s.  1 <= width <= 32768.  An output must be
+ * one of the inputs itself (same address and stride) or not overlap them. */
+typedef struct pd_norm_args {
+  int64_t rows;
+  int32_t width;
+  int32_t dtype;      /* of x, residual, sum and out: PD_DTYPE_BF16 or PD_DTYPE_FP32 */
+  int32_t codes_type; /* pd_codes of codes (PD_CODES_NONE: codes and scales NULL) */
+  float eps;          /* >= 0 */
+  const void* x;
+  int64_t x_stride;
+  const void* residual;
+  int64_t residual_stride;
+  const float* gain; /* [width] */
+  void* sum;
+  int64_t sum_stride;
+  void* out;
+  int64_t out_stride;
+  void* codes; /* one byte each */
+  int64_t codes_stride;
+  float* scales; /* [rows] */
+} pd_norm_args;
+
+pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* args);
+
+/* ---- Product of 8-bit codes ----
+ *
+ *   out[m][n] = act(a_scales[m] w_scales[n] sum_k a[m][k] w[n][k] + bias[n])
+ * a: [M][K] codes of the tokens, w: [N][K] codes of the output channels, both of
+ * codes_type; int8 sums are exact (K <= 131071), E4M3 sums fp32.  bias [N] or
+ * NULL; act: pd_act; out bf16 or fp32 (out_dtype).  K = 0 gives act(bias). */
+typedef struct pd_matmul8_args {
+  int64_t M;
+  int32_t N, K;
+  int32_t codes_type; /* PD_CODES_E4M3 or PD_CODES_INT8 */
+  int32_t out_dtype;
+  int32_t act;
+  const void* a;
+  int64_t a_stride;
+  const float* a_scales; /* [M] */
+  const void* w;
+  int64_t w_stride;
+  const float* w_scales; /* [N] */
+  const float* bias;     /* [N] or NULL */
+  void* out;
+  int64_t out_stride;
+} pd_matmul8_args;
+
+pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args* args);
+
+/* ---- Rotary positions ----
+ *
+ * The head_dim values of a head are head_dim / 2 pairs (u, v): values m and
+ * m + head_dim / 2, or 2 m and 2 m + 1 if interleaved.  The pairs are cut into
+ * three runs of sections[0], sections[1] and sections[2] pairs for the axes t, i
+ * and j (their sum may be less than head_dim / 2: the rest is copied); pair k of
+ * a run of n turns by the angle  p base^(-k / n),  p the token's position on that axis:
+ *   (u, v) -> (u cos - v sin, v cos + u sin)       (inverse: by the negative angle)
+ * Angles are taken to 2^-24 of a turn up to |p| = 2^23.  out may be x itself
+ * (same strides).  head_dim even, at most 256. */
+typedef struct pd_rope_args {
+  int64_t tokens;
+  int32_t heads, head_dim;
+  int32_t dtype; /* PD_DTYPE_BF16 or PD_DTYPE_FP32 */
+  int32_t sections[3];
+  int32_t interleaved, inverse; /* 0 or 1 */
+  double base;                  /* > 0 */
+  const pd_site* sites;         /* [tokens], 16-byte aligned */
+  const void* x;
+  int64_t x_token_stride, x_head_stride;
+  void* out;
+  int64_t out_token_stride, out_head_stride;
+} pd_rope_args;
+
+pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
+
+/* ---- Attention ----
+ *
+ * For query token a of head h, and key token b of head h / (heads / kv_heads):
+ *   z = scale q.k;   z = cap tanh(z / cap) if cap > 0;
+ *   z -= slopes[h] (|t_a - t_b| + |i_a - i_b| + |j_a - j_b|)  if slopes is given
+ *   out = sum_b softmax_b(z) v_b   over the visible tokens b:
+ *     volume_a = volume_b >= 0, and with causal t_b <= t_a or t_b < prefix
+ * Without sites (both NULL) every token is visible, and slopes, causal and
+ * prefix must be unset.  A query that sees nothing gets zeros; keys and values at
+ * invisible places do not reach the result, whatever they hold.  bf16 values;
+ * the probabilities are rounded to bf16 for their product with v, their sum is not.
+ * head_dim: a multiple of 8, at most 128; all rows (strides and addresses) of q,
+ * k, v and out 16-byte aligned; heads a multiple of kv_heads, heads / kv_heads
+ * <= 64; |coordinate| < 2^29.
+ * workspace: device memory of at least predecoder_attention_workspace(args)
+ * bytes, 16-byte aligned (NULL if that is 0), not shared by calls that may
+ * overlap. */
+typedef struct pd_attention_args {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t n_q, n_k; /* tokens of one batch entry */
+  float scale, cap;
+  int32_t causal, prefix; /* causal 0 or 1; prefix >= 0 rounds */
+  const void* q;
+  int64_t q_batch_stride, q_token_stride, q_head_stride;
+  const void* k;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  const void* v;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+  void* out;
+  int64_t out_batch_stride, out_token_stride, out_head_stride;
+  const pd_site* q_sites; /* [batch][n_q], 16-byte aligned */
+  int64_t q_sites_batch_stride; /* in sites; 0: one list for all */
+  const pd_site* k_sites;
+  int64_t k_sites_batch_stride;
+  const float* slopes; /* [heads] */
+  void* workspace;
+  size_t workspace_bytes;
+} pd_attention_args;
+
+/* Bytes of workspace that a call with these arguments uses (its pointers are
+ * not read); 0 for invalid arguments. */
+size_t predecoder_attention_workspace(const pd_attention_args* args);
+
+pd_status predecoder_attention(void* hip_stream, const pd_attention_args* args);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* PREDECODER_OPS_H */

@@ -42,6 +42,18 @@ EXPORTS = ("predecoder_create", "predecoder_create_ex", "predecoder_run", "prede
            "predecoder_create_resnet", "predecoder_graph_create", "predecoder_graph_launch",
            "predecoder_graph_destroy", "predecoder_run_static", "predecoder_peak_mfma", "predecoder_peak_copy")
 
+# The token operators (tokens.py): they work on torch tensors, so their module is loaded when one is first used.
+_TOKEN_OPS = ("rms_norm", "matmul8", "rope", "attention", "attention_workspace", "volume_sites")
+__all__ += list(_TOKEN_OPS)
+
+
+def __getattr__(name):
+    if name in _TOKEN_OPS:
+        from . import tokens
+        value = globals()[name] = getattr(tokens, name)
+        return value
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))
+
 
 class PredecoderError(RuntimeError):
     def __init__(self, status, what):

@@ -1,0 +1,257 @@
+// rms_norm.hip -- root-mean-square norm over the rows of a matrix, with the
+// residual's addition before it and an 8-bit output with one scale per row.
+//
+//   s = x + residual;  y = s / sqrt(mean(s^2) + eps) * gain
+//   scale = max |y| / Q;  code = round(y / scale) = round(s gain Q / max |s gain|)
+//
+// One pass: a row is read once into registers (by LPR lanes with NV granules
+// of 8 values each), both statistics -- the sum of s^2 and the largest
+// |s gain| -- come from there, and every output is written from there.  The
+// code needs no division by the norm: it cancels.  Bound by memory.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "../../include/predecoder_ops.h"
+#include "activation.h"
+#include "token_values.h"
+
+namespace {
+
+using namespace pd;
+
+struct Norm {
+  long long rows;
+  int width;
+  float inv_width, eps, qmax;
+  const void* x;
+  const void* residual;
+  const float* gain;
+  void* sum;
+  void* out;
+  uint8_t* codes;
+  float* scales;
+  long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
+  int int8;
+};
+
+// The column of value e (0 .. 8 NV - 1) of a lane: granules of 8 neighbours,
+// or (rows without wide loads) one value in every LPR.
+template <int LPR, bool WIDE>
+__device__ __forceinline__ int column(int lane, int e) {
+  return WIDE ? ((e >> 3) * LPR + lane) * 8 + (e & 7) : e * LPR + lane;
+}
+
+template <typename T, int LPR, int NV, bool WIDE>
+__device__ __forceinline__ void load_row(const T* __restrict__ p, int lane, int width, float (&v)[8 * NV]) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int g = 0; g < NV; ++g) {
+      const int c = column<LPR, true>(lane, 8 * g);
+      float t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (c < width) load8(p + c, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[8 * g + e] = t[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8 * NV; ++e) {
+      const int c = column<LPR, false>(lane, e);
+      v[e] = c < width ? load1(p + c) : 0.0f;
+    }
+  }
+}
+
+template <typename T, int LPR, int NV, bool WIDE>
+__device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV]) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int g = 0; g < NV; ++g) {
+      const int c = column<LPR, true>(lane, 8 * g);
+      if (c < width) store8(p + c, &v[8 * g]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8 * NV; ++e) {
+      const int c = column<LPR, false>(lane, e);
+      if (c < width) store1(p + c, v[e]);
+    }
+  }
+}
+
+// The row's sum of `a` and largest `b` in every lane of the row.
+template <int LPR>
+__device__ __forceinline__ void reduce_row(float& a, float& b, float* shared) {
+#pragma unroll
+  for (int m = 1; m < (LPR < 64 ? LPR : 64); m <<= 1) {
+    a += __shfl_xor(a, m);
+    b = fmaxf(b, __shfl_xor(b, m));
+  }
+  if constexpr (LPR > 64) {
+    constexpr int W = LPR / 64;
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();  // the row before is done with `shared`
+    if ((threadIdx.x & 63) == 0) {
+      shared[wave] = a;
+      shared[W + wave] = b;
+    }
+    __syncthreads();
+    a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      a += shared[w];
+      b = fmaxf(b, shared[W + w]);
+    }
+  }
+}
+
+template <typename T, int LPR, int NV, bool WIDE>
+__global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const Norm p) {
+  constexpr int THREADS = LPR > 256 ? LPR : 256;
+  constexpr int ROWS = THREADS / LPR;  // rows of a workgroup
+  __shared__ float shared[LPR > 64 ? 2 * (LPR / 64) : 1];
+  const int lane = threadIdx.x % LPR;
+  for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / LPR; row < p.rows;
+       row += (long long)gridDim.x * ROWS) {
+    float s[8 * NV];
+    load_row<T, LPR, NV, WIDE>((const T*)p.x + row * p.x_stride, lane, p.width, s);
+    if (p.residual) {
+      float r[8 * NV];
+      load_row<T, LPR, NV, WIDE>((const T*)p.residual + row * p.residual_stride, lane, p.width, r);
+#pragma unroll
+      for (int e = 0; e < 8 * NV; ++e) s[e] += r[e];
+    }
+    float g[8 * NV];
+    if (p.gain) {
+      load_row<float, LPR, NV, WIDE>(p.gain, lane, p.width, g);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8 * NV; ++e) g[e] = 1.0f;
+    }
+    if (p.sum) store_row<T, LPR, NV, WIDE>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
+    float square = 0.0f, most = 0.0f, check = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8 * NV; ++e) {
+      square = fmaf(s[e], s[e], square);
+      s[e] *= g[e];
+      most = fmaxf(most, fabsf(s[e]));  // drops NaN
+      check = fmaf(s[e], 0.0f, check);  // NaN from an infinite or NaN s gain
+    }
+    if (!(check == 0.0f)) most = INFINITY;
+    reduce_row<LPR>(square, most, shared);
+    const float inv = 1.0f / sqrtf(fmaf(square, p.inv_width, p.eps));
+    if (p.out) {
+      float y[8 * NV];
+#pragma unroll
+      for (int e = 0; e < 8 * NV; ++e) y[e] = s[e] * inv;
+      store_row<T, LPR, NV, WIDE>((T*)p.out + row * p.out_stride, lane, p.width, y);
+    }
+    if (p.codes) {
+      const bool finite = square < INFINITY && most < INFINITY;  // false for a NaN square
+      // rows of tiny values are lifted by a power of two, so that Q / most stays finite
+      const float lift = most < 0x1p-64f ? 0x1p64f : 1.0f;
+      const float q = finite && most > 0.0f ? p.qmax / (most * lift) : 0.0f;
+      if (lane == 0) p.scales[row] = finite ? most * inv / p.qmax : NAN;
+      uint8_t* c = p.codes + row * p.codes_stride;
+      float y[8 * NV];
+#pragma unroll
+      for (int e = 0; e < 8 * NV; ++e) y[e] = finite ? (s[e] * lift) * q : 0.0f;
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          const int at = column<LPR, true>(lane, 8 * n);
+          const float* v = &y[8 * n];
+          if (at < p.width) {
+            uint2 w;
+            if (p.int8) {
+              w.x = int8_pack4(v[0], v[1], v[2], v[3]);
+              w.y = int8_pack4(v[4], v[5], v[6], v[7]);
+            } else {
+              w.x = e4m3_pack4(v[0], v[1], v[2], v[3]);
+              w.y = e4m3_pack4(v[4], v[5], v[6], v[7]);
+            }
+            *(uint2*)(c + at) = w;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8 * NV; ++e) {
+          const int at = column<LPR, false>(lane, e);
+          if (at < p.width) c[at] = (uint8_t)(p.int8 ? int8_pack4(y[e], 0, 0, 0) : e4m3_pack4(y[e], 0, 0, 0));
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int LPR, int NV>
+void launch(const Norm& p, bool wide, hipStream_t st) {
+  constexpr int THREADS = LPR > 256 ? LPR : 256;
+  constexpr int ROWS = THREADS / LPR;
+  const long long want = (p.rows + ROWS - 1) / ROWS;
+  const unsigned blocks = (unsigned)(want < (1 << 21) ? want : (1 << 21));  // threads stay below 2^32
+  if (wide)
+    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true>), dim3(blocks), dim3(THREADS), 0, st, p);
+  else
+    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, false>), dim3(blocks), dim3(THREADS), 0, st, p);
+}
+
+// As few lanes as hold the row with one granule each up to a wave (a wave
+// then reduces several narrow rows at once), then more granules, then a
+// workgroup to a row.
+template <typename T>
+void launch_for_width(const Norm& p, bool wide, hipStream_t st) {
+  if (p.width <= 64) return launch<T, 8, 1>(p, wide, st);
+  if (p.width <= 128) return launch<T, 16, 1>(p, wide, st);
+  if (p.width <= 256) return launch<T, 32, 1>(p, wide, st);
+  if (p.width <= 512) return launch<T, 64, 1>(p, wide, st);
+  if (p.width <= 1024) return launch<T, 64, 2>(p, wide, st);
+  if (p.width <= 2048) return launch<T, 256, 1>(p, wide, st);
+  if (p.width <= 4096) return launch<T, 256, 2>(p, wide, st);
+  if (p.width <= 8192) return launch<T, 1024, 1>(p, wide, st);
+  return launch<T, 1024, 4>(p, wide, st);
+}
+
+bool aligned(const void* p, long long stride, int elem, int to) {
+  return !p || ((uintptr_t)p % to == 0 && (stride * elem) % to == 0);
+}
+
+}  // namespace
+
+extern "C" pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* a) {
+  if (!a || a->rows < 0 || a->width < 1 || !(a->eps >= 0.0f) || !(a->eps < INFINITY)) return PD_ERR_INVALID_ARG;
+  if (a->dtype != PD_DTYPE_BF16 && a->dtype != PD_DTYPE_FP32) return PD_ERR_INVALID_ARG;
+  if (a->codes_type < PD_CODES_NONE || a->codes_type > PD_CODES_INT8) return PD_ERR_INVALID_ARG;
+  if (a->rows == 0) return PD_OK;
+  const bool codes = a->codes_type != PD_CODES_NONE;
+  if (codes != (a->codes != nullptr) || codes != (a->scales != nullptr)) return PD_ERR_INVALID_ARG;
+  if (!a->x || (!a->sum && !a->out && !codes)) return PD_ERR_INVALID_ARG;
+  // an output's rows may not overlap each other; an input's may
+  if (a->rows > 1 && ((a->sum && a->sum_stride < a->width) || (a->out && a->out_stride < a->width) ||
+                      (codes && a->codes_stride < a->width)))
+    return PD_ERR_INVALID_ARG;
+  const int elem = a->dtype == PD_DTYPE_BF16 ? 2 : 4;
+  if ((uintptr_t)a->x % elem || (uintptr_t)a->residual % elem || (uintptr_t)a->sum % elem ||
+      (uintptr_t)a->out % elem || (uintptr_t)a->gain % 4 || (uintptr_t)a->scales % 4)
+    return PD_ERR_INVALID_ARG;
+  if (a->width > 32768) return PD_ERR_UNSUPPORTED;
+  Norm p;
+  p.rows = a->rows;
+  p.width = a->width;
+  p.inv_width = 1.0f / (float)a->width;
+  p.eps = a->eps;
+  p.int8 = a->codes_type == PD_CODES_INT8;
+  p.qmax = p.int8 ? 127.0f : 448.0f;
+  p.x = a->x, p.residual = a->residual, p.gain = a->gain, p.sum = a->sum, p.out = a->out;
+  p.codes = (uint8_t*)a->codes, p.scales = a->scales;
+  p.x_stride = a->x_stride, p.residual_stride = a->residual_stride, p.sum_stride = a->sum_stride;
+  p.out_stride = a->out_stride, p.codes_stride = a->codes_stride;
+  const bool wide = a->width % 8 == 0 && aligned(a->x, a->x_stride, elem, 16) &&
+                    aligned(a->residual, a->residual_stride, elem, 16) && aligned(a->gain, 0, 4, 16) &&
+                    aligned(a->sum, a->sum_stride, elem, 16) && aligned(a->out, a->out_stride, elem, 16) &&
+                    aligned(a->codes, a->codes_stride, 1, 8);
+  if (a->dtype == PD_DTYPE_BF16)
+    launch_for_width<uint16_t>(p, wide, (hipStream_t)hip_stream);
+  else
+    launch_for_width<float>(p, wide, (hipStream_t)hip_stream);
+  return hipGetLastError() == hipSuccess ? PD_OK : PD_ERR_DEVICE;
+}
