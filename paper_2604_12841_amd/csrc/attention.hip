@@ -4,14 +4,23 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  The
 // heads that share keys are rows of one query matrix: row r is token
-// r / group, head r % group of the key head's group.  A workgroup takes 128
-// rows, a wave 32, and 64 keys at a time come through LDS.  A wave computes
-// the transposed scores K Q^T, so a lane holds 32 of the 64 scores of one row
-// (the other half of the wave the rest): maximum and sum need one exchange.
-// The same registers, rounded to bf16, are the right operand of
-// out^T += V^T P^T, whose sum over keys may run in any order as long as V
-// follows it.
+// r / group, head r % group of the key head's group.  A wave takes 32 rows, a
+// workgroup 32 or (four waves) 128, and tiles of keys come through LDS, two in
+// turn: the next one is on its way from memory to registers while this one
+// is worked on.  A wave computes the transposed scores K Q^T, so a lane holds
+// half of the scores of one row (the other half of the wave the rest): maximum
+// and sum need one exchange.  The same registers, rounded to bf16, are the
+// right operand of out^T += V^T P^T, whose sum over keys may run in any order
+// as long as V follows it; V is read transposed from LDS.
+//
+// What to read: a short kernel notes for every tile of 64 keys which volumes
+// and rounds it holds.  A workgroup skips tiles that none of its rows sees, and
+// tiles that all rows of a wave see whole need no mask.
+//
+// Few rows against many keys: the keys are split over workgroups, each
+// leaves its maximum, sum and unscaled result (fp32), and a last kernel joins them.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 
 #include "../../include/predecoder_ops.h"
@@ -22,18 +31,30 @@ namespace {
 using namespace pd;
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int TK = 64;     // keys of a tile
-constexpr int ROWS = 128;  // query rows of a workgroup
+constexpr int TILE = 64;  // keys of a noted tile
+
+// What a tile of keys holds: the range of volumes and of rounds over its tokens (vmin > vmax: none).
+struct Tile {
+  int vmin, vmax, tmin, tmax;
+  int flags;  // HOLES, BYTES
+  int pad[3];
+};
+constexpr int HOLES = 1;  // a place holds no token
+constexpr int BYTES = 2;  // rows and columns of all tokens are in [0, 255]
 
 struct Attn {
-  int heads, kv_heads, group, head_dim;
+  int batch, heads, kv_heads, group, head_dim;
   int n_q, n_k;
-  long long rows;  // n_q * group
-  int causal, prefix;
-  float scale, cap;  // cap 0: none
+  int rows;  // n_q * group
+  int row_tiles, splits, tiles, tiles_per_split;
+  int prefix_last;  // prefix - 1
+  int causal;
+  float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
+  float cap_a, cap_b;
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
@@ -43,6 +64,10 @@ struct Attn {
   const int4* k_sites;
   long long q_sites_b, k_sites_b;
   const float* slopes;
+  const Tile* notes;  // [lists][tiles] or null: nothing is skipped, every tile masked
+  int notes_b;        // tiles from batch entry to batch entry
+  float* part_o;      // [splits][batch][kv_heads][rows][DP]
+  float2* part_ml;    // [splits][batch][kv_heads][rows]: maximum (log2 units), sum
 };
 
 // |a - b| + c
@@ -50,22 +75,89 @@ __device__ __forceinline__ uint32_t far_add(int a, int b, uint32_t c) {
   return (uint32_t)((a > b ? a : b) - (a > b ? b : a)) + c;
 }
 
+// Rounds, rows and columns as bytes, for distances between sites that share t >> 8.
+__device__ __forceinline__ uint32_t site_bytes(const int4 s) {
+  return (uint32_t)(s.x & 255) | (uint32_t)(s.y & 255) << 8 | (uint32_t)(s.z & 255) << 16;
+}
+
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v = min(v, __shfl_xor(v, m));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v = max(v, __shfl_xor(v, m));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+__device__ __forceinline__ bool in_byte(int v) { return (v & ~255) == 0; }
+
+// One wave a tile: what its 64 keys hold.
+__global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __restrict__ sites, long long sites_b, int n_k,
+                                                              int tiles, Tile* __restrict__ notes) {
+  const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (tile >= tiles) return;
+  const int key = tile * TILE + lane;
+  const int4 s = key < n_k ? sites[blockIdx.y * sites_b + key] : make_int4(0, 0, 0, -1);
+  const bool there = s.w >= 0;
+  Tile t;
+  t.vmin = wave_min(there ? s.w : INT_MAX);
+  t.vmax = wave_max(there ? s.w : -1);
+  t.tmin = wave_min(there ? s.x : INT_MAX);
+  t.tmax = wave_max(there ? s.x : INT_MIN);
+  t.flags = (__all(there) ? 0 : HOLES) | (__all(!there || (in_byte(s.y) && in_byte(s.z))) ? BYTES : 0);
+  t.pad[0] = t.pad[1] = t.pad[2] = 0;
+  if (lane == 0) notes[(long long)blockIdx.y * tiles + tile] = t;
+}
+
+// LDS byte of granule g (8 values) of a key's row.  Rows are not padded; which
+// granule lies where is turned by the key, so that the 16 lanes that are
+// served together fall on different banks: K is read 32 keys at a
+// time, one granule each, V four keys at a time, two granules each.
 template <int DP>
-__global__ void __launch_bounds__(256) attention_kernel(const Attn p) {
-  constexpr int KP = DP * 2 + 16;  // bytes of a key's row in LDS
-  constexpr int VP = TK * 2 + 16;  // bytes of a row of V^T
-  __shared__ __attribute__((aligned(16))) uint8_t lk[TK * KP];
-  __shared__ __attribute__((aligned(16))) uint8_t lv[DP * VP];
-  __shared__ int4 ls[TK];
-  __shared__ int odd_v;  // the tile of V holds an infinity or a NaN
+__device__ __forceinline__ int k_place(int key, int g) {
+  const int turn = DP == 128 ? key & 15 : DP == 64 ? (key >> 1) & 7 : (key >> 2) & 3;
+  return key * (DP * 2) + ((g ^ turn) << 4);
+}
+template <int DP>
+__device__ __forceinline__ int v_place(int key, int g) {
+  const int turn = DP == 128 ? (key & 3) << 2 : DP == 64 ? ((key >> 1) & 1) << 2 : 0;
+  return key * (DP * 2) + ((g ^ turn) << 4);
+}
+
+template <int DP, int NW, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
+  constexpr int TK = NW == 1 ? 32 : 64;       // keys of a step: as many as the staging registers hold
+  constexpr int NT = NW * 64, ROWS = NW * 32;
+  constexpr int STEPS = TILE / TK;            // steps of a noted tile
+  constexpr int G = TK * (DP / 8) / NT;       // granules of K (and of V) that a thread stages
+  constexpr int NB = TK / 32;                 // blocks of 32 keys
+  __shared__ __attribute__((aligned(16))) uint8_t lk[2][TK * DP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t lv[2][TK * DP * 2];
+  __shared__ int4 ls[2][TK];
+  __shared__ __attribute__((aligned(16))) uint32_t lb[2][TK];
+  __shared__ int lodd[2][NW];  // a wave staged an infinity or a NaN of V
+  __shared__ int lq[4][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int kvh = blockIdx.y, b = blockIdx.z;
-  const long long row = (long long)blockIdx.x * ROWS + wave * 32 + (lane & 31);
-  const long long r = row < p.rows ? row : p.rows - 1;
-  const int token = (int)(r / p.group), head = kvh * p.group + (int)(r % p.group);
+
+  // Work items of one key head and entry are neighbours on one XCD (workgroups
+  // are dealt to the eight in turn), whose L2 then serves their keys.
+  const unsigned total_items = gridDim.x, xcd = blockIdx.x & 7, per = total_items >> 3, rest = total_items & 7;
+  unsigned item = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+  const int row_tile = item % p.row_tiles;
+  item /= p.row_tiles;
+  const int split = item % p.splits;
+  item /= p.splits;
+  const int kvh = item % p.kv_heads, b = item / p.kv_heads;
+
+  const int row = row_tile * ROWS + wave * 32 + (lane & 31);
+  const int r = row < p.rows ? row : p.rows - 1;  // rows past the end repeat the last: not stored
+  const int token = r / p.group, head = kvh * p.group + r % p.group;
   const uint16_t* q = p.q + b * p.q_b + token * p.q_t + head * p.q_h;
   const uint16_t* kb = p.k + b * p.k_b + kvh * p.k_h;
   const uint16_t* vb = p.v + b * p.v_b + kvh * p.v_h;
+  const int4* sites = p.k_sites ? p.k_sites + b * p.k_sites_b : nullptr;
   bf16x8 fq[DP / 16];
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
@@ -74,121 +166,287 @@ __global__ void __launch_bounds__(256) attention_kernel(const Attn p) {
     fq[s] = __builtin_bit_cast(bf16x8, w);
   }
   const int4 at = p.q_sites ? p.q_sites[b * p.q_sites_b + token] : make_int4(0, 0, 0, 0);
-  const float slope = p.slopes ? p.slopes[head] : 0.0f;
+  const bool there = at.w >= 0;
+  const int volume = there ? at.w : -2;  // keys that hold no token have -1
+  const int last = p.causal ? max(at.x, p.prefix_last) : INT_MAX;  // the last round that the row sees
+  const uint32_t at_bytes = site_bytes(at);
+  const float slope = BIAS ? p.slopes[head] * -LOG2E : 0.0f;
+
+  // what this wave's rows see, and the workgroup's
+  const int wv_min = wave_min(there ? at.w : INT_MAX), wv_max = wave_max(there ? at.w : -1);
+  const int wt_min = wave_min(there ? at.x : INT_MAX), wt_max = wave_max(there ? at.x : INT_MIN);
+  const bool w_plain = __all(there) && wv_min == wv_max;
+  const bool w_bytes = (wt_min >> 8) == (wt_max >> 8) && __all(!there || (in_byte(at.y) && in_byte(at.z)));
+  int gv_min = wv_min, gv_max = wv_max, gt_max = wt_max;
+  if constexpr (NW > 1) {
+    if (lane == 0) lq[0][wave] = wv_min, lq[1][wave] = wv_max, lq[2][wave] = wt_max;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      gv_min = min(gv_min, lq[0][w]);
+      gv_max = max(gv_max, lq[1][w]);
+      gt_max = max(gt_max, lq[2][w]);
+    }
+    gv_min = __builtin_amdgcn_readfirstlane(gv_min);
+    gv_max = __builtin_amdgcn_readfirstlane(gv_max);
+    gt_max = __builtin_amdgcn_readfirstlane(gt_max);
+  }
+  const Tile* notes = p.notes ? p.notes + (long long)b * p.notes_b : nullptr;
+  auto meets = [&](const Tile& t, int vmin, int vmax, int tmax) {
+    return t.vmin <= vmax && t.vmax >= vmin && (!p.causal || t.tmin <= tmax || t.tmin <= p.prefix_last);
+  };
+
+  // The tiles to visit, 64 at a time as a mask.
+  const int end = min(p.tiles, (split + 1) * p.tiles_per_split);
+  int base = split * p.tiles_per_split - 64;
+  uint64_t mask = 0;
+  auto next_tile = [&]() -> int {  // -1: no more
+    while (mask == 0) {
+      base += 64;
+      if (base >= end) return -1;
+      bool visit = base + lane < end;
+      if (visit && notes) visit = meets(notes[base + lane], gv_min, gv_max, gt_max);
+      mask = __ballot(visit);
+    }
+    const int bit = __builtin_ctzll(mask);
+    mask &= mask - 1;
+    return base + bit;
+  };
+
+  // Staging: granules tid + n NT of K and of V; keys past the end repeat the
+  // last (they are masked), columns past head_dim are zeros.
+  uint4 sk[G], sv[G];
+  int4 ss = make_int4(0, 0, 0, -1);
+  auto load_step = [&](int k0) {
+#pragma unroll
+    for (int n = 0; n < G; ++n) {
+      const int c = tid + n * NT, d = (c % (DP / 8)) * 8;
+      const long long key = min(k0 + c / (DP / 8), p.n_k - 1);
+      sk[n] = sv[n] = make_uint4(0, 0, 0, 0);
+      if (d < p.head_dim) {
+        sk[n] = *(const uint4*)(kb + key * p.k_t + d);
+        sv[n] = *(const uint4*)(vb + key * p.v_t + d);
+      }
+    }
+    if (tid < TK) {
+      const int key = k0 + tid;
+      ss = make_int4(0, 0, 0, key < p.n_k ? 0 : -1);
+      if (sites && key < p.n_k) {
+        ss = sites[key];
+        ss.w = ss.w < 0 ? -1 : ss.w;
+      }
+    }
+  };
+  auto store_step = [&](int buf) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int n = 0; n < G; ++n) {
+      const int c = tid + n * NT, key = c / (DP / 8), g = c % (DP / 8);
+      *(uint4*)(lk[buf] + k_place<DP>(key, g)) = sk[n];
+      *(uint4*)(lv[buf] + v_place<DP>(key, g)) = sv[n];
+      const uint32_t u[4] = {sv[n].x, sv[n].y, sv[n].z, sv[n].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
+    }
+    const bool any = __any((odd & 0x80008000u) != 0);
+    if (lane == 0) lodd[buf][wave] = any;
+    if (tid < TK) {
+      ls[buf][tid] = ss;
+      lb[buf][tid] = site_bytes(ss);
+    }
+  };
+
   f32x16 o[DP / 32];
 #pragma unroll
   for (int n = 0; n < DP / 32; ++n)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[n][e] = 0.0f;
-  float top = -INFINITY, total = 0.0f;
-  for (int k0 = 0; k0 < p.n_k; k0 += TK) {
-    __syncthreads();
-    if (tid == 0) odd_v = 0;
-    if (tid < TK) {
-      const int key = k0 + tid;
-      int4 s = make_int4(0, 0, 0, -1);
-      if (key < p.n_k) s = p.k_sites ? p.k_sites[b * p.k_sites_b + key] : make_int4(0, 0, 0, 0);
-      ls[tid] = s;
+  // scores are taken relative to `top`, the row's reference: set by the first tile that it sees, raised when a score
+  // exceeds it by 8 (the sums then stay below 2^8 times their number)
+  float top = 0.0f, total = 0.0f;
+  bool unset = true;
+
+  // LDS places of this lane's operands
+  const int vkey = (lane & 15) >> 2;  // of four keys
+  int v_off[DP / 32];
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m)
+    v_off[m] = v_place<DP>(vkey, 4 * m + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + (lane & 1) * 8 + 4 * half * DP * 2;
+  int k_off[DP / 16];
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) k_off[s] = k_place<DP>(lane & 31, 2 * s + half);
+
+  int tile = next_tile(), step = 0, buf = 0;
+  Tile note = {};
+  if (tile >= 0) {
+    if (notes) note = notes[tile];
+    load_step(tile * TILE);
+    store_step(0);
+  }
+  __syncthreads();
+  while (tile >= 0) {
+    int after = tile, after_step = step + 1;
+    if (after_step == STEPS || tile * TILE + after_step * TK >= p.n_k) after = next_tile(), after_step = 0;
+    Tile after_note = note;
+    if (after >= 0) {
+      if (notes) after_note = notes[after];
+      load_step(after * TILE + after_step * TK);
     }
-    __syncthreads();
-    for (int c = tid; c < TK * (DP / 8); c += 256) {
-      const int kk = c / (DP / 8), d = (c % (DP / 8)) * 8;
-      const bool there = k0 + kk < p.n_k && d < p.head_dim;
-      const long long key = k0 + kk;
-      const uint4 wk = there ? *(const uint4*)(kb + key * p.k_t + d) : make_uint4(0, 0, 0, 0);
-      const uint4 wv = there ? *(const uint4*)(vb + key * p.v_t + d) : make_uint4(0, 0, 0, 0);
-      *(uint4*)(lk + kk * KP + d * 2) = wk;
-      const uint32_t u[4] = {wv.x, wv.y, wv.z, wv.w};
+    __builtin_amdgcn_sched_barrier(0);
+
+    if (!notes || meets(note, wv_min, wv_max, wt_max)) {
+      f32x16 z[NB];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint16_t x = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
-        if ((x & 0x7f80) == 0x7f80) odd_v = 1;
-        *(uint16_t*)(lv + (d + e) * VP + kk * 2) = x;
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[n][e] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          const uint4 w = *(const uint4*)(lk[buf] + k_off[s] + 32 * n * DP * 2);
+          z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z[n], 0, 0, 0);
+        }
       }
-    }
-    __syncthreads();
-    f32x16 z[2];
+      const float off = (CAP ? p.cap_b : 0.0f) - top;
+      // the score in log2 units, relative to the reference; dist: the sites' distance
+      auto score = [&](float x, uint32_t dist) {
+        const float t = BIAS ? fmaf((float)dist, slope, off) : off;
+        if constexpr (CAP)
+          return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * p.c1)), t);
+        else
+          return fmaf(x, p.c1, t);
+      };
+      float most = -INFINITY;
+      const bool whole = notes ? !(note.flags & HOLES) && w_plain && note.vmin == note.vmax && note.vmin == wv_min &&
+                                     (!p.causal || note.tmax <= wt_min || note.tmax <= p.prefix_last) &&
+                                     (!BIAS || (w_bytes && (note.flags & BYTES) && (note.tmin >> 8) == (wt_min >> 8) &&
+                                                (note.tmax >> 8) == (wt_min >> 8)))
+                               : !p.k_sites && (tile + 1) * TILE <= p.n_k;
+      if (whole) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) z[n][e] = 0.0f;
+          for (int g = 0; g < 4; ++g) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if constexpr (BIAS) w = *(const uint4*)&lb[buf][32 * n + 8 * g + 4 * half];
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s) {
-        const uint4 w = *(const uint4*)(lk + (32 * n + (lane & 31)) * KP + (16 * s + 8 * half) * 2);
-        z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z[n], 0, 0, 0);
-      }
-    }
-    float most = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int4 key = ls[32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
-        float x = z[n][e] * p.scale;
-        if (p.cap > 0.0f)
-          x = p.cap - 2.0f * p.cap * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E / p.cap)));
-        if (p.slopes) x -= slope * (float)far_add(at.x, key.x, far_add(at.y, key.y, far_add(at.z, key.z, 0)));
-        const bool seen = key.w == at.w && key.w >= 0 && (!p.causal || key.x <= at.x || key.x < p.prefix);
-        x = seen ? x * LOG2E : -INFINITY;
-        z[n][e] = x;
-        most = fmaxf(most, x);
-      }
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const float was = top;
-    top = fmaxf(top, most);
-    const float base = top == -INFINITY ? 0.0f : top;
-    const float alpha = __builtin_amdgcn_exp2f(was - base);
-    total *= alpha;
-#pragma unroll
-    for (int n = 0; n < DP / 32; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[n][e] *= alpha;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        z[n][e] = __builtin_amdgcn_exp2f(z[n][e] - base);
-        total += z[n][e];
-      }
-    if (odd_v) {
-      // 0 x infinity: only the keys that a row sees may touch it
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          for (int h = 0; h < 2; ++h) {
-            const float pr = bf16_round(__shfl(n ? z[1][e] : z[0][e], (lane & 31) + 32 * h));
-            const int kk = 32 * n + 8 * (e >> 2) + 4 * h + (e & 3);
-            if (pr != 0.0f) {
-#pragma unroll
-              for (int m = 0; m < DP / 32; ++m)
-#pragma unroll
-                for (int f = 0; f < 16; ++f) {
-                  const int d = 32 * m + 8 * (f >> 2) + 4 * half + (f & 3);
-                  o[m][f] = fmaf(pr, load1((const uint16_t*)(lv + d * VP + kk * 2)), o[m][f]);
-                }
+            for (int e = 0; e < 4; ++e) {
+              const float x = score(z[n][4 * g + e], BIAS ? __builtin_amdgcn_sad_u8(u[e], at_bytes, 0) : 0);
+              z[n][4 * g + e] = x;
+              most = fmaxf(most, x);
             }
           }
-    } else {
+      } else {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          uint4 w;
-          w.x = bf16_pack(z[n][8 * s], z[n][8 * s + 1]), w.y = bf16_pack(z[n][8 * s + 2], z[n][8 * s + 3]);
-          w.z = bf16_pack(z[n][8 * s + 4], z[n][8 * s + 5]), w.w = bf16_pack(z[n][8 * s + 6], z[n][8 * s + 7]);
-#pragma unroll
-          for (int m = 0; m < DP / 32; ++m) {
-            const uint8_t* f = lv + (32 * m + (lane & 31)) * VP + (32 * n + 16 * s + 4 * half) * 2;
-            const uint2 lo = *(const uint2*)f, hi = *(const uint2*)(f + 16);
-            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y)), __builtin_bit_cast(bf16x8, w), o[m], 0,
-                0, 0);
+          for (int e = 0; e < 16; ++e) {
+            const int4 key = ls[buf][32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
+            uint32_t dist = 0;
+            if constexpr (BIAS) dist = far_add(at.x, key.x, far_add(at.y, key.y, far_add(at.z, key.z, 0)));
+            const float x = score(z[n][e], dist);
+            const bool seen = key.w == volume && key.x <= last;
+            z[n][e] = seen ? x : -INFINITY;
+            most = fmaxf(most, z[n][e]);
           }
+      }
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const bool raise = most > 8.0f || (unset && most > -INFINITY);
+      if (__any(raise)) {
+        const float up = raise ? most : 0.0f;
+        const float alpha = raise && !unset ? __builtin_amdgcn_exp2f(-up) : 1.0f;
+        if (raise) unset = false;
+        top += up;
+        total *= alpha;
+#pragma unroll
+        for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[n][e] -= up;
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          z[n][e] = __builtin_amdgcn_exp2f(z[n][e]);
+          total += z[n][e];
         }
+      bool odd = false;
+      if (!whole) {
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) any |= lodd[buf][w];
+        odd = __builtin_amdgcn_readfirstlane(any) != 0;
+      }
+      if (odd) {
+        // 0 x infinity: a value that is not finite may only touch the rows that see its key
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            for (int h = 0; h < 2; ++h) {
+              float own = z[0][e];
+#pragma unroll
+              for (int m = 1; m < NB; ++m) own = n == m ? z[m][e] : own;
+              const float pr = bf16_round(__shfl(own, (lane & 31) + 32 * h));
+              const int key = 32 * n + 8 * (e >> 2) + 4 * h + (e & 3);
+              if (pr != 0.0f) {
+#pragma unroll
+                for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+                  for (int f = 0; f < 16; ++f) {
+                    const int d = 32 * m + 8 * (f >> 2) + 4 * half + (f & 3);
+                    const uint16_t* x = (const uint16_t*)(lv[buf] + v_place<DP>(key, d >> 3)) + (d & 7);
+                    o[m][f] = fmaf(pr, load1(x), o[m][f]);
+                  }
+              }
+            }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            uint4 w;
+            w.x = bf16_pack(z[n][8 * s], z[n][8 * s + 1]), w.y = bf16_pack(z[n][8 * s + 2], z[n][8 * s + 3]);
+            w.z = bf16_pack(z[n][8 * s + 4], z[n][8 * s + 5]), w.w = bf16_pack(z[n][8 * s + 6], z[n][8 * s + 7]);
+#pragma unroll
+            for (int m = 0; m < DP / 32; ++m) {
+              // four keys of 16 columns from each 16 lanes' reads: a lane gets its column's
+              typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+              const uint8_t* f = lv[buf] + v_off[m] + (32 * n + 16 * s) * DP * 2;
+              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)f);
+              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(f + 8 * DP * 2));
+              typedef __attribute__((ext_vector_type(8))) short s16x8;
+              const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                             __builtin_bit_cast(bf16x8, w), o[m], 0, 0, 0);
+            }
+          }
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (after >= 0) store_step(buf ^ 1);
+    __syncthreads();
+    tile = after, step = after_step, buf ^= 1, note = after_note;
   }
+
   total += __shfl_xor(total, 32);
   if (row >= p.rows) return;
+  if (p.splits > 1) {
+    const long long at_row = (((long long)split * p.batch + b) * p.kv_heads + kvh) * p.rows + row;
+    float* part = p.part_o + at_row * DP;
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(float4*)(part + 32 * m + 8 * g + 4 * half) =
+            make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
+    // a row without a reference saw nothing, or NaN scores alone
+    if (half == 0) p.part_ml[at_row] = make_float2(unset && total == 0.0f ? -INFINITY : top, total);
+    return;
+  }
   const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
   uint16_t* out = p.out + b * p.o_b + token * p.o_t + head * p.o_h;
 #pragma unroll
@@ -205,6 +463,86 @@ __global__ void __launch_bounds__(256) attention_kernel(const Attn p) {
     }
 }
 
+// Joins the splits of one row: out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
+// DP / 4 lanes read a split's row, the workgroup's groups of them take splits in turn.
+template <int DP>
+__global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
+  constexpr int L = DP / 4, GROUPS = 256 / L;
+  __shared__ float4 so[GROUPS][L];
+  __shared__ float2 sm[GROUPS];
+  const int lane = threadIdx.x % L, g = threadIdx.x / L;
+  const long long item = blockIdx.x;  // (batch, kv_heads, rows)
+  const long long step = (long long)p.batch * p.kv_heads * p.rows;
+  float4 acc = make_float4(0, 0, 0, 0);
+  float top = -INFINITY, total = 0.0f;
+  for (int s = g; s < p.splits; s += GROUPS) {
+    const float2 ml = p.part_ml[s * step + item];
+    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    if (ml.x == -INFINITY) continue;  // the row saw nothing there
+    const float up = fmaxf(top, ml.x);
+    const float a = __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(ml.x - up);
+    acc.x = acc.x * a + o.x * w, acc.y = acc.y * a + o.y * w;
+    acc.z = acc.z * a + o.z * w, acc.w = acc.w * a + o.w * w;
+    total = total * a + ml.y * w;
+    top = up;
+  }
+  so[g][lane] = acc;
+  if (lane == 0) sm[g] = make_float2(top, total);
+  __syncthreads();
+  if (g != 0) return;
+  for (int n = 0; n < GROUPS; ++n) top = fmaxf(top, sm[n].x);
+  acc = make_float4(0, 0, 0, 0), total = 0.0f;
+  for (int n = 0; n < GROUPS; ++n) {
+    if (sm[n].x == -INFINITY) continue;
+    const float w = __builtin_amdgcn_exp2f(sm[n].x - top);
+    acc.x += so[n][lane].x * w, acc.y += so[n][lane].y * w;
+    acc.z += so[n][lane].z * w, acc.w += so[n][lane].w * w;
+    total += sm[n].y * w;
+  }
+  if (4 * lane >= p.head_dim) return;
+  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
+  const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
+  const int token = row / p.group, head = kvh * p.group + row % p.group;
+  uint2 w;
+  w.x = bf16_pack(acc.x * inv, acc.y * inv), w.y = bf16_pack(acc.z * inv, acc.w * inv);
+  *(uint2*)(p.out + b * p.o_b + token * p.o_t + head * p.o_h + 4 * lane) = w;
+}
+
+// How a call runs.
+struct Plan {
+  int waves;  // of a workgroup: 1 or 4
+  int row_tiles, tiles, splits, tiles_per_split;
+  bool notes;
+  size_t notes_bytes, o_bytes, ml_bytes;
+  long long items;
+};
+
+Plan plan_for(const pd_attention_args* a) {
+  Plan n = {};
+  const long long group = a->heads / a->kv_heads, rows = a->n_q * group;
+  n.waves = rows <= 64 ? 1 : 4;
+  n.row_tiles = (int)((rows + 32 * n.waves - 1) / (32 * n.waves));
+  n.tiles = (int)(((long long)a->n_k + TILE - 1) / TILE);
+  // up to four tiles are read whole: the notes' launch would cost more than it saves
+  n.notes = a->k_sites && n.tiles > 4;
+  const long long heads = (long long)a->kv_heads * a->batch, whole = n.row_tiles * heads;
+  // enough waves for the card (256 CUs), at least two tiles each
+  const long long want = 2048 / n.waves;
+  long long splits = whole >= want / 2 ? 1 : want / whole;
+  if (splits > n.tiles / 2) splits = n.tiles / 2;
+  if (splits < 1) splits = 1;
+  n.tiles_per_split = (int)((n.tiles + splits - 1) / splits);
+  if (n.tiles_per_split < 1) n.tiles_per_split = 1;
+  n.splits = n.tiles ? (n.tiles + n.tiles_per_split - 1) / n.tiles_per_split : 1;
+  const int dp = a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128;
+  const long long lists = a->k_sites_batch_stride ? a->batch : 1;
+  n.notes_bytes = n.notes ? (size_t)lists * n.tiles * sizeof(Tile) : 0;
+  n.o_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * dp * 4 : 0;
+  n.ml_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * 8 : 0;
+  n.items = whole * n.splits;
+  return n;
+}
+
 bool rows16(const void* p, long long b, long long t, long long h) {
   return (uintptr_t)p % 16 == 0 && b % 8 == 0 && t % 8 == 0 && h % 8 == 0;
 }
@@ -219,7 +557,13 @@ pd_status check(const pd_attention_args* a, bool pointers) {
   if (a->head_dim % 8 || a->head_dim > 128) return PD_ERR_UNSUPPORTED;
   if (a->heads && a->heads / a->kv_heads > 64) return PD_ERR_UNSUPPORTED;
   if (a->kv_heads > 65535 || a->batch > 65535) return PD_ERR_UNSUPPORTED;  // the grid's axes
-  if (a->heads && (long long)a->n_q * (a->heads / a->kv_heads) >= 1ll << 30) return PD_ERR_UNSUPPORTED;  // its threads
+  if (a->heads && a->batch && a->n_q) {
+    // rows are counted in 32 bits, work items and rows of all heads by the launches (threads below 2^32)
+    if ((long long)a->n_q * (a->heads / a->kv_heads) >= 1ll << 30) return PD_ERR_UNSUPPORTED;
+    const Plan n = plan_for(a);
+    if (n.items >= 1ll << 24 || (n.splits > 1 && (long long)a->n_q * a->heads * a->batch >= 1ll << 24))
+      return PD_ERR_UNSUPPORTED;
+  }
   if (!pointers || !a->batch || !a->heads || !a->n_q) return PD_OK;
   if (!a->q || !a->out || (a->n_k && (!a->k || !a->v))) return PD_ERR_INVALID_ARG;
   // (the sites of no keys may have no address)
@@ -238,16 +582,51 @@ pd_status check(const pd_attention_args* a, bool pointers) {
 
 }  // namespace
 
-extern "C" size_t predecoder_attention_workspace(const pd_attention_args* a) { return check(a, false) != PD_OK ? 0 : 0; }
+extern "C" size_t predecoder_attention_workspace(const pd_attention_args* a) {
+  if (check(a, false) != PD_OK || !a->batch || !a->heads || !a->n_q) return 0;
+  const Plan n = plan_for(a);
+  return n.o_bytes + n.ml_bytes + n.notes_bytes;
+}
+
+namespace {
+
+template <int DP, int NW>
+void launch(const Attn& p, bool cap, bool bias, unsigned items, hipStream_t st) {
+  if (cap && bias)
+    hipLaunchKernelGGL((attention_kernel<DP, NW, true, true>), dim3(items), dim3(NW * 64), 0, st, p);
+  else if (cap)
+    hipLaunchKernelGGL((attention_kernel<DP, NW, true, false>), dim3(items), dim3(NW * 64), 0, st, p);
+  else if (bias)
+    hipLaunchKernelGGL((attention_kernel<DP, NW, false, true>), dim3(items), dim3(NW * 64), 0, st, p);
+  else
+    hipLaunchKernelGGL((attention_kernel<DP, NW, false, false>), dim3(items), dim3(NW * 64), 0, st, p);
+}
+
+template <int DP>
+void launch_width(const Attn& p, const Plan& n, bool cap, bool bias, hipStream_t st) {
+  if (n.waves == 1)
+    launch<DP, 1>(p, cap, bias, (unsigned)n.items, st);
+  else
+    launch<DP, 4>(p, cap, bias, (unsigned)n.items, st);
+  if (p.splits > 1)
+    hipLaunchKernelGGL(attention_join_kernel<DP>, dim3((unsigned)(p.rows * p.kv_heads * p.batch)), dim3(256), 0, st, p);
+}
+
+}  // namespace
 
 extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_args* a) {
   const pd_status ok = check(a, true);
   if (ok != PD_OK) return ok;
   if (!a->batch || !a->heads || !a->n_q) return PD_OK;
+  const Plan n = plan_for(a);
   Attn p;
-  p.heads = a->heads, p.kv_heads = a->kv_heads, p.group = a->heads / a->kv_heads, p.head_dim = a->head_dim;
-  p.n_q = a->n_q, p.n_k = a->n_k, p.rows = (long long)a->n_q * p.group;
-  p.causal = a->causal, p.prefix = a->prefix, p.scale = a->scale, p.cap = a->cap;
+  p.batch = a->batch, p.heads = a->heads, p.kv_heads = a->kv_heads, p.group = a->heads / a->kv_heads;
+  p.head_dim = a->head_dim;
+  p.n_q = a->n_q, p.n_k = a->n_k, p.rows = a->n_q * p.group;
+  p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
+  p.prefix_last = a->prefix - 1, p.causal = a->causal;
+  p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / a->cap : a->scale * LOG2E;
+  p.cap_a = -2.0f * a->cap * LOG2E, p.cap_b = a->cap * LOG2E;
   p.q = (const uint16_t*)a->q, p.k = (const uint16_t*)a->k, p.v = (const uint16_t*)a->v, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;
   p.k_b = a->k_batch_stride, p.k_t = a->k_token_stride, p.k_h = a->k_head_stride;
@@ -256,14 +635,23 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.q_sites = (const int4*)a->q_sites, p.k_sites = (const int4*)a->k_sites;
   p.q_sites_b = a->q_sites_batch_stride, p.k_sites_b = a->k_sites_batch_stride;
   p.slopes = a->slopes;
-  const long long tiles = (p.rows + ROWS - 1) / ROWS;
-  const dim3 grid((unsigned)tiles, (unsigned)a->kv_heads, (unsigned)a->batch);
+  p.part_o = (float*)a->workspace;
+  p.part_ml = (float2*)((char*)a->workspace + n.o_bytes);
+  Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes + n.ml_bytes);
+  p.notes = n.notes ? notes : nullptr;
+  p.notes_b = a->k_sites_batch_stride ? n.tiles : 0;
   const hipStream_t st = (hipStream_t)hip_stream;
+  if (n.notes) {
+    const unsigned lists = a->k_sites_batch_stride ? (unsigned)a->batch : 1u;
+    hipLaunchKernelGGL(attention_notes_kernel, dim3((unsigned)(n.tiles + 3) / 4, lists), dim3(256), 0, st, p.k_sites,
+                       p.k_sites_b, p.n_k, p.tiles, notes);
+  }
+  const bool cap = a->cap > 0.0f, bias = a->slopes != nullptr;
   if (a->head_dim <= 32)
-    hipLaunchKernelGGL(attention_kernel<32>, grid, dim3(256), 0, st, p);
+    launch_width<32>(p, n, cap, bias, st);
   else if (a->head_dim <= 64)
-    hipLaunchKernelGGL(attention_kernel<64>, grid, dim3(256), 0, st, p);
+    launch_width<64>(p, n, cap, bias, st);
   else
-    hipLaunchKernelGGL(attention_kernel<128>, grid, dim3(256), 0, st, p);
+    launch_width<128>(p, n, cap, bias, st);
   return hipGetLastError() == hipSuccess ? PD_OK : PD_ERR_DEVICE;
 }
