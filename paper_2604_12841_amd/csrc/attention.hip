@@ -32,6 +32,7 @@ using namespace pd;
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
@@ -65,6 +66,7 @@ struct Attn {
   long long q_sites_b, k_sites_b;
   const float* slopes;
   const Tile* notes;  // [lists][tiles] or null: nothing is skipped, every tile masked
+  const uint32_t* bytes;  // with notes: site_bytes of every key, [lists][tiles][TILE]
   int notes_b;        // tiles from batch entry to batch entry
   float* part_o;      // [splits][batch][kv_heads][rows][DP]
   float2* part_ml;    // [splits][batch][kv_heads][rows]: maximum (log2 units), sum
@@ -95,7 +97,8 @@ __device__ __forceinline__ bool in_byte(int v) { return (v & ~255) == 0; }
 
 // One wave a tile: what its 64 keys hold.
 __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __restrict__ sites, long long sites_b, int n_k,
-                                                              int tiles, Tile* __restrict__ notes) {
+                                                              int tiles, Tile* __restrict__ notes,
+                                                              uint32_t* __restrict__ bytes) {
   const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (tile >= tiles) return;
   const int key = tile * TILE + lane;
@@ -108,7 +111,21 @@ __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __rest
   t.tmax = wave_max(there ? s.x : INT_MIN);
   t.flags = (__all(there) ? 0 : HOLES) | (__all(!there || (in_byte(s.y) && in_byte(s.z))) ? BYTES : 0);
   t.pad[0] = t.pad[1] = t.pad[2] = 0;
-  if (lane == 0) notes[(long long)blockIdx.y * tiles + tile] = t;
+  const long long at = (long long)blockIdx.y * tiles + tile;
+  if (lane == 0) notes[at] = t;
+  bytes[at * TILE + lane] = site_bytes(s);
+}
+
+typedef const __attribute__((address_space(1))) void global_void;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Send 16 (4) bytes a lane from memory to LDS at `to` + 16 (4) times the lane; lanes that do not take part leave
+// their place as it is.  Complete once the wave has waited for its vector memory operations.
+__device__ __forceinline__ void send16(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void send4(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 4, 0, 0);
 }
 
 // LDS byte of granule g (8 values) of a key's row.  Rows are not padded; which
@@ -127,8 +144,8 @@ __device__ __forceinline__ int v_place(int key, int g) {
 }
 
 template <int DP, int NW, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
-  constexpr int TK = NW == 1 ? 32 : 64;       // keys of a step: as many as the staging registers hold
+__global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) attention_kernel(const Attn p) {
+  constexpr int TK = NW == 1 ? 32 : 64;       // keys of a step
   constexpr int NT = NW * 64, ROWS = NW * 32;
   constexpr int STEPS = TILE / TK;            // steps of a noted tile
   constexpr int G = TK * (DP / 8) / NT;       // granules of K (and of V) that a thread stages
@@ -137,7 +154,6 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
   __shared__ __attribute__((aligned(16))) uint8_t lv[2][TK * DP * 2];
   __shared__ int4 ls[2][TK];
   __shared__ __attribute__((aligned(16))) uint32_t lb[2][TK];
-  __shared__ int lodd[2][NW];  // a wave staged an infinity or a NaN of V
   __shared__ int lq[4][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
 
@@ -167,8 +183,8 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
   }
   const int4 at = p.q_sites ? p.q_sites[b * p.q_sites_b + token] : make_int4(0, 0, 0, 0);
   const bool there = at.w >= 0;
-  const int volume = there ? at.w : -2;  // keys that hold no token have -1
-  const int last = p.causal ? max(at.x, p.prefix_last) : INT_MAX;  // the last round that the row sees
+  // the last round that the row sees (none: INT_MIN is no round)
+  const int last = !there ? INT_MIN : p.causal ? max(at.x, p.prefix_last) : INT_MAX;
   const uint32_t at_bytes = site_bytes(at);
   const float slope = BIAS ? p.slopes[head] * -LOG2E : 0.0f;
 
@@ -192,20 +208,34 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
     gt_max = __builtin_amdgcn_readfirstlane(gt_max);
   }
   const Tile* notes = p.notes ? p.notes + (long long)b * p.notes_b : nullptr;
+  const uint32_t* bytes = p.bytes + (long long)b * p.notes_b * TILE;
   auto meets = [&](const Tile& t, int vmin, int vmax, int tmax) {
     return t.vmin <= vmax && t.vmax >= vmin && (!p.causal || t.tmin <= tmax || t.tmin <= p.prefix_last);
   };
 
-  // The tiles to visit, 64 at a time as a mask.
+  // The tiles to visit, 64 at a time as a mask; each lane holds the note of its tile.
   const int end = min(p.tiles, (split + 1) * p.tiles_per_split);
   int base = split * p.tiles_per_split - 64;
   uint64_t mask = 0;
+  Tile mine = {};
+  auto note_of = [&](int tile) {
+    Tile t;
+    t.vmin = __builtin_amdgcn_readlane(mine.vmin, tile - base);
+    t.vmax = __builtin_amdgcn_readlane(mine.vmax, tile - base);
+    t.tmin = __builtin_amdgcn_readlane(mine.tmin, tile - base);
+    t.tmax = __builtin_amdgcn_readlane(mine.tmax, tile - base);
+    t.flags = __builtin_amdgcn_readlane(mine.flags, tile - base);
+    return t;
+  };
   auto next_tile = [&]() -> int {  // -1: no more
     while (mask == 0) {
       base += 64;
       if (base >= end) return -1;
       bool visit = base + lane < end;
-      if (visit && notes) visit = meets(notes[base + lane], gv_min, gv_max, gt_max);
+      if (visit && notes) {
+        mine = notes[base + lane];
+        visit = meets(mine, gv_min, gv_max, gt_max);
+      }
       mask = __ballot(visit);
     }
     const int bit = __builtin_ctzll(mask);
@@ -213,47 +243,52 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
     return base + bit;
   };
 
-  // Staging: granules tid + n NT of K and of V; keys past the end repeat the
-  // last (they are masked), columns past head_dim are zeros.
-  uint4 sk[G], sv[G];
-  int4 ss = make_int4(0, 0, 0, -1);
-  auto load_step = [&](int k0) {
-#pragma unroll
-    for (int n = 0; n < G; ++n) {
-      const int c = tid + n * NT, d = (c % (DP / 8)) * 8;
-      const long long key = min(k0 + c / (DP / 8), p.n_k - 1);
-      sk[n] = sv[n] = make_uint4(0, 0, 0, 0);
-      if (d < p.head_dim) {
-        sk[n] = *(const uint4*)(kb + key * p.k_t + d);
-        sv[n] = *(const uint4*)(vb + key * p.v_t + d);
-      }
-    }
-    if (tid < TK) {
-      const int key = k0 + tid;
-      ss = make_int4(0, 0, 0, key < p.n_k ? 0 : -1);
-      if (sites && key < p.n_k) {
-        ss = sites[key];
-        ss.w = ss.w < 0 ? -1 : ss.w;
-      }
-    }
+  // Staging, straight into LDS: granule slots tid + n NT of K and of V.  The
+  // thread's keys are KEYS apart, and the column that goes to its slot differs
+  // from n to n by an exclusive or alone.  Keys past the end repeat the last
+  // (they are masked); columns past head_dim stay the zeros that they are set
+  // to here.
+  constexpr int KEYS = NT / (DP / 8);
+  const int key0 = tid / (DP / 8), slot0 = tid % (DP / 8);
+  auto k_column = [&](int n) {
+    return (slot0 ^ (k_place<DP>(key0, 0) >> 4) % (DP / 8) ^ (k_place<DP>(KEYS * n, 0) >> 4) % (DP / 8)) * 8;
   };
-  auto store_step = [&](int buf) {
-    uint32_t odd = 0;
+  const int v_column = (slot0 ^ (v_place<DP>(key0, 0) >> 4) % (DP / 8)) * 8;
+  static_assert(KEYS % 4 == 0 && (KEYS & (KEYS - 1)) == 0, "the turns of a thread's keys");
+  if (p.head_dim < DP) {
+    for (int c = tid; c < TK * (DP / 8); c += NT)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        *(uint4*)(lk[n] + c * 16) = *(uint4*)(lv[n] + c * 16) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+  auto load_step = [&](int buf, int k0) {
+    const int most_key = p.n_k - 1 - k0;
+    const uint16_t* ks = kb + k0 * p.k_t;
+    const uint16_t* vs = vb + k0 * p.v_t;
+    const bool past = most_key < TK - 1;
 #pragma unroll
     for (int n = 0; n < G; ++n) {
-      const int c = tid + n * NT, key = c / (DP / 8), g = c % (DP / 8);
-      *(uint4*)(lk[buf] + k_place<DP>(key, g)) = sk[n];
-      *(uint4*)(lv[buf] + v_place<DP>(key, g)) = sv[n];
-      const uint32_t u[4] = {sv[n].x, sv[n].y, sv[n].z, sv[n].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
+      const int slot = (n * NT + wave * 64) * 16;
+      const int kc = k_column(n);
+      long long k_at = key0 * p.k_t + n * KEYS * p.k_t, v_at = key0 * p.v_t + n * KEYS * p.v_t;
+      if (past) {
+        const long long key = min(key0 + n * KEYS, most_key);
+        k_at = key * p.k_t, v_at = key * p.v_t;
+      }
+      if (kc < p.head_dim) send16(ks + k_at + kc, lk[buf] + slot);
+      if (v_column < p.head_dim) send16(vs + v_at + v_column, lv[buf] + slot);
     }
-    const bool any = __any((odd & 0x80008000u) != 0);
-    if (lane == 0) lodd[buf][wave] = any;
-    if (tid < TK) {
-      ls[buf][tid] = ss;
-      lb[buf][tid] = site_bytes(ss);
+    if (wave == 0 && lane < TK) {
+      if (sites && most_key >= TK - 1) {
+        send16(sites + k0 + lane, ls[buf]);
+      } else {
+        int4 s = make_int4(0, 0, 0, lane <= most_key ? 0 : -1);
+        if (sites && lane <= most_key) s = sites[k0 + lane];
+        ls[buf][lane] = s;
+      }
     }
+    if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0 + lane, lb[buf]);
   };
 
   f32x16 o[DP / 32];
@@ -279,18 +314,18 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
   int tile = next_tile(), step = 0, buf = 0;
   Tile note = {};
   if (tile >= 0) {
-    if (notes) note = notes[tile];
-    load_step(tile * TILE);
-    store_step(0);
+    note = note_of(tile);
+    load_step(0, tile * TILE);
   }
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part is in LDS
   __syncthreads();
   while (tile >= 0) {
     int after = tile, after_step = step + 1;
     if (after_step == STEPS || tile * TILE + after_step * TK >= p.n_k) after = next_tile(), after_step = 0;
     Tile after_note = note;
     if (after >= 0) {
-      if (notes) after_note = notes[after];
-      load_step(after * TILE + after_step * TK);
+      if (after_step == 0) after_note = note_of(after);
+      load_step(buf ^ 1, after * TILE + after_step * TK);
     }
     __builtin_amdgcn_sched_barrier(0);
 
@@ -335,6 +370,7 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
               z[n][4 * g + e] = x;
               most = fmaxf(most, x);
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
       } else {
 #pragma unroll
@@ -345,9 +381,10 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
             uint32_t dist = 0;
             if constexpr (BIAS) dist = far_add(at.x, key.x, far_add(at.y, key.y, far_add(at.z, key.z, 0)));
             const float x = score(z[n][e], dist);
-            const bool seen = key.w == volume && key.x <= last;
+            const bool seen = key.w == at.w && key.x <= last;
             z[n][e] = seen ? x : -INFINITY;
             most = fmaxf(most, z[n][e]);
+            if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four keys' sites in registers at a time
           }
       }
       most = fmaxf(most, __shfl_xor(most, 32));
@@ -374,60 +411,74 @@ __global__ void __launch_bounds__(NW * 64) attention_kernel(const Attn p) {
           z[n][e] = __builtin_amdgcn_exp2f(z[n][e]);
           total += z[n][e];
         }
-      bool odd = false;
+      bool odd = false;  // an infinity or a NaN in V where rows see some keys only
       if (!whole) {
-        int any = 0;
+        uint32_t carry = 0;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) any |= lodd[buf][w];
-        odd = __builtin_amdgcn_readfirstlane(any) != 0;
+        for (int n = 0; n < TK * (DP / 8) / 64; ++n) {
+          const uint4 w = *(const uint4*)(lv[buf] + (lane + 64 * n) * 16);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) carry |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
+        }
+        odd = __any((carry & 0x80008000u) != 0);
       }
+      uint4 pr[NB][2];  // the probabilities in bf16: keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          pr[n][s].x = bf16_pack(z[n][8 * s], z[n][8 * s + 1]), pr[n][s].y = bf16_pack(z[n][8 * s + 2], z[n][8 * s + 3]);
+          pr[n][s].z = bf16_pack(z[n][8 * s + 4], z[n][8 * s + 5]),
+          pr[n][s].w = bf16_pack(z[n][8 * s + 6], z[n][8 * s + 7]);
+        }
+      // V^T of those keys: four keys of 16 columns from each 16 lanes' reads, of which a lane gets its column's
+      auto values = [&](int n, int s, int m) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const uint8_t* f = lv[buf] + v_off[m] + (32 * n + 16 * s) * DP * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)f);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(f + 8 * DP * 2));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
       if (odd) {
-        // 0 x infinity: a value that is not finite may only touch the rows that see its key
-        for (int n = 0; n < NB; ++n)
+        // 0 x infinity: the finite values first; then for each kind of others, whether a row sees one in a column
+#pragma unroll 1
+        for (int kind = 0; kind < 4; ++kind) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            for (int h = 0; h < 2; ++h) {
-              float own = z[0][e];
+          for (int m = 0; m < DP / 32; ++m) {
+            f32x16 acc;
 #pragma unroll
-              for (int m = 1; m < NB; ++m) own = n == m ? z[m][e] : own;
-              const float pr = bf16_round(__shfl(own, (lane & 31) + 32 * h));
-              const int key = 32 * n + 8 * (e >> 2) + 4 * h + (e & 3);
-              if (pr != 0.0f) {
+            for (int e = 0; e < 16; ++e) acc[e] = kind ? 0.0f : o[m][e];
 #pragma unroll
-                for (int m = 0; m < DP / 32; ++m)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                  for (int f = 0; f < 16; ++f) {
-                    const int d = 32 * m + 8 * (f >> 2) + 4 * half + (f & 3);
-                    const uint16_t* x = (const uint16_t*)(lv[buf] + v_place<DP>(key, d >> 3)) + (d & 7);
-                    o[m][f] = fmaf(pr, load1(x), o[m][f]);
-                  }
+              for (int s = 0; s < 2; ++s) {
+                s16x8 a = values(n, s, m);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const int bits = (uint16_t)a[e], of = (bits & 0x7f80) != 0x7f80 ? 0 : bits & 0x7f ? 3 : bits >> 15 ? 2 : 1;
+                  a[e] = (short)(of != kind ? 0 : kind ? 0x3f80 : bits);
+                }
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                              __builtin_bit_cast(bf16x8, pr[n][s]), acc, 0, 0, 0);
               }
-            }
+            const float other = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[m][e] = kind == 0 ? acc[e] : acc[e] != 0.0f ? o[m][e] + other : o[m][e];
+          }
+        }
       } else {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            uint4 w;
-            w.x = bf16_pack(z[n][8 * s], z[n][8 * s + 1]), w.y = bf16_pack(z[n][8 * s + 2], z[n][8 * s + 3]);
-            w.z = bf16_pack(z[n][8 * s + 4], z[n][8 * s + 5]), w.w = bf16_pack(z[n][8 * s + 6], z[n][8 * s + 7]);
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int m = 0; m < DP / 32; ++m) {
-              // four keys of 16 columns from each 16 lanes' reads: a lane gets its column's
-              typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-              const uint8_t* f = lv[buf] + v_off[m] + (32 * n + 16 * s) * DP * 2;
-              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)f);
-              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(f + 8 * DP * 2));
-              typedef __attribute__((ext_vector_type(8))) short s16x8;
-              const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                             __builtin_bit_cast(bf16x8, w), o[m], 0, 0, 0);
-            }
-          }
+            for (int m = 0; m < DP / 32; ++m)
+              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(n, s, m)),
+                                                             __builtin_bit_cast(bf16x8, pr[n][s]), o[m], 0, 0, 0);
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (after >= 0) store_step(buf ^ 1);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the next step's keys are in LDS
     __syncthreads();
     tile = after, step = after_step, buf ^= 1, note = after_note;
   }
@@ -513,7 +564,7 @@ struct Plan {
   int waves;  // of a workgroup: 1 or 4
   int row_tiles, tiles, splits, tiles_per_split;
   bool notes;
-  size_t notes_bytes, o_bytes, ml_bytes;
+  size_t notes_bytes, bytes_bytes, o_bytes, ml_bytes;
   long long items;
 };
 
@@ -537,6 +588,7 @@ Plan plan_for(const pd_attention_args* a) {
   const int dp = a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128;
   const long long lists = a->k_sites_batch_stride ? a->batch : 1;
   n.notes_bytes = n.notes ? (size_t)lists * n.tiles * sizeof(Tile) : 0;
+  n.bytes_bytes = n.notes ? (size_t)lists * n.tiles * TILE * 4 : 0;
   n.o_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * dp * 4 : 0;
   n.ml_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * 8 : 0;
   n.items = whole * n.splits;
@@ -585,7 +637,7 @@ pd_status check(const pd_attention_args* a, bool pointers) {
 extern "C" size_t predecoder_attention_workspace(const pd_attention_args* a) {
   if (check(a, false) != PD_OK || !a->batch || !a->heads || !a->n_q) return 0;
   const Plan n = plan_for(a);
-  return n.o_bytes + n.ml_bytes + n.notes_bytes;
+  return n.o_bytes + n.notes_bytes + n.bytes_bytes + n.ml_bytes;
 }
 
 namespace {
@@ -636,15 +688,17 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.q_sites_b = a->q_sites_batch_stride, p.k_sites_b = a->k_sites_batch_stride;
   p.slopes = a->slopes;
   p.part_o = (float*)a->workspace;
-  p.part_ml = (float2*)((char*)a->workspace + n.o_bytes);
-  Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes + n.ml_bytes);
+  Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes);
+  uint32_t* bytes = (uint32_t*)((char*)notes + n.notes_bytes);
+  p.part_ml = (float2*)((char*)bytes + n.bytes_bytes);
   p.notes = n.notes ? notes : nullptr;
+  p.bytes = bytes;
   p.notes_b = a->k_sites_batch_stride ? n.tiles : 0;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (n.notes) {
     const unsigned lists = a->k_sites_batch_stride ? (unsigned)a->batch : 1u;
     hipLaunchKernelGGL(attention_notes_kernel, dim3((unsigned)(n.tiles + 3) / 4, lists), dim3(256), 0, st, p.k_sites,
-                       p.k_sites_b, p.n_k, p.tiles, notes);
+                       p.k_sites_b, p.n_k, p.tiles, notes, bytes);
   }
   const bool cap = a->cap > 0.0f, bias = a->slopes != nullptr;
   if (a->head_dim <= 32)
