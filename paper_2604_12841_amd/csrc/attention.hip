@@ -33,6 +33,7 @@ using namespace pd;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
@@ -66,15 +67,24 @@ struct Attn {
   long long q_sites_b, k_sites_b;
   const float* slopes;
   const Tile* notes;  // [lists][tiles] or null: nothing is skipped, every tile masked
-  const uint32_t* bytes;  // with notes: site_bytes of every key, [lists][tiles][TILE]
+  const uint32_t* bytes;  // with notes: site_bytes and ordered sites of every key, [lists][tiles][TILE]
+  const uint4* ordered_sites;
   int notes_b;        // tiles from batch entry to batch entry
   float* part_o;      // [splits][batch][kv_heads][rows][DP]
   float2* part_ml;    // [splits][batch][kv_heads][rows]: maximum (log2 units), sum
 };
 
-// |a - b| + c
-__device__ __forceinline__ uint32_t far_add(int a, int b, uint32_t c) {
-  return (uint32_t)((a > b ? a : b) - (a > b ? b : a)) + c;
+// A site as the kernel compares it: coordinates moved to unsigned numbers in the same order, volume -1 for no token.
+__device__ __forceinline__ uint4 ordered(const int4 s) {
+  const uint32_t sign = 0x80000000u;
+  return make_uint4((uint32_t)s.x ^ sign, (uint32_t)s.y ^ sign, (uint32_t)s.z ^ sign, s.w < 0 ? ~0u : (uint32_t)s.w);
+}
+
+// |a - b| + c in one instruction (the compiler takes three for it in a sum of several)
+__device__ __forceinline__ uint32_t far_add(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("v_sad_u32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 
 // Rounds, rows and columns as bytes, for distances between sites that share t >> 8.
@@ -95,10 +105,11 @@ __device__ __forceinline__ int wave_max(int v) {
 
 __device__ __forceinline__ bool in_byte(int v) { return (v & ~255) == 0; }
 
-// One wave a tile: what its 64 keys hold.
+// One wave a tile: what its 64 keys hold, and their sites in the forms that the kernel reads.
 __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __restrict__ sites, long long sites_b, int n_k,
                                                               int tiles, Tile* __restrict__ notes,
-                                                              uint32_t* __restrict__ bytes) {
+                                                              uint32_t* __restrict__ bytes,
+                                                              uint4* __restrict__ ordered_sites) {
   const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (tile >= tiles) return;
   const int key = tile * TILE + lane;
@@ -114,6 +125,7 @@ __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __rest
   const long long at = (long long)blockIdx.y * tiles + tile;
   if (lane == 0) notes[at] = t;
   bytes[at * TILE + lane] = site_bytes(s);
+  ordered_sites[at * TILE + lane] = ordered(s);
 }
 
 typedef const __attribute__((address_space(1))) void global_void;
@@ -152,7 +164,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
   constexpr int NB = TK / 32;                 // blocks of 32 keys
   __shared__ __attribute__((aligned(16))) uint8_t lk[2][TK * DP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t lv[2][TK * DP * 2];
-  __shared__ int4 ls[2][TK];
+  __shared__ uint4 ls[2][TK];  // ordered sites
   __shared__ __attribute__((aligned(16))) uint32_t lb[2][TK];
   __shared__ int lq[4][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
@@ -183,8 +195,10 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
   }
   const int4 at = p.q_sites ? p.q_sites[b * p.q_sites_b + token] : make_int4(0, 0, 0, 0);
   const bool there = at.w >= 0;
-  // the last round that the row sees (none: INT_MIN is no round)
-  const int last = !there ? INT_MIN : p.causal ? max(at.x, p.prefix_last) : INT_MAX;
+  uint4 own = ordered(at);
+  if (!there) own.w = ~1u;  // no key's volume
+  // the last round that the row sees
+  const uint32_t last = p.causal ? (uint32_t)max(at.x, p.prefix_last) ^ 0x80000000u : ~0u;
   const uint32_t at_bytes = site_bytes(at);
   const float slope = BIAS ? p.slopes[head] * -LOG2E : 0.0f;
 
@@ -209,6 +223,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
   }
   const Tile* notes = p.notes ? p.notes + (long long)b * p.notes_b : nullptr;
   const uint32_t* bytes = p.bytes + (long long)b * p.notes_b * TILE;
+  const uint4* ordered_sites = p.ordered_sites + (long long)b * p.notes_b * TILE;
   auto meets = [&](const Tile& t, int vmin, int vmax, int tmax) {
     return t.vmin <= vmax && t.vmax >= vmin && (!p.causal || t.tmin <= tmax || t.tmin <= p.prefix_last);
   };
@@ -280,12 +295,12 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
       if (v_column < p.head_dim) send16(vs + v_at + v_column, lv[buf] + slot);
     }
     if (wave == 0 && lane < TK) {
-      if (sites && most_key >= TK - 1) {
-        send16(sites + k0 + lane, ls[buf]);
+      if (notes) {
+        send16(ordered_sites + k0 + lane, ls[buf]);
       } else {
         int4 s = make_int4(0, 0, 0, lane <= most_key ? 0 : -1);
         if (sites && lane <= most_key) s = sites[k0 + lane];
-        ls[buf][lane] = s;
+        ls[buf][lane] = ordered(s);
       }
     }
     if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0 + lane, lb[buf]);
@@ -342,13 +357,21 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         }
       }
       const float off = (CAP ? p.cap_b : 0.0f) - top;
-      // the score in log2 units, relative to the reference; dist: the sites' distance
-      auto score = [&](float x, uint32_t dist) {
-        const float t = BIAS ? fmaf((float)dist, slope, off) : off;
+      auto capped = [&](float x, float t) {
         if constexpr (CAP)
           return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * p.c1)), t);
         else
           return fmaf(x, p.c1, t);
+      };
+      // the score in log2 units, relative to the reference; dist: the sites' distance
+      auto score = [&](float x, uint32_t dist) {
+        const float t = BIAS ? fmaf((float)dist, slope, off) : off;
+        return capped(x, t);
+      };
+      // dist < 2^10 as an fp16 number below the normal range is dist 2^-24: the mixed multiply-add takes it as it is
+      auto score_near = [&](float x, uint32_t dist) {
+        const float t = BIAS ? fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)dist), slope * 0x1p24f, off) : off;
+        return capped(x, t);
       };
       float most = -INFINITY;
       const bool whole = notes ? !(note.flags & HOLES) && w_plain && note.vmin == note.vmax && note.vmin == wv_min &&
@@ -366,7 +389,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float x = score(z[n][4 * g + e], BIAS ? __builtin_amdgcn_sad_u8(u[e], at_bytes, 0) : 0);
+              const float x = score_near(z[n][4 * g + e], BIAS ? __builtin_amdgcn_sad_u8(u[e], at_bytes, 0) : 0);
               z[n][4 * g + e] = x;
               most = fmaxf(most, x);
             }
@@ -377,11 +400,11 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int4 key = ls[buf][32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
+            const uint4 key = ls[buf][32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
             uint32_t dist = 0;
-            if constexpr (BIAS) dist = far_add(at.x, key.x, far_add(at.y, key.y, far_add(at.z, key.z, 0)));
+            if constexpr (BIAS) dist = far_add(own.x, key.x, far_add(own.y, key.y, far_add(own.z, key.z, 0)));
             const float x = score(z[n][e], dist);
-            const bool seen = key.w == at.w && key.x <= last;
+            const bool seen = key.w == own.w && key.x <= last;
             z[n][e] = seen ? x : -INFINITY;
             most = fmaxf(most, z[n][e]);
             if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four keys' sites in registers at a time
@@ -407,10 +430,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          z[n][e] = __builtin_amdgcn_exp2f(z[n][e]);
-          total += z[n][e];
-        }
+        for (int e = 0; e < 16; ++e) z[n][e] = __builtin_amdgcn_exp2f(z[n][e]);
       bool odd = false;  // an infinity or a NaN in V where rows see some keys only
       if (!whole) {
         uint32_t carry = 0;
@@ -423,14 +443,20 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         }
         odd = __any((carry & 0x80008000u) != 0);
       }
-      uint4 pr[NB][2];  // the probabilities in bf16: keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n
+      // the probabilities in bf16, keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n, and their sum
+      uint4 pr[NB][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          pr[n][s].x = bf16_pack(z[n][8 * s], z[n][8 * s + 1]), pr[n][s].y = bf16_pack(z[n][8 * s + 2], z[n][8 * s + 3]);
-          pr[n][s].z = bf16_pack(z[n][8 * s + 4], z[n][8 * s + 5]),
-          pr[n][s].w = bf16_pack(z[n][8 * s + 6], z[n][8 * s + 7]);
+          uint32_t u[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            u[e] = bf16_pack(z[n][8 * s + 2 * e], z[n][8 * s + 2 * e + 1]);
+            total = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u[e]),
+                                                    __builtin_bit_cast(bf16x2, 0x3f803f80u), total, false);
+          }
+          pr[n][s] = make_uint4(u[0], u[1], u[2], u[3]);
         }
       // V^T of those keys: four keys of 16 columns from each 16 lanes' reads, of which a lane gets its column's
       auto values = [&](int n, int s, int m) {
@@ -440,42 +466,50 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(f + 8 * DP * 2));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       };
+      // what a bf16 value is: 0 finite, 1 / 2 positive / negative infinity, 3 NaN
+      auto kind_of = [](int bits) { return (bits & 0x7f80) != 0x7f80 ? 0 : bits & 0x7f ? 3 : bits >> 15 ? 2 : 1; };
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          s16x8 a[DP / 32];
+#pragma unroll
+          for (int m = 0; m < DP / 32; ++m) a[m] = values(n, s, m);
+          if (odd) {
+#pragma unroll
+            for (int m = 0; m < DP / 32; ++m)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) a[m][e] = kind_of((uint16_t)a[m][e]) ? 0 : a[m][e];
+          }
+#pragma unroll
+          for (int m = 0; m < DP / 32; ++m)
+            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[m]),
+                                                           __builtin_bit_cast(bf16x8, pr[n][s]), o[m], 0, 0, 0);
+        }
       if (odd) {
-        // 0 x infinity: the finite values first; then for each kind of others, whether a row sees one in a column
+        // 0 x infinity: the finite values are in; now, for each kind of others, whether a row sees one in a column
 #pragma unroll 1
-        for (int kind = 0; kind < 4; ++kind) {
+        for (int kind = 1; kind < 4; ++kind) {
+          const float other = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN;
 #pragma unroll
           for (int m = 0; m < DP / 32; ++m) {
-            f32x16 acc;
+            f32x16 there;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[e] = kind ? 0.0f : o[m][e];
+            for (int e = 0; e < 16; ++e) there[e] = 0.0f;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
               for (int s = 0; s < 2; ++s) {
                 s16x8 a = values(n, s, m);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const int bits = (uint16_t)a[e], of = (bits & 0x7f80) != 0x7f80 ? 0 : bits & 0x7f ? 3 : bits >> 15 ? 2 : 1;
-                  a[e] = (short)(of != kind ? 0 : kind ? 0x3f80 : bits);
-                }
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                              __builtin_bit_cast(bf16x8, pr[n][s]), acc, 0, 0, 0);
+                for (int e = 0; e < 8; ++e) a[e] = kind_of((uint16_t)a[e]) == kind ? 0x3f80 : 0;  // 1 or 0
+                there = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                                __builtin_bit_cast(bf16x8, pr[n][s]), there, 0, 0, 0);
               }
-            const float other = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[m][e] = kind == 0 ? acc[e] : acc[e] != 0.0f ? o[m][e] + other : o[m][e];
+            for (int e = 0; e < 16; ++e) o[m][e] += there[e] != 0.0f ? other : 0.0f;
           }
         }
-      } else {
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int m = 0; m < DP / 32; ++m)
-              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(n, s, m)),
-                                                             __builtin_bit_cast(bf16x8, pr[n][s]), o[m], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the next step's keys are in LDS
@@ -564,7 +598,7 @@ struct Plan {
   int waves;  // of a workgroup: 1 or 4
   int row_tiles, tiles, splits, tiles_per_split;
   bool notes;
-  size_t notes_bytes, bytes_bytes, o_bytes, ml_bytes;
+  size_t notes_bytes, bytes_bytes, sites_bytes, o_bytes, ml_bytes;
   long long items;
 };
 
@@ -589,6 +623,7 @@ Plan plan_for(const pd_attention_args* a) {
   const long long lists = a->k_sites_batch_stride ? a->batch : 1;
   n.notes_bytes = n.notes ? (size_t)lists * n.tiles * sizeof(Tile) : 0;
   n.bytes_bytes = n.notes ? (size_t)lists * n.tiles * TILE * 4 : 0;
+  n.sites_bytes = 4 * n.bytes_bytes;
   n.o_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * dp * 4 : 0;
   n.ml_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * 8 : 0;
   n.items = whole * n.splits;
@@ -637,7 +672,7 @@ pd_status check(const pd_attention_args* a, bool pointers) {
 extern "C" size_t predecoder_attention_workspace(const pd_attention_args* a) {
   if (check(a, false) != PD_OK || !a->batch || !a->heads || !a->n_q) return 0;
   const Plan n = plan_for(a);
-  return n.o_bytes + n.notes_bytes + n.bytes_bytes + n.ml_bytes;
+  return n.o_bytes + n.notes_bytes + n.bytes_bytes + n.sites_bytes + n.ml_bytes;
 }
 
 namespace {
@@ -690,15 +725,16 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.part_o = (float*)a->workspace;
   Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes);
   uint32_t* bytes = (uint32_t*)((char*)notes + n.notes_bytes);
-  p.part_ml = (float2*)((char*)bytes + n.bytes_bytes);
+  uint4* ordered_sites = (uint4*)((char*)bytes + n.bytes_bytes);
+  p.part_ml = (float2*)((char*)ordered_sites + n.sites_bytes);
   p.notes = n.notes ? notes : nullptr;
-  p.bytes = bytes;
+  p.bytes = bytes, p.ordered_sites = ordered_sites;
   p.notes_b = a->k_sites_batch_stride ? n.tiles : 0;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (n.notes) {
     const unsigned lists = a->k_sites_batch_stride ? (unsigned)a->batch : 1u;
     hipLaunchKernelGGL(attention_notes_kernel, dim3((unsigned)(n.tiles + 3) / 4, lists), dim3(256), 0, st, p.k_sites,
-                       p.k_sites_b, p.n_k, p.tiles, notes, bytes);
+                       p.k_sites_b, p.n_k, p.tiles, notes, bytes, ordered_sites);
   }
   const bool cap = a->cap > 0.0f, bias = a->slopes != nullptr;
   if (a->head_dim <= 32)
