@@ -12,6 +12,10 @@
 // far below the output's rounding.  For an fp32 output that would be the
 // largest error, so its codes are widened to bf16 (exact) and summed by the
 // bf16 instruction in fp32, at half the rate.
+//
+// Tiles: four waves, two by two, each with MB x NB blocks of 32 x 32; 64 codes
+// of k at a time go through three LDS buffers, two steps ahead of their use.
+// Few tiles: a workgroup's waves share one 32 x 32 block and split k.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -41,15 +45,21 @@ struct Mm {
   const float* w_scales;
   const float* bias;
   void* out;
+  bool lines;  // rows of out are 16-byte aligned
 };
 
-// 16 bytes of a row from column k on, zero past K.
-template <bool WIDE>
+// 16 bytes of a row from column k on, zero past K; nothing outside the row is read.  (Device memory takes unaligned
+// 16-byte loads.)
 __device__ __forceinline__ uint4 row16(const uint8_t* __restrict__ row, int k, int K) {
   uint4 v = make_uint4(0, 0, 0, 0);
-  if constexpr (WIDE) {
-    if (k < K) v = *(const uint4*)(row + k);
-  } else {
+  if (k + 16 <= K) {
+    __builtin_memcpy(&v, row + k, 16);
+  } else if (k < K && K >= 16) {  // the row's last 16 bytes, moved down
+    unsigned __int128 w;
+    __builtin_memcpy(&w, row + K - 16, 16);
+    w >>= 8 * (k + 16 - K);
+    v = __builtin_bit_cast(uint4, w);
+  } else if (k < K) {
     uint32_t u[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < 16; ++e)
@@ -100,58 +110,283 @@ __device__ __forceinline__ void mma64(const uint4 w0, const uint4 w1, const uint
   }
 }
 
-// 64 tokens x 64 channels a workgroup, a 32 x 32 tile a wave, 64 codes of k
-// at a time through LDS.
-template <typename T, int SUM, int ACT, bool WIDE>
-__global__ void __launch_bounds__(256) matmul8_kernel(const Mm p) {
-  constexpr int PITCH = 80;  // bytes of an LDS row: 64 codes, and 16 to spread the banks
-  __shared__ __attribute__((aligned(16))) uint8_t la[64 * PITCH];
-  __shared__ __attribute__((aligned(16))) uint8_t lw[64 * PITCH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tiles_n = (p.N + 63) / 64;
-  const long long m0 = (long long)(blockIdx.x / tiles_n) * 64;
-  const int n0 = (int)(blockIdx.x % tiles_n) * 64;
-  const int r = tid >> 2, kc = (tid & 3) * 16;
-  const long long ra = m0 + r < p.M ? m0 + r : p.M - 1;  // rows past the end repeat the last: not stored
-  const int rw = n0 + r < p.N ? n0 + r : p.N - 1;
-  const uint8_t* pa = p.a + ra * p.a_stride;
-  const uint8_t* pw = p.w + rw * p.w_stride;
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
-  typename Acc<SUM>::type acc;
+// Sends 16 bytes a lane from base + at to LDS byte `to` (the same in all lanes) + 16 times the lane.  Written out
+// rather than with the builtin, for which the compiler waits before any later LDS read, of the other buffers too; the
+// kernel counts the loads in flight itself.  No register is an output.
+__device__ __forceinline__ void send16(const uint8_t* base, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base));
+}
+
+template <int N>
+__device__ __forceinline__ void wait_sent() {  // all but the last N loads are there
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+
+// The scales, bias, activation and rounding of a wave's blocks, through LDS to whole lines.  acc[mb][nb]: tokens 32 mb,
+// channels 32 nb on; `stage`: 16 KB of LDS of this wave's own.
+template <typename T, int SUM, int ACT, int MB, int NB>
+__device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&acc)[MB][NB], long long m0, int n0,
+                                       uint8_t* stage, bool lines) {
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  constexpr int PER = sizeof(T) == 2 && NB > 1 ? 2 : 1;     // blocks of channels a pass
+  constexpr int ROW = PER * 32 * (int)sizeof(T);            // bytes of a token's row: 64 or 128
+  constexpr int GR = ROW / 16;                              // granules of a row
+  float sa[MB];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0;
-  for (int k0 = 0; k0 < p.K; k0 += 64) {
-    const uint4 va = row16<WIDE>(pa, k0 + kc, p.K), vw = row16<WIDE>(pw, k0 + kc, p.K);
-    __syncthreads();
-    *(uint4*)(la + r * PITCH + kc) = va;
-    *(uint4*)(lw + r * PITCH + kc) = vw;
-    __syncthreads();
-    const uint8_t* fa = la + (wm + (lane & 31)) * PITCH + (lane >> 5) * 32;
-    const uint8_t* fw = lw + (wn + (lane & 31)) * PITCH + (lane >> 5) * 32;
-    const uint4 a0 = *(const uint4*)fa, a1 = *(const uint4*)(fa + 16);
-    const uint4 w0 = *(const uint4*)fw, w1 = *(const uint4*)(fw + 16);
-    mma64<SUM>(w0, w1, a0, a1, acc);
+  for (int mb = 0; mb < MB; ++mb) {
+    const long long m = m0 + 32 * mb + (lane & 31);
+    sa[mb] = p.a_scales[m < p.M ? m : p.M - 1];
   }
-  const long long m = m0 + wm + (lane & 31);
-  if (m >= p.M) return;
-  const float sa = p.a_scales[m];
-  T* out = (T*)p.out + m * p.out_stride;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int n = n0 + wn + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-    if (n < p.N) {
-      store1(out + n, act_fn<ACT>(fmaf((float)acc[e], sa * p.w_scales[n], p.bias ? p.bias[n] : 0.0f)));
+  for (int pass = 0; pass < NB / PER; ++pass) {
+#pragma unroll
+    for (int q = 0; q < PER; ++q)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int nb = pass * PER + q;
+        float sw[4], b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int n = min(n0 + 32 * nb + 8 * g + 4 * half + e, p.N - 1);
+          sw[e] = p.w_scales[n];
+          b[e] = p.bias ? p.bias[n] : 0.0f;
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = act_fn<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * sw[e], sa[mb], b[e]));
+          const int r = 32 * mb + (lane & 31);
+          if constexpr (sizeof(T) == 2) {
+            const int at = r * ROW + (((4 * q + g) ^ (r >> 1 & (GR - 1))) << 4) + 8 * half;
+            *(uint2*)(stage + at) = make_uint2(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]));
+          } else {
+            const int at = r * ROW + (((2 * g + half) ^ (r >> 1 & (GR - 1))) << 4);
+            *(float4*)(stage + at) = make_float4(v[0], v[1], v[2], v[3]);
+          }
+        }
+      }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's rows are in LDS
+    __builtin_amdgcn_wave_barrier();
+    constexpr int E = 16 / (int)sizeof(T);  // values of a granule
+#pragma unroll
+    for (int i = 0; i < MB * GR / 2; ++i) {
+      const int c = lane + 64 * i, r = c / GR, g = c % GR;
+      const long long m = m0 + r;
+      const int n = n0 + 32 * PER * pass + g * E;
+      const uint4 w = *(const uint4*)(stage + r * ROW + ((g ^ (r >> 1 & (GR - 1))) << 4));
+      if (m < p.M && n < p.N) {
+        T* to = (T*)p.out + m * p.out_stride + n;
+        if (lines && n + E <= p.N) {
+          *(uint4*)to = w;
+        } else {
+          T v[E];
+          __builtin_memcpy(v, &w, 16);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (n + e < p.N) to[e] = v[e];
+        }
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads are done before the next pass writes
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <typename T, int SUM, int ACT, int MB, int NB, bool WIDE>
+__global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
+  constexpr int TM = 64 * MB, TN = 64 * NB;
+  constexpr int BUF = (TM + TN) * 64;        // bytes of a step: tokens, then channels
+  constexpr int SENDS = BUF / 1024 / 4;      // 1 KB pieces that a wave loads a step
+  constexpr int STAGE = 32 * MB * (sizeof(T) == 2 && NB == 1 ? 64 : 128);
+  constexpr int LDS = 3 * BUF > 4 * STAGE ? 3 * BUF : 4 * STAGE;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroups are dealt to the eight XCDs in turn: an XCD takes neighbouring
+  // items, which read the same tokens.
+  const unsigned items = gridDim.x, xcd = blockIdx.x & 7, per = items >> 3, rest = items & 7;
+  const unsigned item = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+  const int tiles_n = (p.N + TN - 1) / TN;
+  const long long m0 = (long long)(item / tiles_n) * TM;
+  const int n0 = (int)(item % tiles_n) * TN;
+  const int wm = wave & 1, wn = wave >> 1;
+  const int steps = (p.K + 63) / 64;
+
+  // Granule slot s of a step's buffer: row s / 4 (tokens, then channels), and
+  // granule (s % 4) ^ (row / 4 % 4) of its 64 bytes: the 16 lanes that read at
+  // once then fall on all banks.  A wave loads slots (wave SENDS + n) 64 + lane.
+  uint32_t from[SENDS];  // byte offset of the slot's granule from the tile's first row
+  const uint8_t* const a0 = p.a + m0 * p.a_stride;
+  const uint8_t* const w0 = p.w + n0 * p.w_stride;
+  const uint8_t* rows[WIDE ? 1 : SENDS];
+#pragma unroll
+  for (int n = 0; n < SENDS; ++n) {
+    const int row = ((wave * SENDS + n) * 64 + lane) / 4, g = (lane & 3) ^ (row >> 2 & 3);
+    const bool token = row < TM;  // uniform: 16 rows a piece
+    const int r = token ? (int)min((long long)row, p.M - 1 - m0) : min(row - TM, p.N - 1 - n0);
+    if constexpr (WIDE)
+      from[n] = (uint32_t)r * (uint32_t)(token ? p.a_stride : p.w_stride) + g * 16;
+    else
+      from[n] = g * 16, rows[n] = token ? a0 + r * p.a_stride : w0 + r * p.w_stride;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
+  auto send_step = [&](int step, int buf) {  // WIDE
+    const int k0 = step * 64;
+#pragma unroll
+    for (int n = 0; n < SENDS; ++n) {
+      const int piece = wave * SENDS + n;
+      const uint8_t* base = (piece * 16 < TM ? a0 : w0) + k0;
+      if (k0 + 64 <= p.K) {
+        send16(base, from[n], lds0 + buf * BUF + piece * 1024);
+      } else if (k0 + (int)((lane & 3) ^ (lane >> 4 & 3)) * 16 < p.K) {
+        send16(base, from[n], lds0 + buf * BUF + piece * 1024);
+      } else {
+        *(uint4*)(lds + buf * BUF + piece * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  };
+  uint4 staged[WIDE ? 1 : SENDS];
+  auto load_step = [&](int step) {
+#pragma unroll
+    for (int n = 0; n < (WIDE ? 0 : SENDS); ++n) staged[n] = row16(rows[n], step * 64 + from[n], p.K);
+  };
+  auto store_step = [&](int buf) {
+#pragma unroll
+    for (int n = 0; n < (WIDE ? 0 : SENDS); ++n)
+      *(uint4*)(lds + buf * BUF + (wave * SENDS + n) * 1024 + lane * 16) = staged[n];
+  };
+
+  typename Acc<SUM>::type acc[MB][NB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0;
+
+  // this lane's row of a block, and the granules 2 half, 2 half + 1 of it
+  const int turn = lane >> 2 & 3, h2 = lane >> 5 << 1;
+  const int g0 = (h2 ^ turn) << 4, g1 = ((h2 + 1) ^ turn) << 4;
+  const int arow = (wm * 32 * MB + (lane & 31)) * 64, wrow = (TM + wn * 32 * NB + (lane & 31)) * 64;
+  auto compute = [&](int buf) {
+    const uint8_t* const s = lds + buf * BUF;
+    uint4 fa[MB][2], fw[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      fw[nb][0] = *(const uint4*)(s + wrow + nb * 2048 + g0);
+      fw[nb][1] = *(const uint4*)(s + wrow + nb * 2048 + g1);
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      fa[mb][0] = *(const uint4*)(s + arow + mb * 2048 + g0);
+      fa[mb][1] = *(const uint4*)(s + arow + mb * 2048 + g1);
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) mma64<SUM>(fw[nb][0], fw[nb][1], fa[mb][0], fa[mb][1], acc[mb][nb]);
+  };
+
+  if constexpr (WIDE) {
+    if (steps > 0) send_step(0, 0);
+    if (steps > 1) send_step(1, 1);
+    int buf = 0;
+    for (int step = 0; step < steps; ++step) {
+      if (step + 1 < steps)
+        wait_sent<SENDS>();
+      else
+        wait_sent<0>();
+      __syncthreads();  // step's codes are there for all; buffer (step + 2) % 3 is read to the end
+      if (step + 2 < steps) send_step(step + 2, buf == 0 ? 2 : buf - 1);
+      compute(buf);
+      buf = buf == 2 ? 0 : buf + 1;
+    }
+  } else {
+    if (steps > 0) {
+      load_step(0);
+      store_step(0);
+    }
+    int buf = 0;
+    for (int step = 0; step < steps; ++step) {
+      if (step + 1 < steps) load_step(step + 1);
+      __syncthreads();
+      compute(buf);
+      buf = buf == 2 ? 0 : buf + 1;
+      if (step + 1 < steps) store_step(buf);
     }
   }
+  __syncthreads();
+  finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, lds + wave * STAGE, p.lines);
+}
+
+// 32 tokens x 32 channels a workgroup of eight waves, each with every eighth step of k, straight from memory.
+template <typename T, int SUM, int ACT, bool WIDE>
+__global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
+  constexpr int W = 8;
+  __shared__ __attribute__((aligned(16))) typename Acc<SUM>::type sums[W / 2][64];
+  __shared__ __attribute__((aligned(16))) uint8_t stage[32 * 128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int tiles_n = (p.N + 31) / 32;
+  const long long m0 = (long long)(blockIdx.x / tiles_n) * 32;
+  const int n0 = (int)(blockIdx.x % tiles_n) * 32;
+  const long long ra = min(m0 + (lane & 31), p.M - 1);
+  const int rw = min(n0 + (lane & 31), p.N - 1);
+  const uint8_t* const pa = p.a + ra * p.a_stride;
+  const uint8_t* const pw = p.w + rw * p.w_stride;
+  typename Acc<SUM>::type acc[1][1];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[0][0][e] = 0;
+  auto load = [&](const uint8_t* row, int k) {
+    if constexpr (WIDE) return k < p.K ? *(const uint4*)(row + k) : make_uint4(0, 0, 0, 0);
+    else return row16(row, k, p.K);
+  };
+#pragma unroll 4
+  for (int k0 = wave * 64; k0 < p.K; k0 += W * 64) {
+    const int k = k0 + 32 * half;
+    const uint4 a0 = load(pa, k), a1 = load(pa, k + 16), w0 = load(pw, k), w1 = load(pw, k + 16);
+    mma64<SUM>(w0, w1, a0, a1, acc[0][0]);
+  }
+  // waves 4 .. 7 to 0 .. 3, then 2 and 3, then 1: one order of sums
+#pragma unroll
+  for (int n = W / 2; n > 0; n >>= 1) {
+    if (wave >= n && wave < 2 * n) sums[wave - n][lane] = acc[0][0];
+    __syncthreads();
+    if (wave < n) {
+      const typename Acc<SUM>::type other = sums[wave][lane];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[0][0][e] += other[e];
+    }
+    __syncthreads();
+  }
+  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, stage, p.lines);
+}
+
+template <typename T, int SUM, int ACT, int MB, int NB>
+void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
+  const unsigned blocks = (unsigned)(((p.M + 64 * MB - 1) / (64 * MB)) * ((p.N + 64 * NB - 1) / (64 * NB)));
+  if (wide)
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, true>), dim3(blocks), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, false>), dim3(blocks), dim3(256), 0, st, p);
 }
 
 template <typename T, int SUM, int ACT>
 void launch(const Mm& p, bool wide, hipStream_t st) {
-  const long long blocks = ((p.M + 63) / 64) * ((p.N + 63) / 64);
-  if (wide)
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, true>), dim3((unsigned)blocks), dim3(256), 0, st, p);
-  else
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, false>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+  auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
+  if (tiles(256, 128) >= 384) {
+    launch_tiles<T, SUM, ACT, 4, 2>(p, wide, st);
+  } else if (tiles(64, 64) >= 192) {
+    launch_tiles<T, SUM, ACT, 1, 1>(p, wide, st);
+  } else {
+    const unsigned blocks = (unsigned)tiles(32, 32);
+    if (wide)
+      hipLaunchKernelGGL((matmul8_few_kernel<T, SUM, ACT, true>), dim3(blocks), dim3(512), 0, st, p);
+    else
+      hipLaunchKernelGGL((matmul8_few_kernel<T, SUM, ACT, false>), dim3(blocks), dim3(512), 0, st, p);
+  }
 }
 
 }  // namespace
@@ -175,8 +410,11 @@ extern "C" pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args*
   p.a = (const uint8_t*)a->a, p.w = (const uint8_t*)a->w;
   p.a_stride = a->a_stride, p.w_stride = a->w_stride, p.out_stride = a->out_stride;
   p.a_scales = a->a_scales, p.w_scales = a->w_scales, p.bias = a->bias, p.out = a->out;
+  p.lines = (uintptr_t)a->out % 16 == 0 && (a->out_stride * elem) % 16 == 0;
+  // 256 rows of a tile within 32-bit offsets
   const bool wide = a->K % 16 == 0 && (uintptr_t)a->a % 16 == 0 && (uintptr_t)a->w % 16 == 0 &&
-                    a->a_stride % 16 == 0 && a->w_stride % 16 == 0;
+                    a->a_stride % 16 == 0 && a->w_stride % 16 == 0 && a->a_stride >= 0 && a->w_stride >= 0 &&
+                    a->a_stride < (1 << 23) && a->w_stride < (1 << 23);
   const hipStream_t st = (hipStream_t)hip_stream;
   const bool int8 = a->codes_type == PD_CODES_INT8;
   with_activation(a->act, [&](auto act) {
