@@ -125,20 +125,15 @@ __device__ __forceinline__ void wait_sent() {  // all but the last N loads are t
 }
 
 // The scales, bias, activation and rounding of a wave's blocks, through LDS to whole lines.  acc[mb][nb]: tokens 32 mb,
-// channels 32 nb on; `stage`: 16 KB of LDS of this wave's own.
+// channels 32 nb on; sa: the scales of this lane's tokens; sw: the channels' scales and, ws further, biases in LDS;
+// `stage`: LDS of this wave's own, 64 or 128 bytes a token.
 template <typename T, int SUM, int ACT, int MB, int NB>
 __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&acc)[MB][NB], long long m0, int n0,
-                                       uint8_t* stage, bool lines) {
+                                       const float (&sa)[MB], const float* sw, int ws, uint8_t* stage) {
   const int lane = threadIdx.x & 63, half = lane >> 5;
   constexpr int PER = sizeof(T) == 2 && NB > 1 ? 2 : 1;     // blocks of channels a pass
   constexpr int ROW = PER * 32 * (int)sizeof(T);            // bytes of a token's row: 64 or 128
   constexpr int GR = ROW / 16;                              // granules of a row
-  float sa[MB];
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb) {
-    const long long m = m0 + 32 * mb + (lane & 31);
-    sa[mb] = p.a_scales[m < p.M ? m : p.M - 1];
-  }
 #pragma unroll
   for (int pass = 0; pass < NB / PER; ++pass) {
 #pragma unroll
@@ -146,19 +141,15 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int nb = pass * PER + q;
-        float sw[4], b[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int n = min(n0 + 32 * nb + 8 * g + 4 * half + e, p.N - 1);
-          sw[e] = p.w_scales[n];
-          b[e] = p.bias ? p.bias[n] : 0.0f;
-        }
+        const float4 s4 = *(const float4*)(sw + 32 * nb + 8 * g + 4 * half);
+        const float4 b4 = *(const float4*)(sw + ws + 32 * nb + 8 * g + 4 * half);
+        const float s[4] = {s4.x, s4.y, s4.z, s4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            v[e] = act_fn<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * sw[e], sa[mb], b[e]));
+            v[e] = act_fn<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * s[e], sa[mb], b[e]));
           const int r = 32 * mb + (lane & 31);
           if constexpr (sizeof(T) == 2) {
             const int at = r * ROW + (((4 * q + g) ^ (r >> 1 & (GR - 1))) << 4) + 8 * half;
@@ -180,7 +171,7 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
       const uint4 w = *(const uint4*)(stage + r * ROW + ((g ^ (r >> 1 & (GR - 1))) << 4));
       if (m < p.M && n < p.N) {
         T* to = (T*)p.out + m * p.out_stride + n;
-        if (lines && n + E <= p.N) {
+        if (p.lines && n + E <= p.N) {
           *(uint4*)to = w;
         } else {
           T v[E];
@@ -196,6 +187,18 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
   }
 }
 
+// This lane's tokens' scales, and N channels' scales and biases to LDS (complete after a barrier).
+template <int MB, int N>
+__device__ __forceinline__ void load_scales(const Mm& p, long long m0, int n0, float (&sa)[MB], float* sw) {
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) sa[mb] = p.a_scales[min(m0 + 32 * mb + (threadIdx.x & 31), p.M - 1)];
+  if (threadIdx.x < N) {
+    const int n = min(n0 + (int)threadIdx.x, p.N - 1);
+    sw[threadIdx.x] = p.w_scales[n];
+    sw[N + threadIdx.x] = p.bias ? p.bias[n] : 0.0f;
+  }
+}
+
 template <typename T, int SUM, int ACT, int MB, int NB, bool WIDE>
 __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
   constexpr int TM = 64 * MB, TN = 64 * NB;
@@ -204,6 +207,7 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
   constexpr int STAGE = 32 * MB * (sizeof(T) == 2 && NB == 1 ? 64 : 128);
   constexpr int LDS = 3 * BUF > 4 * STAGE ? 3 * BUF : 4 * STAGE;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
+  __shared__ __attribute__((aligned(16))) float sw[2 * TN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroups are dealt to the eight XCDs in turn: an XCD takes neighbouring
   // items, which read the same tokens.
@@ -214,6 +218,8 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
   const int n0 = (int)(item % tiles_n) * TN;
   const int wm = wave & 1, wn = wave >> 1;
   const int steps = (p.K + 63) / 64;
+  float sa[MB];
+  load_scales<MB, TN>(p, m0 + wm * 32 * MB, n0, sa, sw);
 
   // Granule slot s of a step's buffer: row s / 4 (tokens, then channels), and
   // granule (s % 4) ^ (row / 4 % 4) of its 64 bytes: the 16 lanes that read at
@@ -319,7 +325,7 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
     }
   }
   __syncthreads();
-  finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, lds + wave * STAGE, p.lines);
+  finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, sa, sw + wn * 32 * NB, TN, lds + wave * STAGE);
 }
 
 // 32 tokens x 32 channels a workgroup of eight waves, each with every eighth step of k, straight from memory.
@@ -328,6 +334,7 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
   constexpr int W = 8;
   __shared__ __attribute__((aligned(16))) typename Acc<SUM>::type sums[W / 2][64];
   __shared__ __attribute__((aligned(16))) uint8_t stage[32 * 128];
+  __shared__ __attribute__((aligned(16))) float sw[2 * 32];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const int tiles_n = (p.N + 31) / 32;
   const long long m0 = (long long)(blockIdx.x / tiles_n) * 32;
@@ -336,6 +343,8 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
   const int rw = min(n0 + (lane & 31), p.N - 1);
   const uint8_t* const pa = p.a + ra * p.a_stride;
   const uint8_t* const pw = p.w + rw * p.w_stride;
+  float sa[1];
+  load_scales<1, 32>(p, m0, n0, sa, sw);
   typename Acc<SUM>::type acc[1][1];
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[0][0][e] = 0;
@@ -343,7 +352,6 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
     if constexpr (WIDE) return k < p.K ? *(const uint4*)(row + k) : make_uint4(0, 0, 0, 0);
     else return row16(row, k, p.K);
   };
-#pragma unroll 4
   for (int k0 = wave * 64; k0 < p.K; k0 += W * 64) {
     const int k = k0 + 32 * half;
     const uint4 a0 = load(pa, k), a1 = load(pa, k + 16), w0 = load(pw, k), w1 = load(pw, k + 16);
@@ -361,7 +369,7 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
     }
     __syncthreads();
   }
-  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, stage, p.lines);
+  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, sa, sw, 32, stage);
 }
 
 template <typename T, int SUM, int ACT, int MB, int NB>
