@@ -199,39 +199,44 @@ __device__ __forceinline__ void load_scales(const Mm& p, long long m0, int n0, f
   }
 }
 
-template <typename T, int SUM, int ACT, int MB, int NB, bool WIDE>
-__global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
-  constexpr int TM = 64 * MB, TN = 64 * NB;
-  constexpr int BUF = (TM + TN) * 64;        // bytes of a step: tokens, then channels
-  constexpr int SENDS = BUF / 1024 / 4;      // 1 KB pieces that a wave loads a step
+// 2 x WN waves of MB x NB blocks; BK codes of k a step, BUFS steps in LDS.
+template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS, bool WIDE>
+__global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
+  constexpr int TM = 64 * MB, TN = 32 * NB * WN;
+  constexpr int BUF = (TM + TN) * BK;          // bytes of a step: tokens, then channels
+  constexpr int SENDS = BUF / 1024 / (2 * WN);  // 1 KB pieces that a wave loads a step
   constexpr int STAGE = 32 * MB * (sizeof(T) == 2 && NB == 1 ? 64 : 128);
-  constexpr int LDS = 3 * BUF > 4 * STAGE ? 3 * BUF : 4 * STAGE;
+  constexpr int LDS = BUFS * BUF > 2 * WN * STAGE ? BUFS * BUF : 2 * WN * STAGE;
+  constexpr int GR = BK / 16;                  // granules of a row
   __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
   __shared__ __attribute__((aligned(16))) float sw[2 * TN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroups are dealt to the eight XCDs in turn: an XCD takes neighbouring
-  // items, which read the same tokens.
+  // items, eight tiles of tokens by all channels, whose codes stay in its L2.
   const unsigned items = gridDim.x, xcd = blockIdx.x & 7, per = items >> 3, rest = items & 7;
   const unsigned item = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
-  const int tiles_n = (p.N + TN - 1) / TN;
-  const long long m0 = (long long)(item / tiles_n) * TM;
-  const int n0 = (int)(item % tiles_n) * TN;
+  const unsigned tiles_n = (p.N + TN - 1) / TN, tiles_m = items / tiles_n;
+  const unsigned band = item / (8 * tiles_n), in_band = item - band * 8 * tiles_n;
+  const unsigned high = min(8u, tiles_m - 8 * band);
+  const long long m0 = (long long)(8 * band + in_band % high) * TM;
+  const int n0 = (int)(in_band / high) * TN;
   const int wm = wave & 1, wn = wave >> 1;
-  const int steps = (p.K + 63) / 64;
+  const int steps = (p.K + BK - 1) / BK;
   float sa[MB];
   load_scales<MB, TN>(p, m0 + wm * 32 * MB, n0, sa, sw);
 
-  // Granule slot s of a step's buffer: row s / 4 (tokens, then channels), and
-  // granule (s % 4) ^ (row / 4 % 4) of its 64 bytes: the 16 lanes that read at
-  // once then fall on all banks.  A wave loads slots (wave SENDS + n) 64 + lane.
-  uint32_t from[SENDS];  // byte offset of the slot's granule from the tile's first row
+  // Granule slot s of a step's buffer: row s / GR (tokens, then channels), and
+  // granule (s % GR) ^ turn of its BK bytes: the 16 lanes that read at once
+  // then fall on all banks.  A wave loads slots (wave SENDS + n) 64 + lane.
+  auto turn_of = [](int row) { return BK == 64 ? row >> 2 & 3 : row >> 1 & 7; };
   const uint8_t* const a0 = p.a + m0 * p.a_stride;
   const uint8_t* const w0 = p.w + n0 * p.w_stride;
+  uint32_t from[SENDS];  // byte offset of the slot's granule from the tile's first row, or in its row
   const uint8_t* rows[WIDE ? 1 : SENDS];
 #pragma unroll
   for (int n = 0; n < SENDS; ++n) {
-    const int row = ((wave * SENDS + n) * 64 + lane) / 4, g = (lane & 3) ^ (row >> 2 & 3);
-    const bool token = row < TM;  // uniform: 16 rows a piece
+    const int row = ((wave * SENDS + n) * 64 + lane) / GR, g = (lane & (GR - 1)) ^ turn_of(row);
+    const bool token = row < TM;  // uniform: whole rows a piece
     const int r = token ? (int)min((long long)row, p.M - 1 - m0) : min(row - TM, p.N - 1 - n0);
     if constexpr (WIDE)
       from[n] = (uint32_t)r * (uint32_t)(token ? p.a_stride : p.w_stride) + g * 16;
@@ -240,24 +245,29 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
   auto send_step = [&](int step, int buf) {  // WIDE
-    const int k0 = step * 64;
+    const int k0 = step * BK;
+    const uint32_t to = lds0 + buf * BUF + wave * SENDS * 1024;
+    const uint8_t* const ak = a0 + k0;
+    const uint8_t* const wk = w0 + k0;
+    if (k0 + BK <= p.K) {
 #pragma unroll
-    for (int n = 0; n < SENDS; ++n) {
-      const int piece = wave * SENDS + n;
-      const uint8_t* base = (piece * 16 < TM ? a0 : w0) + k0;
-      if (k0 + 64 <= p.K) {
-        send16(base, from[n], lds0 + buf * BUF + piece * 1024);
-      } else if (k0 + (int)((lane & 3) ^ (lane >> 4 & 3)) * 16 < p.K) {
-        send16(base, from[n], lds0 + buf * BUF + piece * 1024);
-      } else {
-        *(uint4*)(lds + buf * BUF + piece * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+      for (int n = 0; n < SENDS; ++n)
+        send16((wave * SENDS + n) * (1024 / BK) < TM ? ak : wk, from[n], to + n * 1024);
+    } else {
+#pragma unroll
+      for (int n = 0; n < SENDS; ++n) {
+        const int row = ((wave * SENDS + n) * 64 + lane) / GR, g = (lane & (GR - 1)) ^ turn_of(row);
+        if (k0 + g * 16 < p.K)
+          send16((wave * SENDS + n) * (1024 / BK) < TM ? ak : wk, from[n], to + n * 1024);
+        else
+          *(uint4*)(lds + buf * BUF + (wave * SENDS + n) * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
       }
     }
   };
   uint4 staged[WIDE ? 1 : SENDS];
   auto load_step = [&](int step) {
 #pragma unroll
-    for (int n = 0; n < (WIDE ? 0 : SENDS); ++n) staged[n] = row16(rows[n], step * 64 + from[n], p.K);
+    for (int n = 0; n < (WIDE ? 0 : SENDS); ++n) staged[n] = row16(rows[n], step * BK + from[n], p.K);
   };
   auto store_step = [&](int buf) {
 #pragma unroll
@@ -273,42 +283,46 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0;
 
-  // this lane's row of a block, and the granules 2 half, 2 half + 1 of it
-  const int turn = lane >> 2 & 3, h2 = lane >> 5 << 1;
-  const int g0 = (h2 ^ turn) << 4, g1 = ((h2 + 1) ^ turn) << 4;
-  const int arow = (wm * 32 * MB + (lane & 31)) * 64, wrow = (TM + wn * 32 * NB + (lane & 31)) * 64;
+  // this lane's row of a block, and granules 4 u + 2 half, + 1 of it
+  const int turn = turn_of(lane & 31), h2 = lane >> 5 << 1;
+  const int arow = (wm * 32 * MB + (lane & 31)) * BK, wrow = (TM + wn * 32 * NB + (lane & 31)) * BK;
   auto compute = [&](int buf) {
     const uint8_t* const s = lds + buf * BUF;
-    uint4 fa[MB][2], fw[NB][2];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      fw[nb][0] = *(const uint4*)(s + wrow + nb * 2048 + g0);
-      fw[nb][1] = *(const uint4*)(s + wrow + nb * 2048 + g1);
+    for (int u = 0; u < BK / 64; ++u) {
+      const int g0 = ((4 * u + h2) ^ turn) << 4, g1 = ((4 * u + h2 + 1) ^ turn) << 4;
+      uint4 fa[MB][2], fw[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        fw[nb][0] = *(const uint4*)(s + wrow + nb * 32 * BK + g0);
+        fw[nb][1] = *(const uint4*)(s + wrow + nb * 32 * BK + g1);
+      }
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        fa[mb][0] = *(const uint4*)(s + arow + mb * 32 * BK + g0);
+        fa[mb][1] = *(const uint4*)(s + arow + mb * 32 * BK + g1);
+      }
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) mma64<SUM>(fw[nb][0], fw[nb][1], fa[mb][0], fa[mb][1], acc[mb][nb]);
     }
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      fa[mb][0] = *(const uint4*)(s + arow + mb * 2048 + g0);
-      fa[mb][1] = *(const uint4*)(s + arow + mb * 2048 + g1);
-    }
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) mma64<SUM>(fw[nb][0], fw[nb][1], fa[mb][0], fa[mb][1], acc[mb][nb]);
   };
 
   if constexpr (WIDE) {
-    if (steps > 0) send_step(0, 0);
-    if (steps > 1) send_step(1, 1);
+#pragma unroll
+    for (int s = 0; s < BUFS - 1; ++s)
+      if (s < steps) send_step(s, s);
     int buf = 0;
     for (int step = 0; step < steps; ++step) {
-      if (step + 1 < steps)
-        wait_sent<SENDS>();
-      else
+      if (BUFS == 2 || step + 1 >= steps)
         wait_sent<0>();
-      __syncthreads();  // step's codes are there for all; buffer (step + 2) % 3 is read to the end
-      if (step + 2 < steps) send_step(step + 2, buf == 0 ? 2 : buf - 1);
+      else
+        wait_sent<SENDS>();
+      __syncthreads();  // step's codes are there for all; the buffer before it is read to the end
+      if (step + BUFS - 1 < steps) send_step(step + BUFS - 1, buf == 0 ? BUFS - 1 : buf - 1);
       compute(buf);
-      buf = buf == 2 ? 0 : buf + 1;
+      buf = buf == BUFS - 1 ? 0 : buf + 1;
     }
   } else {
     if (steps > 0) {
@@ -320,7 +334,7 @@ __global__ void __launch_bounds__(256, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) 
       if (step + 1 < steps) load_step(step + 1);
       __syncthreads();
       compute(buf);
-      buf = buf == 2 ? 0 : buf + 1;
+      buf = buf == BUFS - 1 ? 0 : buf + 1;
       if (step + 1 < steps) store_step(buf);
     }
   }
@@ -372,22 +386,23 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
   if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, sa, sw, 32, stage);
 }
 
-template <typename T, int SUM, int ACT, int MB, int NB>
+template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS>
 void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
-  const unsigned blocks = (unsigned)(((p.M + 64 * MB - 1) / (64 * MB)) * ((p.N + 64 * NB - 1) / (64 * NB)));
+  constexpr int TM = 64 * MB, TN = 32 * NB * WN;
+  const unsigned blocks = (unsigned)(((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN));
   if (wide)
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, true>), dim3(blocks), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true>), dim3(blocks), dim3(128 * WN), 0, st, p);
   else
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, false>), dim3(blocks), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, false>), dim3(blocks), dim3(128 * WN), 0, st, p);
 }
 
 template <typename T, int SUM, int ACT>
 void launch(const Mm& p, bool wide, hipStream_t st) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
   if (tiles(256, 128) >= 384) {
-    launch_tiles<T, SUM, ACT, 4, 2>(p, wide, st);
+    launch_tiles<T, SUM, ACT, 4, 2, 2, 64, 3>(p, wide, st);
   } else if (tiles(64, 64) >= 192) {
-    launch_tiles<T, SUM, ACT, 1, 1>(p, wide, st);
+    launch_tiles<T, SUM, ACT, 1, 1, 2, 64, 3>(p, wide, st);
   } else {
     const unsigned blocks = (unsigned)tiles(32, 32);
     if (wide)
