@@ -124,9 +124,9 @@ __device__ __forceinline__ void wait_sent() {  // all but the last N loads are t
   asm volatile("" ::: "memory");
 }
 
-// The scales, bias, activation and rounding of a wave's blocks, through LDS to whole lines.  acc[mb][nb]: tokens 32 mb,
-// channels 32 nb on; sa: the scales of this lane's tokens; sw: the channels' scales and, ws further, biases in LDS;
-// `stage`: LDS of this wave's own, 64 or 128 bytes a token.
+// The scales, bias, activation and rounding of a wave's blocks, 32 tokens at a time through LDS to whole lines.
+// acc[mb][nb]: tokens m0 + 32 mb, channels n0 + 32 nb on; sa: the scales of this lane's tokens; sw: the channels'
+// scales and, ws further, biases in LDS; `stage`: 4 KB of LDS of this wave's own.
 template <typename T, int SUM, int ACT, int MB, int NB>
 __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&acc)[MB][NB], long long m0, int n0,
                                        const float (&sa)[MB], const float* sw, int ws, uint8_t* stage) {
@@ -134,23 +134,24 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
   constexpr int PER = sizeof(T) == 2 && NB > 1 ? 2 : 1;     // blocks of channels a pass
   constexpr int ROW = PER * 32 * (int)sizeof(T);            // bytes of a token's row: 64 or 128
   constexpr int GR = ROW / 16;                              // granules of a row
+  constexpr int E = 16 / (int)sizeof(T);                    // values of a granule
 #pragma unroll
-  for (int pass = 0; pass < NB / PER; ++pass) {
+  for (int pass = 0; pass < NB / PER; ++pass)
 #pragma unroll
-    for (int q = 0; q < PER; ++q)
+    for (int mb = 0; mb < MB; ++mb) {
+      const int r = lane & 31;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int nb = pass * PER + q;
-        const float4 s4 = *(const float4*)(sw + 32 * nb + 8 * g + 4 * half);
-        const float4 b4 = *(const float4*)(sw + ws + 32 * nb + 8 * g + 4 * half);
-        const float s[4] = {s4.x, s4.y, s4.z, s4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
+      for (int q = 0; q < PER; ++q)
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
+        for (int g = 0; g < 4; ++g) {
+          const int nb = pass * PER + q;
+          const float4 s4 = *(const float4*)(sw + 32 * nb + 8 * g + 4 * half);
+          const float4 b4 = *(const float4*)(sw + ws + 32 * nb + 8 * g + 4 * half);
+          const float s[4] = {s4.x, s4.y, s4.z, s4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             v[e] = act_fn<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * s[e], sa[mb], b[e]));
-          const int r = 32 * mb + (lane & 31);
           if constexpr (sizeof(T) == 2) {
             const int at = r * ROW + (((4 * q + g) ^ (r >> 1 & (GR - 1))) << 4) + 8 * half;
             *(uint2*)(stage + at) = make_uint2(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]));
@@ -159,90 +160,110 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
             *(float4*)(stage + at) = make_float4(v[0], v[1], v[2], v[3]);
           }
         }
-      }
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's rows are in LDS
-    __builtin_amdgcn_wave_barrier();
-    constexpr int E = 16 / (int)sizeof(T);  // values of a granule
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's rows are in LDS
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < MB * GR / 2; ++i) {
-      const int c = lane + 64 * i, r = c / GR, g = c % GR;
-      const long long m = m0 + r;
-      const int n = n0 + 32 * PER * pass + g * E;
-      const uint4 w = *(const uint4*)(stage + r * ROW + ((g ^ (r >> 1 & (GR - 1))) << 4));
-      if (m < p.M && n < p.N) {
-        T* to = (T*)p.out + m * p.out_stride + n;
-        if (p.lines && n + E <= p.N) {
-          *(uint4*)to = w;
-        } else {
-          T v[E];
-          __builtin_memcpy(v, &w, 16);
+      for (int i = 0; i < GR / 2; ++i) {
+        const int c = lane + 64 * i, rr = c / GR, g = c % GR;
+        const long long m = m0 + 32 * mb + rr;
+        const int n = n0 + 32 * PER * pass + g * E;
+        const uint4 w = *(const uint4*)(stage + rr * ROW + ((g ^ (rr >> 1 & (GR - 1))) << 4));
+        if (m < p.M && n < p.N) {
+          T* to = (T*)p.out + m * p.out_stride + n;
+          if (p.lines && n + E <= p.N) {
+            *(uint4*)to = w;
+          } else {
+            T v[E];
+            __builtin_memcpy(v, &w, 16);
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (n + e < p.N) to[e] = v[e];
+            for (int e = 0; e < E; ++e)
+              if (n + e < p.N) to[e] = v[e];
+          }
         }
       }
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads are done before the next rows are written
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads are done before the next pass writes
-    __builtin_amdgcn_wave_barrier();
-  }
 }
 
-// This lane's tokens' scales, and N channels' scales and biases to LDS (complete after a barrier).
-template <int MB, int N>
-__device__ __forceinline__ void load_scales(const Mm& p, long long m0, int n0, float (&sa)[MB], float* sw) {
+// The scales and biases of a tile on their way: this lane's tokens', and channel threadIdx.x's.
+template <int MB>
+struct Scales {
+  float a[MB], w, bias;
+};
+template <int MB>
+__device__ __forceinline__ Scales<MB> load_scales(const Mm& p, long long m0, int n0) {
+  Scales<MB> s;
 #pragma unroll
-  for (int mb = 0; mb < MB; ++mb) sa[mb] = p.a_scales[min(m0 + 32 * mb + (threadIdx.x & 31), p.M - 1)];
+  for (int mb = 0; mb < MB; ++mb) s.a[mb] = p.a_scales[min(m0 + 32 * mb + (threadIdx.x & 31), p.M - 1)];
+  const int n = min(n0 + (int)threadIdx.x, p.N - 1);
+  s.w = p.w_scales[n];
+  s.bias = p.bias ? p.bias[n] : 0.0f;
+  return s;
+}
+template <int MB, int N>
+__device__ __forceinline__ void keep_scales(const Scales<MB>& s, float* sw) {  // complete after a barrier
   if (threadIdx.x < N) {
-    const int n = min(n0 + (int)threadIdx.x, p.N - 1);
-    sw[threadIdx.x] = p.w_scales[n];
-    sw[N + threadIdx.x] = p.bias ? p.bias[n] : 0.0f;
+    sw[threadIdx.x] = s.w;
+    sw[N + threadIdx.x] = s.bias;
   }
 }
 
-// 2 x WN waves of MB x NB blocks; BK codes of k a step, BUFS steps in LDS.
+// 2 x WN waves of MB x NB blocks; BK codes of k a step, BUFS steps in LDS.  With wide loads a workgroup takes several
+// tiles, and the loads run on into the next one: its first steps arrive while this one's results are written.
 template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS, bool WIDE>
 __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
   constexpr int BUF = (TM + TN) * BK;          // bytes of a step: tokens, then channels
   constexpr int SENDS = BUF / 1024 / (2 * WN);  // 1 KB pieces that a wave loads a step
-  constexpr int STAGE = 32 * MB * (sizeof(T) == 2 && NB == 1 ? 64 : 128);
-  constexpr int LDS = BUFS * BUF > 2 * WN * STAGE ? BUFS * BUF : 2 * WN * STAGE;
+  // results go through a buffer whose codes are used up, or, where it is too small, through LDS of their own
+  constexpr int STAGE = 32 * (sizeof(T) == 2 && NB == 1 ? 64 : 128);  // bytes of a wave's
+  constexpr bool OWN = 2 * WN * STAGE > BUF;
   constexpr int GR = BK / 16;                  // granules of a row
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[BUFS * BUF + (OWN ? 2 * WN * STAGE : 0)];
   __shared__ __attribute__((aligned(16))) float sw[2 * TN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroups are dealt to the eight XCDs in turn: an XCD takes neighbouring
-  // items, eight tiles of tokens by all channels, whose codes stay in its L2.
-  const unsigned items = gridDim.x, xcd = blockIdx.x & 7, per = items >> 3, rest = items & 7;
-  const unsigned item = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
-  const unsigned tiles_n = (p.N + TN - 1) / TN, tiles_m = items / tiles_n;
-  const unsigned band = item / (8 * tiles_n), in_band = item - band * 8 * tiles_n;
-  const unsigned high = min(8u, tiles_m - 8 * band);
-  const long long m0 = (long long)(8 * band + in_band % high) * TM;
-  const int n0 = (int)(in_band / high) * TN;
+  // tiles, bands of eight by all channels, whose codes stay in its L2.
+  const unsigned tiles_n = (p.N + TN - 1) / TN, tiles_m = (unsigned)((p.M + TM - 1) / TM), items = tiles_m * tiles_n;
+  const unsigned xcd = blockIdx.x & 7, per = items >> 3, rest = items & 7;
+  const unsigned first = xcd * per + min(xcd, rest), end = first + per + (xcd < rest);
+  const unsigned stride = (gridDim.x - xcd + 7) >> 3;  // workgroups of this XCD
+  auto place = [&](unsigned item, long long& m0, int& n0) {
+    const unsigned band = item / (8 * tiles_n), in_band = item - band * 8 * tiles_n;
+    const unsigned high = min(8u, tiles_m - 8 * band);
+    m0 = (long long)(8 * band + in_band % high) * TM;
+    n0 = (int)(in_band / high) * TN;
+  };
   const int wm = wave & 1, wn = wave >> 1;
   const int steps = (p.K + BK - 1) / BK;
-  float sa[MB];
-  load_scales<MB, TN>(p, m0 + wm * 32 * MB, n0, sa, sw);
 
   // Granule slot s of a step's buffer: row s / GR (tokens, then channels), and
   // granule (s % GR) ^ turn of its BK bytes: the 16 lanes that read at once
   // then fall on all banks.  A wave loads slots (wave SENDS + n) 64 + lane.
   auto turn_of = [](int row) { return BK == 64 ? row >> 2 & 3 : row >> 1 & 7; };
-  const uint8_t* const a0 = p.a + m0 * p.a_stride;
-  const uint8_t* const w0 = p.w + n0 * p.w_stride;
+  // the tile that loads are for
+  const uint8_t* a0;
+  const uint8_t* w0;
   uint32_t from[SENDS];  // byte offset of the slot's granule from the tile's first row, or in its row
   const uint8_t* rows[WIDE ? 1 : SENDS];
+  auto aim = [&](unsigned item) {
+    long long m0;
+    int n0;
+    place(item, m0, n0);
+    a0 = p.a + m0 * p.a_stride;
+    w0 = p.w + n0 * p.w_stride;
 #pragma unroll
-  for (int n = 0; n < SENDS; ++n) {
-    const int row = ((wave * SENDS + n) * 64 + lane) / GR, g = (lane & (GR - 1)) ^ turn_of(row);
-    const bool token = row < TM;  // uniform: whole rows a piece
-    const int r = token ? (int)min((long long)row, p.M - 1 - m0) : min(row - TM, p.N - 1 - n0);
-    if constexpr (WIDE)
-      from[n] = (uint32_t)r * (uint32_t)(token ? p.a_stride : p.w_stride) + g * 16;
-    else
-      from[n] = g * 16, rows[n] = token ? a0 + r * p.a_stride : w0 + r * p.w_stride;
-  }
+    for (int n = 0; n < SENDS; ++n) {
+      const int row = ((wave * SENDS + n) * 64 + lane) / GR, g = (lane & (GR - 1)) ^ turn_of(row);
+      const bool token = (wave * SENDS + n) * (1024 / BK) < TM;  // whole rows a piece
+      const int r = token ? (int)min((long long)row, p.M - 1 - m0) : min(row - TM, p.N - 1 - n0);
+      if constexpr (WIDE)
+        from[n] = (uint32_t)r * (uint32_t)(token ? p.a_stride : p.w_stride) + g * 16;
+      else
+        from[n] = g * 16, rows[n] = token ? a0 + r * p.a_stride : w0 + r * p.w_stride;
+    }
+  };
   const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
   auto send_step = [&](int step, int buf) {  // WIDE
     const int k0 = step * BK;
@@ -276,13 +297,6 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
   };
 
   typename Acc<SUM>::type acc[MB][NB];
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0;
-
   // this lane's row of a block, and granules 4 u + 2 half, + 1 of it
   const int turn = turn_of(lane & 31), h2 = lane >> 5 << 1;
   const int arow = (wm * 32 * MB + (lane & 31)) * BK, wrow = (TM + wn * 32 * NB + (lane & 31)) * BK;
@@ -309,22 +323,81 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
     }
   };
 
-  if constexpr (WIDE) {
+  auto clear = [&] {
 #pragma unroll
-    for (int s = 0; s < BUFS - 1; ++s)
-      if (s < steps) send_step(s, s);
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0;
+  };
+  auto results = [&](unsigned item, const Scales<MB>& s, int buf) {  // through LDS buffer `buf`
+    long long m0;
+    int n0;
+    place(item, m0, n0);
+    keep_scales<MB, TN>(s, sw);
+    __syncthreads();  // ... and all waves are done with the buffer
+    finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, s.a, sw + wn * 32 * NB, TN,
+                                lds + (OWN ? BUFS : buf) * BUF + wave * STAGE);
+  };
+  auto scales = [&](unsigned item) {
+    long long m0;
+    int n0;
+    place(item, m0, n0);
+    return load_scales<MB>(p, m0 + wm * 32 * MB, n0);
+  };
+
+  unsigned item = first + (blockIdx.x >> 3);
+  if (item >= end) return;
+  if constexpr (WIDE) {
+    static_assert(BUFS == 3, "two steps ahead");
+    unsigned next = item;  // the tile and the step that loads are for
+    int next_step = 0, next_buf = 0;
+    auto send_next = [&] {
+      if (next >= end) return;
+      if (next_step == 0) aim(next);
+      send_step(next_step, next_buf);
+      next_buf = next_buf == 2 ? 0 : next_buf + 1;
+      if (++next_step == steps) next_step = 0, next += stride;
+    };
+    if (steps > 0) {
+      send_next();
+      send_next();
+    }
     int buf = 0;
-    for (int step = 0; step < steps; ++step) {
-      if (BUFS == 2 || step + 1 >= steps)
-        wait_sent<0>();
-      else
-        wait_sent<SENDS>();
-      __syncthreads();  // step's codes are there for all; the buffer before it is read to the end
-      if (step + BUFS - 1 < steps) send_step(step + BUFS - 1, buf == 0 ? BUFS - 1 : buf - 1);
-      compute(buf);
-      buf = buf == BUFS - 1 ? 0 : buf + 1;
+    bool there = false;  // the step's loads have been waited for
+    for (; item < end; item += stride) {
+      const Scales<MB> s = scales(item);
+      clear();
+      for (int step = 0; step < steps; ++step) {
+        // all but the newest loads, those of the step after this one; the last of all has none behind it
+        if (!there) {
+          if (step + 1 < steps || item + stride < end)
+            wait_sent<SENDS>();
+          else
+            wait_sent<0>();
+        }
+        there = false;
+        __syncthreads();  // the step's codes are there for all; the buffer before it is read to the end
+        send_next();
+        compute(buf);
+        buf = buf == 2 ? 0 : buf + 1;
+      }
+      if (steps > 0 && item + stride < end) {
+        // wait for the next tile's first step before the stores are behind its loads
+        if (steps > 1 || item + 2 * stride < end)
+          wait_sent<SENDS>();
+        else
+          wait_sent<0>();
+        there = true;
+      }
+      results(item, s, buf == 0 ? 2 : buf - 1);
+      if (steps == 0) __syncthreads();  // the scales' LDS is read to the end
     }
   } else {
+    const Scales<MB> s = scales(item);
+    clear();
+    aim(item);
     if (steps > 0) {
       load_step(0);
       store_step(0);
@@ -337,9 +410,9 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
       buf = buf == BUFS - 1 ? 0 : buf + 1;
       if (step + 1 < steps) store_step(buf);
     }
+    __syncthreads();
+    results(item, s, 0);
   }
-  __syncthreads();
-  finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, sa, sw + wn * 32 * NB, TN, lds + wave * STAGE);
 }
 
 // 32 tokens x 32 channels a workgroup of eight waves, each with every eighth step of k, straight from memory.
@@ -347,7 +420,7 @@ template <typename T, int SUM, int ACT, bool WIDE>
 __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
   constexpr int W = 8;
   __shared__ __attribute__((aligned(16))) typename Acc<SUM>::type sums[W / 2][64];
-  __shared__ __attribute__((aligned(16))) uint8_t stage[32 * 128];
+  __shared__ __attribute__((aligned(16))) uint8_t stage[4096];
   __shared__ __attribute__((aligned(16))) float sw[2 * 32];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const int tiles_n = (p.N + 31) / 32;
@@ -357,8 +430,8 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
   const int rw = min(n0 + (lane & 31), p.N - 1);
   const uint8_t* const pa = p.a + ra * p.a_stride;
   const uint8_t* const pw = p.w + rw * p.w_stride;
-  float sa[1];
-  load_scales<1, 32>(p, m0, n0, sa, sw);
+  const Scales<1> s = load_scales<1>(p, m0, n0);
+  keep_scales<1, 32>(s, sw);
   typename Acc<SUM>::type acc[1][1];
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[0][0][e] = 0;
@@ -383,17 +456,19 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
     }
     __syncthreads();
   }
-  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, sa, sw, 32, stage);
+  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, s.a, sw, 32, stage);
 }
 
 template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS>
 void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
-  const unsigned blocks = (unsigned)(((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN));
+  const unsigned items = (unsigned)(((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN));
+  const unsigned most = 256 * (MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4);  // workgroups that the card holds at once
   if (wide)
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true>), dim3(blocks), dim3(128 * WN), 0, st, p);
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true>), dim3(items < most ? items : most),
+                       dim3(128 * WN), 0, st, p);
   else
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, false>), dim3(blocks), dim3(128 * WN), 0, st, p);
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, false>), dim3(items), dim3(128 * WN), 0, st, p);
 }
 
 template <typename T, int SUM, int ACT>
@@ -401,6 +476,8 @@ void launch(const Mm& p, bool wide, hipStream_t st) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
   if (tiles(256, 128) >= 384) {
     launch_tiles<T, SUM, ACT, 4, 2, 2, 64, 3>(p, wide, st);
+  } else if (tiles(128, 128) >= 256) {
+    launch_tiles<T, SUM, ACT, 2, 2, 2, 64, 3>(p, wide, st);
   } else if (tiles(64, 64) >= 192) {
     launch_tiles<T, SUM, ACT, 1, 1, 2, 64, 3>(p, wide, st);
   } else {
