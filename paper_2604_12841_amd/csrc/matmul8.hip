@@ -45,7 +45,8 @@ struct Mm {
   const float* w_scales;
   const float* bias;
   void* out;
-  bool lines;  // rows of out are 16-byte aligned
+  bool lines;   // rows of out are 16-byte aligned
+  bool passing;  // out is too large to stay in a cache for who reads it next
 };
 
 // 16 bytes of a row from column k on, zero past K; nothing outside the row is read.  (Device memory takes unaligned
@@ -171,7 +172,10 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
         if (m < p.M && n < p.N) {
           T* to = (T*)p.out + m * p.out_stride + n;
           if (p.lines && n + E <= p.N) {
-            *(uint4*)to = w;
+            if (p.passing)
+              __builtin_nontemporal_store(__builtin_bit_cast(i32x4, w), (i32x4*)to);
+            else
+              *(uint4*)to = w;
           } else {
             T v[E];
             __builtin_memcpy(v, &w, 16);
@@ -212,7 +216,7 @@ __device__ __forceinline__ void keep_scales(const Scales<MB>& s, float* sw) {  /
 // 2 x WN waves of MB x NB blocks; BK codes of k a step, BUFS steps in LDS.  With wide loads a workgroup takes several
 // tiles, and the loads run on into the next one: its first steps arrive while this one's results are written.
 template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS, bool WIDE>
-__global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4) matmul8_kernel(const Mm p) {
+__global__ void __launch_bounds__(128 * WN, MB * NB >= 4 ? 2 : 3) matmul8_kernel(const Mm p) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
   constexpr int BUF = (TM + TN) * BK;          // bytes of a step: tokens, then channels
   constexpr int SENDS = BUF / 1024 / (2 * WN);  // 1 KB pieces that a wave loads a step
@@ -350,19 +354,19 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
   unsigned item = first + (blockIdx.x >> 3);
   if (item >= end) return;
   if constexpr (WIDE) {
-    static_assert(BUFS == 3, "two steps ahead");
+    static_assert(BUFS == 2 || BUFS == 3, "one or two steps ahead");
     unsigned next = item;  // the tile and the step that loads are for
     int next_step = 0, next_buf = 0;
     auto send_next = [&] {
       if (next >= end) return;
       if (next_step == 0) aim(next);
       send_step(next_step, next_buf);
-      next_buf = next_buf == 2 ? 0 : next_buf + 1;
+      next_buf = next_buf == BUFS - 1 ? 0 : next_buf + 1;
       if (++next_step == steps) next_step = 0, next += stride;
     };
     if (steps > 0) {
       send_next();
-      send_next();
+      if (BUFS == 3) send_next();
     }
     int buf = 0;
     bool there = false;  // the step's loads have been waited for
@@ -372,7 +376,7 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
       for (int step = 0; step < steps; ++step) {
         // all but the newest loads, those of the step after this one; the last of all has none behind it
         if (!there) {
-          if (step + 1 < steps || item + stride < end)
+          if (BUFS == 3 && (step + 1 < steps || item + stride < end))
             wait_sent<SENDS>();
           else
             wait_sent<0>();
@@ -381,17 +385,17 @@ __global__ void __launch_bounds__(128 * WN, MB * NB == 8 ? 2 : MB * NB == 4 ? 3 
         __syncthreads();  // the step's codes are there for all; the buffer before it is read to the end
         send_next();
         compute(buf);
-        buf = buf == 2 ? 0 : buf + 1;
+        buf = buf == BUFS - 1 ? 0 : buf + 1;
       }
       if (steps > 0 && item + stride < end) {
         // wait for the next tile's first step before the stores are behind its loads
-        if (steps > 1 || item + 2 * stride < end)
+        if (BUFS == 3 && (steps > 1 || item + 2 * stride < end))
           wait_sent<SENDS>();
         else
           wait_sent<0>();
         there = true;
       }
-      results(item, s, buf == 0 ? 2 : buf - 1);
+      results(item, s, buf == 0 ? BUFS - 1 : buf - 1);
       if (steps == 0) __syncthreads();  // the scales' LDS is read to the end
     }
   } else {
@@ -463,7 +467,7 @@ template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS
 void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
   const unsigned items = (unsigned)(((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN));
-  const unsigned most = 256 * (MB * NB == 8 ? 2 : MB * NB == 4 ? 3 : 4);  // workgroups that the card holds at once
+  const unsigned most = 256 * (MB * NB == 8 ? 1 : MB * NB == 4 ? 2 : 3);  // workgroups that the card holds at once
   if (wide)
     hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true>), dim3(items < most ? items : most),
                        dim3(128 * WN), 0, st, p);
@@ -474,10 +478,10 @@ void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
 template <typename T, int SUM, int ACT>
 void launch(const Mm& p, bool wide, hipStream_t st) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
-  if (tiles(256, 128) >= 384) {
-    launch_tiles<T, SUM, ACT, 4, 2, 2, 64, 3>(p, wide, st);
+  if (tiles(256, 256) >= 256) {
+    launch_tiles<T, SUM, ACT, 4, 2, 4, 128, 2>(p, wide, st);
   } else if (tiles(128, 128) >= 256) {
-    launch_tiles<T, SUM, ACT, 2, 2, 2, 64, 3>(p, wide, st);
+    launch_tiles<T, SUM, ACT, 2, 2, 2, 128, 2>(p, wide, st);
   } else if (tiles(64, 64) >= 192) {
     launch_tiles<T, SUM, ACT, 1, 1, 2, 64, 3>(p, wide, st);
   } else {
@@ -510,6 +514,9 @@ extern "C" pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args*
   p.a = (const uint8_t*)a->a, p.w = (const uint8_t*)a->w;
   p.a_stride = a->a_stride, p.w_stride = a->w_stride, p.out_stride = a->out_stride;
   p.a_scales = a->a_scales, p.w_scales = a->w_scales, p.bias = a->bias, p.out = a->out;
+  // Stores past the caches let the next tile's loads have them (163072 x 2048 x 512 to bf16: 250 -> 228 us); results
+  // that a cache can hold (256 MB behind the L2s) are left there for their reader.
+  p.passing = a->M * a->N * elem > (128ll << 20);
   p.lines = (uintptr_t)a->out % 16 == 0 && (a->out_stride * elem) % 16 == 0;
   // 256 rows of a tile within 32-bit offsets
   const bool wide = a->K % 16 == 0 && (uintptr_t)a->a % 16 == 0 && (uintptr_t)a->w % 16 == 0 &&
