@@ -8,6 +8,7 @@ A token is one site of one round of a volume.  Its place is a row (t, i, j, volu
 volume < 0 marks a row that holds no token.
 """
 import ctypes
+import struct
 
 import torch
 
@@ -62,7 +63,7 @@ _fn = None
 
 
 def _functions():
-    """The library's functions with their argument types, looked up once."""
+    """The library's functions, taking the structures above; looked up once."""
     global _fn
     if _fn is None:
         L = lib()
@@ -76,19 +77,47 @@ def _functions():
     return _fn
 
 
-def _raw_stream(stream, device):
+# A small call's time is the host's: arguments are packed by struct (the structures' layout, native alignment), a third
+# of the time that filling a ctypes structure takes, and handed over by functions that take the bytes.
+_FORMAT = {_i64: "q", _i32: "i", _f32: "f", ctypes.c_double: "d", _vp: "P", ctypes.c_size_t: "N", _i32 * 3: "3i"}
+
+
+def _packer(args):
+    s = struct.Struct("@" + "".join(_FORMAT[f[1]] for f in args._fields_))
+    assert s.size <= ctypes.sizeof(args) < s.size + 8  # (no padding at the end)
+    return s.pack
+
+
+_pack_norm, _pack_matmul8 = _packer(NormArgs), _packer(Matmul8Args)
+_pack_rope, _pack_attention = _packer(RopeArgs), _packer(AttentionArgs)
+_fast = {}
+
+
+def _by_bytes(name):
+    """The library's function `name`, taking packed arguments."""
+    f = _fast.get(name)
+    if f is None:
+        f = lib()[name]
+        work = name == "predecoder_attention_workspace"
+        f.argtypes = [ctypes.c_char_p] if work else [_vp, ctypes.c_char_p]
+        f.restype = ctypes.c_size_t if work else _i32
+        _fast[name] = f
+    return f
+
+
+def _raw_stream(stream, index):
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _call(name, args, stream, device):
-    f = getattr(_functions(), name)
-    if device.index == torch.cuda.current_device():
-        st = f(_raw_stream(stream, device), args)
+def _call(name, args, stream, index):
+    f = _by_bytes(name)
+    if index == torch.cuda.current_device():
+        st = f(_raw_stream(stream, index), args)
     else:
-        with torch.cuda.device(device):
-            st = f(_raw_stream(stream, device), args)
+        with torch.cuda.device(index):
+            st = f(_raw_stream(stream, index), args)
     if st != PD_OK:
         raise PredecoderError(st, name)
 
@@ -98,30 +127,38 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _matrix(t, what, shape, dtype, device):
-    """Pointer and row stride of a device matrix with contiguous rows; (None, 0) for None."""
+def _index(t, what):
+    """The index of the GPU that a tensor is on."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError("%s must be a tensor on the GPU" % what)
+    return index
+
+
+def _matrix(t, what, shape, dtype, index):
+    """Pointer and row stride of a device matrix with contiguous rows; zeros for None."""
     if t is None:
-        return None, 0
-    if t.device != device or not t.is_cuda:
-        raise ValueError("%s must be a tensor on %s" % (what, device if device.type == "cuda" else "the GPU"))
+        return 0, 0
+    if t.get_device() != index:
+        raise ValueError("%s must be a tensor on GPU %d" % (what, index))
     if t.dtype != dtype:
         raise ValueError("%s has type %s, expected %s" % (what, t.dtype, dtype))
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
-    s = t.stride()
-    if s[1] != 1 and shape[1] > 1:
+    stride, one = t.stride()
+    if one != 1 and shape[1] > 1:
         raise ValueError("the rows of %s must be contiguous" % what)
-    return t.data_ptr(), s[0]
+    return t.data_ptr(), stride
 
 
-def _vector(t, what, n, dtype, device):
-    """Pointer of a contiguous device vector of n values; None for None."""
+def _vector(t, what, n, index):
+    """Pointer of a contiguous device vector of n float32 values; 0 for None."""
     if t is None:
-        return None
-    if t.device != device or not t.is_cuda:
-        raise ValueError("%s must be a tensor on %s" % (what, device if device.type == "cuda" else "the GPU"))
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous vector of %d values of type %s" % (what, n, dtype))
+        return 0
+    if t.get_device() != index:
+        raise ValueError("%s must be a tensor on GPU %d" % (what, index))
+    if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d float32 values" % (what, n))
     return t.data_ptr()
 
 
@@ -131,21 +168,23 @@ def rms_norm(x, gain=None, eps=1e-6, residual=None, sum_out=None, out=None, code
     Writes what is given of: sum_out (s), out (y; both of x's type), codes [rows][width] (float8_e4m3fn or int8)
     with scales [rows]: y / scale rounded, scale = max |y| / 448 or / 127."""
     _need(x.dim() == 2, "x must be a matrix")
-    _need(x.dtype in _VALUES, "x must be bfloat16 or float32")
-    _need(codes is None or codes.dtype in _CODES, "codes must be float8_e4m3fn or int8")
+    dt, shape, dev = x.dtype, x.shape, _index(x, "x")
+    _need(dt in _VALUES, "x must be bfloat16 or float32")
     _need((codes is None) == (scales is None), "codes and scales go together")
     _need(sum_out is not None or out is not None or codes is not None, "no output is given")
-    shape, dt, dev = x.shape, x.dtype, x.device
     rows, width = shape
     px, sx = _matrix(x, "x", shape, dt, dev)
     pr, sr = _matrix(residual, "residual", shape, dt, dev)
     ps, ss = _matrix(sum_out, "sum_out", shape, dt, dev)
     po, so = _matrix(out, "out", shape, dt, dev)
-    ct = CODES_NONE if codes is None else _CODES[codes.dtype]
-    pc, sc = _matrix(codes, "codes", shape, codes.dtype if codes is not None else None, dev)
-    a = NormArgs(rows, width, _VALUES[dt], ct, eps, px, sx, pr, sr, _vector(gain, "gain", width, torch.float32, dev), ps,
-                 ss, po, so, pc, sc, _vector(scales, "scales", rows, torch.float32, dev))
-    _call("predecoder_rms_norm", a, stream, dev)
+    ct = pc = sc = CODES_NONE
+    if codes is not None:
+        _need(codes.dtype in _CODES, "codes must be float8_e4m3fn or int8")
+        ct = _CODES[codes.dtype]
+        pc, sc = _matrix(codes, "codes", shape, codes.dtype, dev)
+    _call("predecoder_rms_norm", _pack_norm(rows, width, _VALUES[dt], ct, eps, px, sx, pr, sr,
+                                            _vector(gain, "gain", width, dev), ps, ss, po, so, pc, sc,
+                                            _vector(scales, "scales", rows, dev)), stream, dev)
 
 
 def matmul8(a, a_scales, w, w_scales, out, bias=None, act="none", stream=None):
@@ -154,35 +193,34 @@ def matmul8(a, a_scales, w, w_scales, out, bias=None, act="none", stream=None):
     a [M][K] and w [N][K]: 8-bit codes of one type (float8_e4m3fn or int8); scales and bias float32; act "none", "gelu" or
     "relu" (or an ACT_ constant); out [M][N] bfloat16 or float32."""
     _need(a.dim() == 2 and w.dim() == 2, "a and w must be matrices")
-    _need(a.dtype in _CODES, "a must be float8_e4m3fn or int8")
-    _need(out.dtype in _VALUES, "out must be bfloat16 or float32")
+    dt, to, dev = a.dtype, out.dtype, _index(a, "a")
+    _need(dt in _CODES, "a must be float8_e4m3fn or int8")
+    _need(to in _VALUES, "out must be bfloat16 or float32")
     M, K = a.shape
     N = w.shape[0]
-    dev = a.device
-    pa, sa = _matrix(a, "a", (M, K), a.dtype, dev)
-    pw, sw = _matrix(w, "w", (N, K), a.dtype, dev)
-    po, so = _matrix(out, "out", (M, N), out.dtype, dev)
+    pa, sa = _matrix(a, "a", (M, K), dt, dev)
+    pw, sw = _matrix(w, "w", (N, K), dt, dev)
+    po, so = _matrix(out, "out", (M, N), to, dev)
     code = _ACTS[act] if isinstance(act, str) else int(act)
-    args = Matmul8Args(M, N, K, _CODES[a.dtype], _VALUES[out.dtype], code, pa, sa,
-                       _vector(a_scales, "a_scales", M, torch.float32, dev), pw, sw,
-                       _vector(w_scales, "w_scales", N, torch.float32, dev),
-                       _vector(bias, "bias", N, torch.float32, dev), po, so)
-    _call("predecoder_matmul8", args, stream, dev)
+    _call("predecoder_matmul8", _pack_matmul8(M, N, K, _CODES[dt], _VALUES[to], code, pa, sa,
+                                              _vector(a_scales, "a_scales", M, dev), pw, sw,
+                                              _vector(w_scales, "w_scales", N, dev), _vector(bias, "bias", N, dev),
+                                              po, so), stream, dev)
 
 
-def _sites(t, what, n, device, batch=None):
+def _sites(t, what, n, index, batch=None):
     """Pointer and batch stride (in sites) of int32 sites [n][4] or, with a batch, [batch][n][4]."""
-    _need(t.is_cuda and t.device == device, "%s must be a tensor on %s" % (what, device))
-    _need(t.dtype == torch.int32, "%s must be int32" % what)
-    shape = tuple(t.shape)
-    _need(shape == (n, 4) or (batch is not None and shape == (batch, n, 4)),
-          "%s has shape %s, expected %s" % (what, shape, (n, 4)))
-    s = t.stride()
-    _need(n == 0 or (s[-1] == 1 and (n == 1 or s[-2] == 4)), "%s must be contiguous" % what)
-    if t.dim() == 2:
+    if t.get_device() != index or t.dtype != torch.int32:
+        raise ValueError("%s must be an int32 tensor on GPU %d" % (what, index))
+    shape, s = t.shape, t.stride()
+    if shape != (n, 4) and (batch is None or shape != (batch, n, 4)):
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(shape), (n, 4)))
+    if n and (s[-1] != 1 or (n > 1 and s[-2] != 4)):
+        raise ValueError("%s must be contiguous" % what)
+    if len(shape) == 2 or batch == 1:
         return t.data_ptr(), 0
-    _need(batch == 1 or s[0] % 4 == 0, "%s must hold whole sites from entry to entry" % what)
-    return t.data_ptr(), s[0] // 4 if batch > 1 else 0
+    _need(s[0] % 4 == 0, "%s must hold whole sites from entry to entry" % what)
+    return t.data_ptr(), s[0] // 4
 
 
 def rope(x, sites, out, sections, base=10000.0, interleaved=False, inverse=False, stream=None):
@@ -190,50 +228,50 @@ def rope(x, sites, out, sections, base=10000.0, interleaved=False, inverse=False
 
     sections: pairs of a head that turn with the round, the row and the column; pair k of n turns by base^(-k/n) a step.
     A pair is values m and m + head_dim / 2, or 2 m and 2 m + 1 if interleaved.  inverse turns back."""
-    _need(x.dim() == 3 and out.dim() == 3, "x and out must be [tokens][heads][head_dim]")
-    _need(x.dtype in _VALUES and out.dtype == x.dtype, "x and out must both be bfloat16 or both float32")
-    _need(x.shape == out.shape, "x and out differ in shape")
-    _need(x.is_cuda and out.device == x.device, "x and out must be tensors on one GPU")
-    n, H, D = x.shape
-    sx, so = x.stride(), out.stride()
-    _need(D <= 1 or (sx[2] == 1 and so[2] == 1), "the rows of a head must be contiguous")
-    ps, _ = _sites(sites, "sites", n, x.device)
-    a = RopeArgs(n, H, D, _VALUES[x.dtype], (_i32 * 3)(*sections), int(interleaved), int(inverse), base, ps,
-                 x.data_ptr(), sx[0], sx[1], out.data_ptr(), so[0], so[1])
-    _call("predecoder_rope", a, stream, x.device)
+    dt, shape, dev = x.dtype, x.shape, _index(x, "x")
+    _need(len(shape) == 3 and out.shape == shape, "x and out must be [tokens][heads][head_dim] of one shape")
+    _need(dt in _VALUES and out.dtype == dt, "x and out must both be bfloat16 or both float32")
+    _need(out.get_device() == dev, "x and out must be tensors on one GPU")
+    n, H, D = shape
+    xt, xh, x1 = x.stride()
+    ot, oh, o1 = out.stride()
+    _need(D <= 1 or (x1 == 1 and o1 == 1), "the rows of a head must be contiguous")
+    s0, s1, s2 = sections
+    _call("predecoder_rope", _pack_rope(n, H, D, _VALUES[dt], s0, s1, s2, bool(interleaved), bool(inverse), base,
+                                        _sites(sites, "sites", n, dev)[0], x.data_ptr(), xt, xh, out.data_ptr(), ot, oh),
+          stream, dev)
 
 
 def _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix):
     """The arguments of predecoder_attention for these tensors, without a workspace."""
     _need(q.dim() == 4 and k.dim() == 4, "q and k must be [batch][tokens][heads][head_dim]")
-    B, nq, H, D = q.shape
-    nk, Hk = k.shape[1], k.shape[2]
-    dev = q.device
+    shape, dev = q.shape, _index(q, "q")
+    B, nq, H, D = shape
+    _, nk, Hk, _ = k.shape
     fields = []
-    for t, what, shape in ((q, "q", q.shape), (k, "k", (B, nk, Hk, D)), (v, "v", (B, nk, Hk, D)), (out, "out", q.shape)):
-        if not t.is_cuda or t.device != dev or t.dtype != torch.bfloat16 or t.shape != shape:
-            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(shape)))
-        s = t.stride()
-        if s[3] != 1 and D > 1:
+    for t, what, want in ((q, "q", shape), (k, "k", (B, nk, Hk, D)), (v, "v", (B, nk, Hk, D)), (out, "out", shape)):
+        if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != want:
+            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(want)))
+        sb, st, sh, one = t.stride()
+        if one != 1 and D > 1:
             raise ValueError("the rows of a head must be contiguous in %s" % what)
-        fields += [t.data_ptr(), s[0], s[1], s[2]]
+        fields += (t.data_ptr(), sb, st, sh)
     _need((q_sites is None) == (k_sites is None), "q_sites and k_sites go together")
-    pq = pk = None
-    bq = bk = 0
+    pq = pk = bq = bk = 0
     if q_sites is not None:
         pq, bq = _sites(q_sites, "q_sites", nq, dev, B)
         pk, bk = _sites(k_sites, "k_sites", nk, dev, B)
     if scale is None:
         scale = D ** -0.5
-    return AttentionArgs(B, H, Hk, D, nq, nk, scale, cap, int(causal), int(prefix), *fields, pq, bq, pk, bk,
-                         _vector(slopes, "slopes", H, torch.float32, dev), None, 0)
+    return (B, H, Hk, D, nq, nk, scale, cap, bool(causal), int(prefix), *fields, pq, bq, pk, bk,
+            _vector(slopes, "slopes", H, dev))
 
 
 def attention_workspace(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slopes=None, causal=False,
                         prefix=0):
     """Bytes of workspace of attention() with these arguments."""
     a = _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix)
-    return int(_functions().predecoder_attention_workspace(a))
+    return _by_bytes("predecoder_attention_workspace")(_pack_attention(*a, 0, 0))
 
 
 def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slopes=None, causal=False, prefix=0,
@@ -245,20 +283,23 @@ def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slo
     below prefix.  sites: [n][4] for all batch entries or [batch][n][4].  workspace: a device tensor of at least
     attention_workspace() bytes (needed with a raw stream handle; otherwise allocated here)."""
     a = _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix)
-    need = _functions().predecoder_attention_workspace(a)
+    dev = q.get_device()
+    ptr = 0
     if workspace is not None:
-        _need(workspace.is_cuda and workspace.device == q.device and workspace.is_contiguous(),
+        _need(workspace.get_device() == dev and workspace.is_contiguous(),
               "workspace must be a contiguous tensor on the GPU of q")
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    elif need:
-        if stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        else:
-            _need(isinstance(stream, torch.cuda.Stream), "a raw stream handle needs a workspace from the caller")
-            with torch.cuda.stream(stream):  # its memory goes back to the stream that uses it
+        ptr, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = _by_bytes("predecoder_attention_workspace")(_pack_attention(*a, 0, 0))
+        if need:
+            if stream is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), need
-    _call("predecoder_attention", a, stream, q.device)
+            else:
+                _need(isinstance(stream, torch.cuda.Stream), "a raw stream handle needs a workspace from the caller")
+                with torch.cuda.stream(stream):  # its memory goes back to the stream that uses it
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            ptr = workspace.data_ptr()
+    _call("predecoder_attention", _pack_attention(*a, ptr, need), stream, dev)
 
 
 def volume_sites(d, T, volume=0, first_round=0, layout="plaquette", device="cuda"):
