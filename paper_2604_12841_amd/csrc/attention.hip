@@ -38,6 +38,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 64;  // keys of a noted tile
+// tanh u for |u| <= 0.35 is u (TANH1 + u^2 (TANH3 + u^2 TANH5)) within 4.9e-7 (fitted for the least largest error)
+constexpr float TANH1 = 0.9999902f, TANH3 = -0.33268409f, TANH5 = 0.12248027f;
 
 // What a tile of keys holds: the range of volumes and of rounds over its tokens (vmin > vmax: none).
 struct Tile {
@@ -57,6 +59,7 @@ struct Attn {
   int causal;
   float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
   float cap_a, cap_b;
+  float small, poly1, poly3, poly5;  // |q.k| <= small: z = x (poly1 + x^2 (poly3 + x^2 poly5)) is the cap
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
@@ -92,15 +95,20 @@ __device__ __forceinline__ uint32_t site_bytes(const int4 s) {
   return (uint32_t)(s.x & 255) | (uint32_t)(s.y & 255) << 8 | (uint32_t)(s.z & 255) << 16;
 }
 
+// The smallest / largest value of a wave's lanes: inside rows of 16 lanes, then from row to row up to lane 63.
+template <int CTRL>
+__device__ __forceinline__ int moved(int v) {
+  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = min(v, __shfl_xor(v, m));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = min(v, moved<0x111>(v)), v = min(v, moved<0x112>(v)), v = min(v, moved<0x114>(v)), v = min(v, moved<0x118>(v));
+  v = min(v, moved<0x142>(v)), v = min(v, moved<0x143>(v));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = max(v, __shfl_xor(v, m));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = max(v, moved<0x111>(v)), v = max(v, moved<0x112>(v)), v = max(v, moved<0x114>(v)), v = max(v, moved<0x118>(v));
+  v = max(v, moved<0x142>(v)), v = max(v, moved<0x143>(v));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 __device__ __forceinline__ bool in_byte(int v) { return (v & ~255) == 0; }
@@ -156,7 +164,7 @@ __device__ __forceinline__ int v_place(int key, int g) {
 }
 
 template <int DP, int NW, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) attention_kernel(const Attn p) {
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW == 2 && DP < 128 ? 2 : 1) attention_kernel(const Attn p) {
   constexpr int TK = NW == 1 ? 32 : 64;       // keys of a step
   constexpr int NT = NW * 64, ROWS = NW * 32;
   constexpr int STEPS = TILE / TK;            // steps of a noted tile
@@ -301,6 +309,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         int4 s = make_int4(0, 0, 0, lane <= most_key ? 0 : -1);
         if (sites && lane <= most_key) s = sites[k0 + lane];
         ls[buf][lane] = ordered(s);
+        lb[buf][lane] = site_bytes(s);
       }
     }
     if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0 + lane, lb[buf]);
@@ -356,7 +365,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
           z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z[n], 0, 0, 0);
         }
       }
-      const float off = (CAP ? p.cap_b : 0.0f) - top;
+      const float off = (CAP ? p.cap_b : 0.0f) - top, off_small = -top;
       auto capped = [&](float x, float t) {
         if constexpr (CAP)
           return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * p.c1)), t);
@@ -373,13 +382,28 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
         const float t = BIAS ? fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)dist), slope * 0x1p24f, off) : off;
         return capped(x, t);
       };
+      // the same where no score of the wave's tile exceeds 0.35 of the cap: four instructions instead of five, of which
+      // two run at half rate
+      auto score_small = [&](float x, uint32_t dist) {
+        const float t = BIAS ? fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)dist), slope * 0x1p24f, off_small) : off_small;
+        const float w = x * x;
+        return fmaf(x, fmaf(w, fmaf(w, p.poly5, p.poly3), p.poly1), t);
+      };
       float most = -INFINITY;
-      const bool whole = notes ? !(note.flags & HOLES) && w_plain && note.vmin == note.vmax && note.vmin == wv_min &&
-                                     (!p.causal || note.tmax <= wt_min || note.tmax <= p.prefix_last) &&
-                                     (!BIAS || (w_bytes && (note.flags & BYTES) && (note.tmin >> 8) == (wt_min >> 8) &&
-                                                (note.tmax >> 8) == (wt_min >> 8)))
-                               : !p.k_sites && (tile + 1) * TILE <= p.n_k;
-      if (whole) {
+      bool whole;  // every row sees every key, and the bytes give the distances
+      if (notes) {
+        whole = !(note.flags & HOLES) && w_plain && note.vmin == note.vmax && note.vmin == wv_min &&
+                (!p.causal || note.tmax <= wt_min || note.tmax <= p.prefix_last) &&
+                (!BIAS || (w_bytes && (note.flags & BYTES) && (note.tmin >> 8) == (wt_min >> 8) &&
+                           (note.tmax >> 8) == (wt_min >> 8)));
+      } else {
+        const uint4 s = ls[buf][lane & (TK - 1)];
+        const uint32_t t0 = (uint32_t)wt_min ^ 0x80000000u, seen_by_all = p.causal ? (uint32_t)max(wt_min, p.prefix_last) ^ 0x80000000u : ~0u;
+        whole = w_plain && __all(s.w == (uint32_t)wv_min && s.x <= seen_by_all &&
+                                 (!BIAS || ((s.x ^ t0) < 256u && (s.y ^ 0x80000000u) < 256u && (s.z ^ 0x80000000u) < 256u)));
+        if (BIAS && !w_bytes) whole = false;
+      }
+      auto scores = [&](auto&& score_of) {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -389,12 +413,26 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float x = score_near(z[n][4 * g + e], BIAS ? __builtin_amdgcn_sad_u8(u[e], at_bytes, 0) : 0);
+              const float x = score_of(z[n][4 * g + e], BIAS ? __builtin_amdgcn_sad_u8(u[e], at_bytes, 0) : 0);
               z[n][4 * g + e] = x;
               most = fmaxf(most, x);
             }
-            __builtin_amdgcn_sched_barrier(0);
           }
+      };
+      if (whole) {
+        if constexpr (CAP) {
+          float size = 0.0f;
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) size = fmaxf(fmaxf(size, fabsf(z[n][e])), fabsf(z[n][e + 1]));
+          if (__any(size > p.small))
+            scores(score_near);
+          else
+            scores(score_small);
+        } else {
+          scores(score_near);
+        }
       } else {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -410,9 +448,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 128 ? 2 : 3) atte
             if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four keys' sites in registers at a time
           }
       }
-      most = fmaxf(most, __shfl_xor(most, 32));
-      const bool raise = most > 8.0f || (unset && most > -INFINITY);
-      if (__any(raise)) {
+      if (__any(most > 8.0f || (unset && most > -INFINITY))) {
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const bool raise = most > 8.0f || (unset && most > -INFINITY);
         const float up = raise ? most : 0.0f;
         const float alpha = raise && !unset ? __builtin_amdgcn_exp2f(-up) : 1.0f;
         if (raise) unset = false;
@@ -595,7 +633,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
 
 // How a call runs.
 struct Plan {
-  int waves;  // of a workgroup: 1 or 4
+  int waves;  // of a workgroup: 1, 2 or 4
   int row_tiles, tiles, splits, tiles_per_split;
   bool notes;
   size_t notes_bytes, bytes_bytes, sites_bytes, o_bytes, ml_bytes;
@@ -605,7 +643,9 @@ struct Plan {
 Plan plan_for(const pd_attention_args* a) {
   Plan n = {};
   const long long group = a->heads / a->kv_heads, rows = a->n_q * group;
-  n.waves = rows <= 64 ? 1 : 4;
+  // workgroups of 64 rows where those of 128 would leave over a tenth of their rows empty
+  const long long full4 = (rows + 127) / 128 * 128, full2 = (rows + 63) / 64 * 64;
+  n.waves = rows <= 32 ? 1 : 10 * (full4 - full2) > full4 ? 2 : 4;
   n.row_tiles = (int)((rows + 32 * n.waves - 1) / (32 * n.waves));
   n.tiles = (int)(((long long)a->n_k + TILE - 1) / TILE);
   // up to four tiles are read whole: the notes' launch would cost more than it saves
@@ -693,6 +733,8 @@ template <int DP>
 void launch_width(const Attn& p, const Plan& n, bool cap, bool bias, hipStream_t st) {
   if (n.waves == 1)
     launch<DP, 1>(p, cap, bias, (unsigned)n.items, st);
+  else if (n.waves == 2)
+    launch<DP, 2>(p, cap, bias, (unsigned)n.items, st);
   else
     launch<DP, 4>(p, cap, bias, (unsigned)n.items, st);
   if (p.splits > 1)
@@ -713,6 +755,13 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
   p.prefix_last = a->prefix - 1, p.causal = a->causal;
   p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / a->cap : a->scale * LOG2E;
+  if (a->cap > 0.0f) {
+    const float u = a->scale / a->cap, c = a->cap * LOG2E;
+    p.small = 0.35f / fabsf(u);
+    p.poly1 = c * u * TANH1, p.poly3 = c * u * u * u * TANH3, p.poly5 = c * u * u * u * u * u * TANH5;
+  } else {
+    p.small = p.poly1 = p.poly3 = p.poly5 = 0.0f;
+  }
   p.cap_a = -2.0f * a->cap * LOG2E, p.cap_b = a->cap * LOG2E;
   p.q = (const uint16_t*)a->q, p.k = (const uint16_t*)a->k, p.v = (const uint16_t*)a->v, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;

@@ -113,7 +113,7 @@ def _raw_stream(stream, index):
 
 def _call(name, args, stream, index):
     f = _by_bytes(name)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         st = f(_raw_stream(stream, index), args)
     else:
         with torch.cuda.device(index):
