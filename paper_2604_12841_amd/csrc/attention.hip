@@ -587,48 +587,54 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
 }
 
 // Joins the splits of one row: out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
-// DP / 4 lanes read a split's row, the workgroup's groups of them take splits in turn.
+// The weights first, one split a thread; then DP / 4 lanes read a split's row, and the workgroup's groups of them take
+// splits in turn.
+constexpr int MOST_SPLITS = 256;
+
 template <int DP>
 __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
   constexpr int L = DP / 4, GROUPS = 256 / L;
   __shared__ float4 so[GROUPS][L];
-  __shared__ float2 sm[GROUPS];
-  const int lane = threadIdx.x % L, g = threadIdx.x / L;
+  __shared__ float weight[MOST_SPLITS];
+  __shared__ float2 sm[4];
+  const int tid = threadIdx.x, lane = tid % L, g = tid / L;
   const long long item = blockIdx.x;  // (batch, kv_heads, rows)
   const long long step = (long long)p.batch * p.kv_heads * p.rows;
+  const float2 ml = tid < p.splits ? p.part_ml[tid * step + item] : make_float2(-INFINITY, 0.0f);
+  float top = ml.x;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  if ((tid & 63) == 0) sm[tid >> 6].x = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(sm[0].x, sm[1].x), fmaxf(sm[2].x, sm[3].x));
+  const float w = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);  // 0: the row saw nothing there
+  float total = ml.x == -INFINITY ? 0.0f : ml.y * w;
+  weight[tid] = w;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+  if ((tid & 63) == 0) sm[tid >> 6].y = total;
+  __syncthreads();
+  total = (sm[0].y + sm[1].y) + (sm[2].y + sm[3].y);
   float4 acc = make_float4(0, 0, 0, 0);
-  float top = -INFINITY, total = 0.0f;
+#pragma unroll 4
   for (int s = g; s < p.splits; s += GROUPS) {
-    const float2 ml = p.part_ml[s * step + item];
     const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
-    if (ml.x == -INFINITY) continue;  // the row saw nothing there
-    const float up = fmaxf(top, ml.x);
-    const float a = __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(ml.x - up);
-    acc.x = acc.x * a + o.x * w, acc.y = acc.y * a + o.y * w;
-    acc.z = acc.z * a + o.z * w, acc.w = acc.w * a + o.w * w;
-    total = total * a + ml.y * w;
-    top = up;
+    const float a = weight[s];
+    acc.x = fmaf(o.x, a, acc.x), acc.y = fmaf(o.y, a, acc.y), acc.z = fmaf(o.z, a, acc.z), acc.w = fmaf(o.w, a, acc.w);
   }
   so[g][lane] = acc;
-  if (lane == 0) sm[g] = make_float2(top, total);
   __syncthreads();
-  if (g != 0) return;
-  for (int n = 0; n < GROUPS; ++n) top = fmaxf(top, sm[n].x);
-  acc = make_float4(0, 0, 0, 0), total = 0.0f;
-  for (int n = 0; n < GROUPS; ++n) {
-    if (sm[n].x == -INFINITY) continue;
-    const float w = __builtin_amdgcn_exp2f(sm[n].x - top);
-    acc.x += so[n][lane].x * w, acc.y += so[n][lane].y * w;
-    acc.z += so[n][lane].z * w, acc.w += so[n][lane].w * w;
-    total += sm[n].y * w;
+  if (g != 0 || 4 * lane >= p.head_dim) return;
+  for (int n = 1; n < GROUPS; ++n) {
+    const float4 o = so[n][lane];
+    acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
   }
-  if (4 * lane >= p.head_dim) return;
   const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
   const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
   const int token = row / p.group, head = kvh * p.group + row % p.group;
-  uint2 w;
-  w.x = bf16_pack(acc.x * inv, acc.y * inv), w.y = bf16_pack(acc.z * inv, acc.w * inv);
-  *(uint2*)(p.out + b * p.o_b + token * p.o_t + head * p.o_h + 4 * lane) = w;
+  uint2 v;
+  v.x = bf16_pack(acc.x * inv, acc.y * inv), v.y = bf16_pack(acc.z * inv, acc.w * inv);
+  *(uint2*)(p.out + b * p.o_b + token * p.o_t + head * p.o_h + 4 * lane) = v;
 }
 
 // How a call runs.
@@ -655,6 +661,7 @@ Plan plan_for(const pd_attention_args* a) {
   const long long want = 2048 / n.waves;
   long long splits = whole >= want / 2 ? 1 : want / whole;
   if (splits > n.tiles / 2) splits = n.tiles / 2;
+  if (splits > MOST_SPLITS) splits = MOST_SPLITS;
   if (splits < 1) splits = 1;
   n.tiles_per_split = (int)((n.tiles + splits - 1) / splits);
   if (n.tiles_per_split < 1) n.tiles_per_split = 1;
