@@ -57,6 +57,7 @@ struct Attn {
   int row_tiles, splits, tiles, tiles_per_split;
   int prefix_last;  // prefix - 1
   int causal;
+  bool plain_rows;  // the keys of a tile lie within 32-bit offsets, and head_dim fills the rows in LDS
   float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
   float cap_a, cap_b;
   float small, poly1, poly3, poly5;  // |q.k| <= small: z = x (poly1 + x^2 (poly3 + x^2 poly5)) is the cap
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   __shared__ uint4 ls[2][TK];  // ordered sites
   __shared__ __attribute__((aligned(16))) uint32_t lb[2][TK];
   __shared__ int lq[4][NW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
 
   // Work items of one key head and entry are neighbours on one XCD (workgroups
   // are dealt to the eight in turn), whose L2 then serves their keys.
@@ -278,6 +279,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   };
   const int v_column = (slot0 ^ (v_place<DP>(key0, 0) >> 4) % (DP / 8)) * 8;
   static_assert(KEYS % 4 == 0 && (KEYS & (KEYS - 1)) == 0, "the turns of a thread's keys");
+  // bytes from a step's first key to this thread's first one
+  const uint32_t k_lane = (uint32_t)(key0 * p.k_t) * 2u, v_lane = (uint32_t)(key0 * p.v_t + v_column) * 2u;
   if (p.head_dim < DP) {
     for (int c = tid; c < TK * (DP / 8); c += NT)
 #pragma unroll
@@ -289,18 +292,25 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
     const int most_key = p.n_k - 1 - k0;
     const uint16_t* ks = kb + k0 * p.k_t;
     const uint16_t* vs = vb + k0 * p.v_t;
-    const bool past = most_key < TK - 1;
+    if (most_key >= TK - 1 && p.plain_rows) {
 #pragma unroll
-    for (int n = 0; n < G; ++n) {
-      const int slot = (n * NT + wave * 64) * 16;
-      const int kc = k_column(n);
-      long long k_at = key0 * p.k_t + n * KEYS * p.k_t, v_at = key0 * p.v_t + n * KEYS * p.v_t;
-      if (past) {
-        const long long key = min(key0 + n * KEYS, most_key);
-        k_at = key * p.k_t, v_at = key * p.v_t;
+      for (int n = 0; n < G; ++n) {
+        const int slot = (n * NT + wave * 64) * 16;
+        const int kc = k_column(n);
+        const char* const kn = (const char*)(ks + n * KEYS * p.k_t);
+        const char* const vn = (const char*)(vs + n * KEYS * p.v_t);
+        send16(kn + (k_lane + 2u * kc), lk[buf] + slot);
+        send16(vn + v_lane, lv[buf] + slot);
       }
-      if (kc < p.head_dim) send16(ks + k_at + kc, lk[buf] + slot);
-      if (v_column < p.head_dim) send16(vs + v_at + v_column, lv[buf] + slot);
+    } else {
+#pragma unroll
+      for (int n = 0; n < G; ++n) {
+        const int slot = (n * NT + wave * 64) * 16;
+        const int kc = k_column(n);
+        const long long key = min(key0 + n * KEYS, most_key);
+        if (kc < p.head_dim) send16(ks + key * p.k_t + kc, lk[buf] + slot);
+        if (v_column < p.head_dim) send16(vs + key * p.v_t + v_column, lv[buf] + slot);
+      }
     }
     if (wave == 0 && lane < TK) {
       if (notes) {
@@ -778,6 +788,8 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.q_sites = (const int4*)a->q_sites, p.k_sites = (const int4*)a->k_sites;
   p.q_sites_b = a->q_sites_batch_stride, p.k_sites_b = a->k_sites_batch_stride;
   p.slopes = a->slopes;
+  auto near = [](long long t) { return t >= 0 && t < (1ll << 24); };
+  p.plain_rows = near(p.k_t) && near(p.v_t) && (p.head_dim == 32 || p.head_dim == 64 || p.head_dim == 128);
   p.part_o = (float*)a->workspace;
   Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes);
   uint32_t* bytes = (uint32_t*)((char*)notes + n.notes_bytes);
