@@ -137,16 +137,25 @@ __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __rest
   ordered_sites[at * TILE + lane] = ordered(s);
 }
 
-typedef const __attribute__((address_space(1))) void global_void;
-typedef __attribute__((address_space(3))) void lds_void;
-
-// Send 16 (4) bytes a lane from memory to LDS at `to` + 16 (4) times the lane; lanes that do not take part leave
-// their place as it is.  Complete once the wave has waited for its vector memory operations.
-__device__ __forceinline__ void send16(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 16, 0, 0);
+// Send 16 (4) bytes a lane from memory to LDS at `to` (the same in all lanes) + 16 (4) times the lane; lanes that do
+// not take part leave their place as it is.  Complete after sent().  Written out rather than with the builtin, for
+// which the compiler waits before any later LDS read, of the other buffer too; no register is an output.
+__device__ __forceinline__ uint32_t lds_byte(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
-__device__ __forceinline__ void send4(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 4, 0, 0);
+__device__ __forceinline__ void send16(const void* from, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte(to)), "v"(from));
+}
+__device__ __forceinline__ void send16(const void* base, uint32_t at, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
+}
+__device__ __forceinline__ void send4(const void* base, uint32_t at, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
+}
+__device__ __forceinline__ void sent() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
 }
 
 // LDS byte of granule g (8 values) of a key's row.  Rows are not padded; which
@@ -256,9 +265,11 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
       base += 64;
       if (base >= end) return -1;
       bool visit = base + lane < end;
-      if (visit && notes) {
-        mine = notes[base + lane];
-        visit = meets(mine, gv_min, gv_max, gt_max);
+      if (notes) {
+        mine = notes[min(base + lane, end - 1)];
+        // (nothing else is on its way here; waiting at once keeps waits for these registers off the loads sent next)
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        visit = visit && meets(mine, gv_min, gv_max, gt_max);
       }
       mask = __ballot(visit);
     }
@@ -299,8 +310,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         const int kc = k_column(n);
         const char* const kn = (const char*)(ks + n * KEYS * p.k_t);
         const char* const vn = (const char*)(vs + n * KEYS * p.v_t);
-        send16(kn + (k_lane + 2u * kc), lk[buf] + slot);
-        send16(vn + v_lane, lv[buf] + slot);
+        send16(kn, k_lane + 2u * kc, lk[buf] + slot);
+        send16(vn, v_lane, lv[buf] + slot);
       }
     } else {
 #pragma unroll
@@ -314,7 +325,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
     }
     if (wave == 0 && lane < TK) {
       if (notes) {
-        send16(ordered_sites + k0 + lane, ls[buf]);
+        send16(ordered_sites + k0, 16u * lane, ls[buf]);
       } else {
         int4 s = make_int4(0, 0, 0, lane <= most_key ? 0 : -1);
         if (sites && lane <= most_key) s = sites[k0 + lane];
@@ -322,7 +333,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         lb[buf][lane] = site_bytes(s);
       }
     }
-    if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0 + lane, lb[buf]);
+    if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0, 4u * lane, lb[buf]);
   };
 
   f32x16 o[DP / 32];
@@ -351,7 +362,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
     note = note_of(tile);
     load_step(0, tile * TILE);
   }
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part is in LDS
+  sent();
   __syncthreads();
   while (tile >= 0) {
     int after = tile, after_step = step + 1;
@@ -560,7 +571,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         }
       }
     }
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the next step's keys are in LDS
+    sent();
     __syncthreads();
     tile = after, step = after_step, buf ^= 1, note = after_note;
   }
