@@ -38,6 +38,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 64;  // keys of a noted tile
+constexpr int RUN = 4;    // neighbouring work items of one XCD
+constexpr int FEW_SPLITS = 16;  // up to as many: a row's splits that saw nothing leave no result
 // tanh u for |u| <= 0.35 is u (TANH1 + u^2 (TANH3 + u^2 TANH5)) within 4.9e-7 (fitted for the least largest error)
 constexpr float TANH1 = 0.9999902f, TANH3 = -0.33268409f, TANH5 = 0.12248027f;
 
@@ -54,6 +56,7 @@ struct Attn {
   int batch, heads, kv_heads, group, head_dim;
   int n_q, n_k;
   int rows;  // n_q * group
+  unsigned items;  // row_tiles * splits * kv_heads * batch
   int row_tiles, splits, tiles, tiles_per_split;
   int prefix_last;  // prefix - 1
   int causal;
@@ -187,10 +190,11 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   __shared__ int lq[4][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
 
-  // Work items of one key head and entry are neighbours on one XCD (workgroups
-  // are dealt to the eight in turn), whose L2 then serves their keys.
-  const unsigned total_items = gridDim.x, xcd = blockIdx.x & 7, per = total_items >> 3, rest = total_items & 7;
-  unsigned item = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+  // Workgroups are dealt to the eight XCDs in turn.  An XCD takes RUN
+  // neighbouring items, which read the same keys, in its L2; longer runs would
+  // leave XCDs idle where items see unequal numbers of keys.
+  unsigned item = ((blockIdx.x >> 3) / RUN * 8 + (blockIdx.x & 7)) * RUN + (blockIdx.x >> 3) % RUN;
+  if (item >= p.items) return;
   const int row_tile = item % p.row_tiles;
   item /= p.row_tiles;
   const int split = item % p.splits;
@@ -581,14 +585,15 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   if (p.splits > 1) {
     const long long at_row = (((long long)split * p.batch + b) * p.kv_heads + kvh) * p.rows + row;
     float* part = p.part_o + at_row * DP;
+    const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
+    if (!none || p.splits > FEW_SPLITS)  // (the join of many reads them all at once)
 #pragma unroll
     for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(float4*)(part + 32 * m + 8 * g + 4 * half) =
             make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
-    // a row without a reference saw nothing, or NaN scores alone
-    if (half == 0) p.part_ml[at_row] = make_float2(unset && total == 0.0f ? -INFINITY : top, total);
+    if (half == 0) p.part_ml[at_row] = make_float2(none ? -INFINITY : top, total);
     return;
   }
   const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
@@ -605,6 +610,16 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         *(uint2*)(out + d) = w;
       }
     }
+}
+
+// Values 4 lane .. 4 lane + 3 of row `item` of (batch, kv_heads, rows).
+__device__ __forceinline__ void store_joined(const Attn& p, long long item, int lane, float4 acc, float total) {
+  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
+  const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
+  const int token = row / p.group, head = kvh * p.group + row % p.group;
+  uint2 v;
+  v.x = bf16_pack(acc.x * inv, acc.y * inv), v.y = bf16_pack(acc.z * inv, acc.w * inv);
+  *(uint2*)(p.out + b * p.o_b + token * p.o_t + head * p.o_h + 4 * lane) = v;
 }
 
 // Joins the splits of one row: out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
@@ -639,8 +654,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
   float4 acc = make_float4(0, 0, 0, 0);
 #pragma unroll 4
   for (int s = g; s < p.splits; s += GROUPS) {
-    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
     const float a = weight[s];
+    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
     acc.x = fmaf(o.x, a, acc.x), acc.y = fmaf(o.y, a, acc.y), acc.z = fmaf(o.z, a, acc.z), acc.w = fmaf(o.w, a, acc.w);
   }
   so[g][lane] = acc;
@@ -650,12 +665,31 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
     const float4 o = so[n][lane];
     acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
   }
-  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
-  const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
-  const int token = row / p.group, head = kvh * p.group + row % p.group;
-  uint2 v;
-  v.x = bf16_pack(acc.x * inv, acc.y * inv), v.y = bf16_pack(acc.z * inv, acc.w * inv);
-  *(uint2*)(p.out + b * p.o_b + token * p.o_t + head * p.o_h + 4 * lane) = v;
+  store_joined(p, item, lane, acc, total);
+}
+
+// The same for up to FEW_SPLITS splits: DP / 4 lanes a row, one split after the other.
+
+template <int DP>
+__global__ void __launch_bounds__(256) attention_join_few_kernel(const Attn p) {
+  constexpr int L = DP / 4;
+  const int lane = threadIdx.x % L;
+  const long long step = (long long)p.batch * p.kv_heads * p.rows;
+  const long long item = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (item >= step || 4 * lane >= p.head_dim) return;
+  float top = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[s * step + item].x);
+  float4 acc = make_float4(0, 0, 0, 0);
+  float total = 0.0f;
+  for (int s = 0; s < p.splits; ++s) {
+    const float2 ml = p.part_ml[s * step + item];
+    if (ml.x == -INFINITY) continue;  // the row saw nothing there
+    const float w = __builtin_amdgcn_exp2f(ml.x - top);
+    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    acc.x = fmaf(o.x, w, acc.x), acc.y = fmaf(o.y, w, acc.y), acc.z = fmaf(o.z, w, acc.z), acc.w = fmaf(o.w, w, acc.w);
+    total = fmaf(ml.y, w, total);
+  }
+  store_joined(p, item, lane, acc, total);
 }
 
 // How a call runs.
@@ -678,16 +712,24 @@ Plan plan_for(const pd_attention_args* a) {
   // up to four tiles are read whole: the notes' launch would cost more than it saves
   n.notes = a->k_sites && n.tiles > 4;
   const long long heads = (long long)a->kv_heads * a->batch, whole = n.row_tiles * heads;
-  // enough waves for the card (256 CUs), at least two tiles each
-  const long long want = 2048 / n.waves;
-  long long splits = whole >= want / 2 ? 1 : want / whole;
-  if (splits > n.tiles / 2) splits = n.tiles / 2;
+  // Splits: to fill the card once (512 workgroups of four waves, or 2048 waves of few rows), down to 8 (2) tiles each;
+  // and, while they keep 32 tiles, until there are eight times as many, which evens out rows that see unequal numbers of tiles.  A
+  // split's result costs about as much as 5 tiles of its rows.
+  const long long fill = 2048 / n.waves, even = 8 * 512 * 4 / n.waves;
+  const long long least = n.waves == 1 ? 2 : 8;
+  long long splits = (fill + whole - 1) / whole;
+  if (splits > n.tiles / least) splits = n.tiles / least;
+  long long more = (even + whole - 1) / whole;
+  if (more > n.tiles / 32) more = n.tiles / 32;
+  if (splits < more) splits = more;
   if (splits > MOST_SPLITS) splits = MOST_SPLITS;
+  const int dp = a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128;
+  const long long most = (1ll << 30) / (heads * rows * dp * 4);  // 1 GB of workspace
+  if (splits > most) splits = most;
   if (splits < 1) splits = 1;
   n.tiles_per_split = (int)((n.tiles + splits - 1) / splits);
   if (n.tiles_per_split < 1) n.tiles_per_split = 1;
   n.splits = n.tiles ? (n.tiles + n.tiles_per_split - 1) / n.tiles_per_split : 1;
-  const int dp = a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128;
   const long long lists = a->k_sites_batch_stride ? a->batch : 1;
   n.notes_bytes = n.notes ? (size_t)lists * n.tiles * sizeof(Tile) : 0;
   n.bytes_bytes = n.notes ? (size_t)lists * n.tiles * TILE * 4 : 0;
@@ -759,14 +801,21 @@ void launch(const Attn& p, bool cap, bool bias, unsigned items, hipStream_t st) 
 
 template <int DP>
 void launch_width(const Attn& p, const Plan& n, bool cap, bool bias, hipStream_t st) {
+  const unsigned blocks = (p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN);
   if (n.waves == 1)
-    launch<DP, 1>(p, cap, bias, (unsigned)n.items, st);
+    launch<DP, 1>(p, cap, bias, blocks, st);
   else if (n.waves == 2)
-    launch<DP, 2>(p, cap, bias, (unsigned)n.items, st);
+    launch<DP, 2>(p, cap, bias, blocks, st);
   else
-    launch<DP, 4>(p, cap, bias, (unsigned)n.items, st);
+    launch<DP, 4>(p, cap, bias, blocks, st);
   if (p.splits > 1)
-    hipLaunchKernelGGL(attention_join_kernel<DP>, dim3((unsigned)(p.rows * p.kv_heads * p.batch)), dim3(256), 0, st, p);
+  {
+    const long long rows = (long long)p.rows * p.kv_heads * p.batch, group = 256 / (DP / 4);
+    if (p.splits <= FEW_SPLITS)
+      hipLaunchKernelGGL(attention_join_few_kernel<DP>, dim3((unsigned)((rows + group - 1) / group)), dim3(256), 0, st, p);
+    else
+      hipLaunchKernelGGL(attention_join_kernel<DP>, dim3((unsigned)rows), dim3(256), 0, st, p);
+  }
 }
 
 }  // namespace
@@ -780,7 +829,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.batch = a->batch, p.heads = a->heads, p.kv_heads = a->kv_heads, p.group = a->heads / a->kv_heads;
   p.head_dim = a->head_dim;
   p.n_q = a->n_q, p.n_k = a->n_k, p.rows = a->n_q * p.group;
-  p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
+  p.items = (unsigned)n.items, p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
   p.prefix_last = a->prefix - 1, p.causal = a->causal;
   p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / a->cap : a->scale * LOG2E;
   if (a->cap > 0.0f) {
