@@ -39,7 +39,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 64;  // keys of a noted tile
 constexpr int RUN = 4;    // neighbouring work items of one XCD
-constexpr int FEW_SPLITS = 16;  // up to as many: a row's splits that saw nothing leave no result
+constexpr int FEW_SPLITS = 32;  // up to as many: a row's splits that saw nothing leave no result
 // tanh u for |u| <= 0.35 is u (TANH1 + u^2 (TANH3 + u^2 TANH5)) within 4.9e-7 (fitted for the least largest error)
 constexpr float TANH1 = 0.9999902f, TANH3 = -0.33268409f, TANH5 = 0.12248027f;
 
@@ -77,7 +77,11 @@ struct Attn {
   const uint32_t* bytes;  // with notes: site_bytes and ordered sites of every key, [lists][tiles][TILE]
   const uint4* ordered_sites;
   int notes_b;        // tiles from batch entry to batch entry
-  float* part_o;      // [splits][batch][kv_heads][rows][DP]
+  // results of splits, [splits][batch][kv_heads][blocks of 32 rows (of all, if there are fewer)], four values each: few
+  // splits: [DP / 4][block_rows], so that a wave writes whole lines; many: [block_rows][DP / 4], so that a row's join
+  // reads whole lines
+  float4* part_o;
+  int blocks, block_rows, part_c, part_r;
   float2* part_ml;    // [splits][batch][kv_heads][rows]: maximum (log2 units), sum
 };
 
@@ -85,6 +89,13 @@ struct Attn {
 __device__ __forceinline__ uint4 ordered(const int4 s) {
   const uint32_t sign = 0x80000000u;
   return make_uint4((uint32_t)s.x ^ sign, (uint32_t)s.y ^ sign, (uint32_t)s.z ^ sign, s.w < 0 ? ~0u : (uint32_t)s.w);
+}
+
+// Values 4 c .. 4 c + 3 of a row in part_o.
+template <int DP>
+__device__ __forceinline__ long long part_at(const Attn& p, int split, int b, int kvh, int row, int c) {
+  const long long block = (((long long)split * p.batch + b) * p.kv_heads + kvh) * p.blocks + (row >> 5);
+  return block * (DP / 4) * p.block_rows + c * p.part_c + (row & 31) * p.part_r;
 }
 
 // |a - b| + c in one instruction (the compiler takes three for it in a sum of several)
@@ -584,15 +595,16 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   if (row >= p.rows) return;
   if (p.splits > 1) {
     const long long at_row = (((long long)split * p.batch + b) * p.kv_heads + kvh) * p.rows + row;
-    float* part = p.part_o + at_row * DP;
     const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
-    if (!none || p.splits > FEW_SPLITS)  // (the join of many reads them all at once)
+    if (!none || p.splits > FEW_SPLITS) {      // (the join of many reads them all at once)
+      float4* part = p.part_o + part_at<DP>(p, split, b, kvh, row, half);
 #pragma unroll
-    for (int m = 0; m < DP / 32; ++m)
+      for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(float4*)(part + 32 * m + 8 * g + 4 * half) =
-            make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
+        for (int g = 0; g < 4; ++g)
+          part[(8 * m + 2 * g) * p.part_c] =
+              make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
+    }
     if (half == 0) p.part_ml[at_row] = make_float2(none ? -INFINITY : top, total);
     return;
   }
@@ -612,10 +624,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
     }
 }
 
-// Values 4 lane .. 4 lane + 3 of row `item` of (batch, kv_heads, rows).
-__device__ __forceinline__ void store_joined(const Attn& p, long long item, int lane, float4 acc, float total) {
+// Values 4 lane .. 4 lane + 3 of a row.
+__device__ __forceinline__ void store_joined(const Attn& p, int b, int kvh, int row, int lane, float4 acc, float total) {
   const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
-  const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
   const int token = row / p.group, head = kvh * p.group + row % p.group;
   uint2 v;
   v.x = bf16_pack(acc.x * inv, acc.y * inv), v.y = bf16_pack(acc.z * inv, acc.w * inv);
@@ -635,6 +646,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
   __shared__ float2 sm[4];
   const int tid = threadIdx.x, lane = tid % L, g = tid / L;
   const long long item = blockIdx.x;  // (batch, kv_heads, rows)
+  const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
   const long long step = (long long)p.batch * p.kv_heads * p.rows;
   const float2 ml = tid < p.splits ? p.part_ml[tid * step + item] : make_float2(-INFINITY, 0.0f);
   float top = ml.x;
@@ -655,7 +667,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
 #pragma unroll 4
   for (int s = g; s < p.splits; s += GROUPS) {
     const float a = weight[s];
-    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    const float4 o = p.part_o[part_at<DP>(p, s, b, kvh, row, lane)];
     acc.x = fmaf(o.x, a, acc.x), acc.y = fmaf(o.y, a, acc.y), acc.z = fmaf(o.z, a, acc.z), acc.w = fmaf(o.w, a, acc.w);
   }
   so[g][lane] = acc;
@@ -665,31 +677,39 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Attn p) {
     const float4 o = so[n][lane];
     acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
   }
-  store_joined(p, item, lane, acc, total);
+  store_joined(p, b, kvh, row, lane, acc, total);
 }
 
-// The same for up to FEW_SPLITS splits: DP / 4 lanes a row, one split after the other.
-
+// The same for up to FEW_SPLITS splits: a workgroup joins a block of 32 rows, one split after the other.
 template <int DP>
 __global__ void __launch_bounds__(256) attention_join_few_kernel(const Attn p) {
-  constexpr int L = DP / 4;
-  const int lane = threadIdx.x % L;
-  const long long step = (long long)p.batch * p.kv_heads * p.rows;
-  const long long item = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  if (item >= step || 4 * lane >= p.head_dim) return;
+  const int r = threadIdx.x & 31, c0 = threadIdx.x >> 5;
+  const unsigned group = blockIdx.x / p.blocks;  // (batch, kv_heads)
+  const int kvh = group % p.kv_heads, b = group / p.kv_heads, row = (int)(blockIdx.x % p.blocks) * 32 + r;
+  if (row >= p.rows) return;
+  const long long step = (long long)p.batch * p.kv_heads * p.rows, item = (long long)group * p.rows + row;
   float top = -INFINITY;
   for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[s * step + item].x);
-  float4 acc = make_float4(0, 0, 0, 0);
+  float4 acc[DP / 32];
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n) acc[n] = make_float4(0, 0, 0, 0);
   float total = 0.0f;
   for (int s = 0; s < p.splits; ++s) {
     const float2 ml = p.part_ml[s * step + item];
     if (ml.x == -INFINITY) continue;  // the row saw nothing there
     const float w = __builtin_amdgcn_exp2f(ml.x - top);
-    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
-    acc.x = fmaf(o.x, w, acc.x), acc.y = fmaf(o.y, w, acc.y), acc.z = fmaf(o.z, w, acc.z), acc.w = fmaf(o.w, w, acc.w);
+    const float4* part = p.part_o + part_at<DP>(p, s, b, kvh, row, c0);
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n) {
+      const float4 o = part[8 * n * p.part_c];
+      acc[n].x = fmaf(o.x, w, acc[n].x), acc[n].y = fmaf(o.y, w, acc[n].y);
+      acc[n].z = fmaf(o.z, w, acc[n].z), acc[n].w = fmaf(o.w, w, acc[n].w);
+    }
     total = fmaf(ml.y, w, total);
   }
-  store_joined(p, item, lane, acc, total);
+#pragma unroll
+  for (int n = 0; n < DP / 32; ++n)
+    if (4 * (c0 + 8 * n) < p.head_dim) store_joined(p, b, kvh, row, c0 + 8 * n, acc[n], total);
 }
 
 // How a call runs.
@@ -734,7 +754,8 @@ Plan plan_for(const pd_attention_args* a) {
   n.notes_bytes = n.notes ? (size_t)lists * n.tiles * sizeof(Tile) : 0;
   n.bytes_bytes = n.notes ? (size_t)lists * n.tiles * TILE * 4 : 0;
   n.sites_bytes = 4 * n.bytes_bytes;
-  n.o_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * dp * 4 : 0;
+  const long long part_rows = rows < 32 ? rows : (rows + 31) / 32 * 32;
+  n.o_bytes = n.splits > 1 ? (size_t)n.splits * heads * part_rows * dp * 4 : 0;
   n.ml_bytes = n.splits > 1 ? (size_t)n.splits * heads * rows * 8 : 0;
   n.items = whole * n.splits;
   return n;
@@ -810,11 +831,11 @@ void launch_width(const Attn& p, const Plan& n, bool cap, bool bias, hipStream_t
     launch<DP, 4>(p, cap, bias, blocks, st);
   if (p.splits > 1)
   {
-    const long long rows = (long long)p.rows * p.kv_heads * p.batch, group = 256 / (DP / 4);
+    const unsigned groups = (unsigned)(p.kv_heads * p.batch);
     if (p.splits <= FEW_SPLITS)
-      hipLaunchKernelGGL(attention_join_few_kernel<DP>, dim3((unsigned)((rows + group - 1) / group)), dim3(256), 0, st, p);
+      hipLaunchKernelGGL(attention_join_few_kernel<DP>, dim3(groups * p.blocks), dim3(256), 0, st, p);
     else
-      hipLaunchKernelGGL(attention_join_kernel<DP>, dim3((unsigned)rows), dim3(256), 0, st, p);
+      hipLaunchKernelGGL(attention_join_kernel<DP>, dim3(groups * p.rows), dim3(256), 0, st, p);
   }
 }
 
@@ -850,7 +871,11 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.slopes = a->slopes;
   auto near = [](long long t) { return t >= 0 && t < (1ll << 24); };
   p.plain_rows = near(p.k_t) && near(p.v_t) && (p.head_dim == 32 || p.head_dim == 64 || p.head_dim == 128);
-  p.part_o = (float*)a->workspace;
+  p.part_o = (float4*)a->workspace;
+  p.blocks = (p.rows + 31) / 32, p.block_rows = p.rows < 32 ? p.rows : 32;
+  const bool few = n.splits <= FEW_SPLITS;
+  p.part_c = few ? p.block_rows : 1;
+  p.part_r = few ? 1 : (a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128) / 4;
   Tile* notes = (Tile*)((char*)a->workspace + n.o_bytes);
   uint32_t* bytes = (uint32_t*)((char*)notes + n.notes_bytes);
   uint4* ordered_sites = (uint4*)((char*)bytes + n.bytes_bytes);
