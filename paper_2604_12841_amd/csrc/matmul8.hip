@@ -46,7 +46,7 @@ struct Mm {
   const float* bias;
   void* out;
   bool lines;   // rows of out are 16-byte aligned
-  bool passing;  // out is too large to stay in a cache for who reads it next
+  bool passing;  // see token_values.h
 };
 
 // 16 bytes of a row from column k on, zero past K; nothing outside the row is read.  (Device memory takes unaligned
@@ -172,10 +172,7 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
         if (m < p.M && n < p.N) {
           T* to = (T*)p.out + m * p.out_stride + n;
           if (p.lines && n + E <= p.N) {
-            if (p.passing)
-              __builtin_nontemporal_store(__builtin_bit_cast(i32x4, w), (i32x4*)to);
-            else
-              *(uint4*)to = w;
+            store16(to, w, p.passing);
           } else {
             T v[E];
             __builtin_memcpy(v, &w, 16);
@@ -514,9 +511,8 @@ extern "C" pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args*
   p.a = (const uint8_t*)a->a, p.w = (const uint8_t*)a->w;
   p.a_stride = a->a_stride, p.w_stride = a->w_stride, p.out_stride = a->out_stride;
   p.a_scales = a->a_scales, p.w_scales = a->w_scales, p.bias = a->bias, p.out = a->out;
-  // Stores past the caches let the next tile's loads have them (163072 x 2048 x 512 to bf16: 250 -> 228 us); results
-  // that a cache can hold (256 MB behind the L2s) are left there for their reader.
-  p.passing = a->M * a->N * elem > (128ll << 20);
+  // (163072 x 2048 x 512 to bf16: 250 -> 228 us)
+  p.passing = a->M * a->N * elem > PASSING_BYTES;
   p.lines = (uintptr_t)a->out % 16 == 0 && (a->out_stride * elem) % 16 == 0;
   // 256 rows of a tile within 32-bit offsets
   const bool wide = a->K % 16 == 0 && (uintptr_t)a->a % 16 == 0 && (uintptr_t)a->w % 16 == 0 &&

@@ -32,6 +32,7 @@ struct Norm {
   float* scales;
   long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
   int int8;
+  bool passing;  // sum and out, see token_values.h
 };
 
 // The column of value e (0 .. 8 NV - 1) of a lane: granules of 8 neighbours,
@@ -62,12 +63,13 @@ __device__ __forceinline__ void load_row(const T* __restrict__ p, int lane, int 
 }
 
 template <typename T, int LPR, int NV, bool WIDE>
-__device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV]) {
+__device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV],
+                                          bool passing) {
   if constexpr (WIDE) {
 #pragma unroll
     for (int g = 0; g < NV; ++g) {
       const int c = column<LPR, true>(lane, 8 * g);
-      if (c < width) store8(p + c, &v[8 * g]);
+      if (c < width) store8(p + c, &v[8 * g], passing);
     }
   } else {
 #pragma unroll
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) g[e] = 1.0f;
     }
-    if (p.sum) store_row<T, LPR, NV, WIDE>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
+    if (p.sum) store_row<T, LPR, NV, WIDE>((T*)p.sum + row * p.sum_stride, lane, p.width, s, p.passing);
     float square = 0.0f, most = 0.0f, check = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8 * NV; ++e) {
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
       float y[8 * NV];
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) y[e] = s[e] * inv;
-      store_row<T, LPR, NV, WIDE>((T*)p.out + row * p.out_stride, lane, p.width, y);
+      store_row<T, LPR, NV, WIDE>((T*)p.out + row * p.out_stride, lane, p.width, y, p.passing);
     }
     if (p.codes) {
       const bool finite = square < INFINITY && most < INFINITY;  // false for a NaN square
@@ -188,7 +190,11 @@ void launch(const Norm& p, bool wide, hipStream_t st) {
   constexpr int THREADS = LPR > 256 ? LPR : 256;
   constexpr int ROWS = THREADS / LPR;
   const long long want = (p.rows + ROWS - 1) / ROWS;
-  const unsigned blocks = (unsigned)(want < (1 << 21) ? want : (1 << 21));  // threads stay below 2^32
+  // Waves of narrow rows take several, sixteen workgroups to a CU at most (rows of 128 to 512: 10 % less time than one each);
+  // where a workgroup shares a row that only lengthens its chain of barriers (2048 fp32 columns: 7 % more), and the
+  // bound keeps threads below 2^32.
+  const long long most = LPR <= 64 ? 4096 : 1 << 21;
+  const unsigned blocks = (unsigned)(want < most ? want : most);
   if (wide)
     hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true>), dim3(blocks), dim3(THREADS), 0, st, p);
   else
@@ -243,6 +249,7 @@ extern "C" pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* a
   p.qmax = p.int8 ? 127.0f : 448.0f;
   p.x = a->x, p.residual = a->residual, p.gain = a->gain, p.sum = a->sum, p.out = a->out;
   p.codes = (uint8_t*)a->codes, p.scales = a->scales;
+  p.passing = a->rows * a->width * elem > PASSING_BYTES;
   p.x_stride = a->x_stride, p.residual_stride = a->residual_stride, p.sum_stride = a->sum_stride;
   p.out_stride = a->out_stride, p.codes_stride = a->codes_stride;
   const bool wide = a->width % 8 == 0 && aligned(a->x, a->x_stride, elem, 16) &&

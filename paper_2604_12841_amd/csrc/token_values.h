@@ -30,14 +30,27 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 
-__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
+// A result is "passing" if it is too large for the 256 MB behind the L2s to keep for its reader together with
+// anything else: it is stored past the caches, which leaves them, and the memory's time, to what is still read.
+constexpr long long PASSING_BYTES = 128ll << 20;
+
+__device__ __forceinline__ void store16(void* p, const uint4 w, bool passing) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  if (passing)  // (written out: the compiler makes one ordinary store of the two branches)
+    asm volatile("global_store_dwordx4 %0, %1, off nt" ::"v"(p), "v"(__builtin_bit_cast(u32x4, w)));
+  else
+    *(uint4*)p = w;
+}
+
+__device__ __forceinline__ void store8(uint16_t* p, const float* v, bool passing) {
   uint4 w;
   w.x = bf16_pack(v[0], v[1]), w.y = bf16_pack(v[2], v[3]);
   w.z = bf16_pack(v[4], v[5]), w.w = bf16_pack(v[6], v[7]);
-  *(uint4*)p = w;
+  store16(p, w, passing);
 }
 
-__device__ __forceinline__ void store8(float* p, const float* v) {
+// (Never past the caches: each of the two stores covers half of every line, which the L2 has to put together.)
+__device__ __forceinline__ void store8(float* p, const float* v, bool) {
   *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
   *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
