@@ -153,18 +153,19 @@ __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __rest
 
 // Send 16 (4) bytes a lane from memory to LDS at `to` (the same in all lanes) + 16 (4) times the lane; lanes that do
 // not take part leave their place as it is.  Complete after sent().  Written out rather than with the builtin, for
-// which the compiler waits before any later LDS read, of the other buffer too; no register is an output.
+// which the compiler waits before any later LDS read, of the other buffer too; no register is an output.  (The wait
+// states are those that the load needs after writes of m0 and, by vector instructions, of its scalar base.)
 __device__ __forceinline__ uint32_t lds_byte(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 __device__ __forceinline__ void send16(const void* from, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte(to)), "v"(from));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte(to)), "v"(from));
 }
 __device__ __forceinline__ void send16(const void* base, uint32_t at, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
 }
 __device__ __forceinline__ void send4(const void* base, uint32_t at, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
 }
 __device__ __forceinline__ void sent() {
   asm volatile("" ::: "memory");

@@ -113,9 +113,10 @@ __device__ __forceinline__ void mma64(const uint4 w0, const uint4 w1, const uint
 
 // Sends 16 bytes a lane from base + at to LDS byte `to` (the same in all lanes) + 16 times the lane.  Written out
 // rather than with the builtin, for which the compiler waits before any later LDS read, of the other buffers too; the
-// kernel counts the loads in flight itself.  No register is an output.
+// kernel counts the loads in flight itself.  No register is an output.  (The wait states are those that the load needs
+// after writes of m0 and, by vector instructions, of its scalar base.)
 __device__ __forceinline__ void send16(const uint8_t* base, uint32_t at, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base));
 }
 
 template <int N>
@@ -128,7 +129,7 @@ __device__ __forceinline__ void wait_sent() {  // all but the last N loads are t
 // The scales, bias, activation and rounding of a wave's blocks, 32 tokens at a time through LDS to whole lines.
 // acc[mb][nb]: tokens m0 + 32 mb, channels n0 + 32 nb on; sa: the scales of this lane's tokens; sw: the channels'
 // scales and, ws further, biases in LDS; `stage`: 4 KB of LDS of this wave's own.
-template <typename T, int SUM, int ACT, int MB, int NB>
+template <typename T, int SUM, int ACT, int MB, int NB, bool PASSING>
 __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&acc)[MB][NB], long long m0, int n0,
                                        const float (&sa)[MB], const float* sw, int ws, uint8_t* stage) {
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -172,7 +173,7 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
         if (m < p.M && n < p.N) {
           T* to = (T*)p.out + m * p.out_stride + n;
           if (p.lines && n + E <= p.N) {
-            store16(to, w, p.passing);
+            store16<PASSING>(to, w);
           } else {
             T v[E];
             __builtin_memcpy(v, &w, 16);
@@ -212,7 +213,7 @@ __device__ __forceinline__ void keep_scales(const Scales<MB>& s, float* sw) {  /
 
 // 2 x WN waves of MB x NB blocks; BK codes of k a step, BUFS steps in LDS.  With wide loads a workgroup takes several
 // tiles, and the loads run on into the next one: its first steps arrive while this one's results are written.
-template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS, bool WIDE>
+template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS, bool WIDE, bool PASSING>
 __global__ void __launch_bounds__(128 * WN, MB * NB >= 4 ? 2 : 3) matmul8_kernel(const Mm p) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
   constexpr int BUF = (TM + TN) * BK;          // bytes of a step: tokens, then channels
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(128 * WN, MB * NB >= 4 ? 2 : 3) matmul8_kernel
     place(item, m0, n0);
     keep_scales<MB, TN>(s, sw);
     __syncthreads();  // ... and all waves are done with the buffer
-    finish<T, SUM, ACT, MB, NB>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, s.a, sw + wn * 32 * NB, TN,
+    finish<T, SUM, ACT, MB, NB, PASSING>(p, acc, m0 + wm * 32 * MB, n0 + wn * 32 * NB, s.a, sw + wn * 32 * NB, TN,
                                 lds + (OWN ? BUFS : buf) * BUF + wave * STAGE);
   };
   auto scales = [&](unsigned item) {
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(512) matmul8_few_kernel(const Mm p) {
     }
     __syncthreads();
   }
-  if (wave == 0) finish<T, SUM, ACT, 1, 1>(p, acc, m0, n0, s.a, sw, 32, stage);
+  if (wave == 0) finish<T, SUM, ACT, 1, 1, false>(p, acc, m0, n0, s.a, sw, 32, stage);
 }
 
 template <typename T, int SUM, int ACT, int MB, int NB, int WN, int BK, int BUFS>
@@ -465,11 +466,16 @@ void launch_tiles(const Mm& p, bool wide, hipStream_t st) {
   constexpr int TM = 64 * MB, TN = 32 * NB * WN;
   const unsigned items = (unsigned)(((p.M + TM - 1) / TM) * ((p.N + TN - 1) / TN));
   const unsigned most = 256 * (MB * NB == 8 ? 1 : MB * NB == 4 ? 2 : 3);  // workgroups that the card holds at once
-  if (wide)
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true>), dim3(items < most ? items : most),
-                       dim3(128 * WN), 0, st, p);
+  constexpr bool MAY_PASS = MB * NB == 8;  // smaller tiles have smaller results
+  if (wide && MAY_PASS && p.passing)
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true, MAY_PASS>),
+                       dim3(items < most ? items : most), dim3(128 * WN), 0, st, p);
+  else if (wide)
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, true, false>),
+                       dim3(items < most ? items : most), dim3(128 * WN), 0, st, p);
   else
-    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, false>), dim3(items), dim3(128 * WN), 0, st, p);
+    hipLaunchKernelGGL((matmul8_kernel<T, SUM, ACT, MB, NB, WN, BK, BUFS, false, false>), dim3(items), dim3(128 * WN), 0,
+                       st, p);
 }
 
 template <typename T, int SUM, int ACT>

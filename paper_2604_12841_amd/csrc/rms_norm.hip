@@ -32,7 +32,7 @@ struct Norm {
   float* scales;
   long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
   int int8;
-  bool passing;  // sum and out, see token_values.h
+  bool passing;  // bf16 sum and out, see token_values.h
 };
 
 // The column of value e (0 .. 8 NV - 1) of a lane: granules of 8 neighbours,
@@ -62,14 +62,13 @@ __device__ __forceinline__ void load_row(const T* __restrict__ p, int lane, int 
   }
 }
 
-template <typename T, int LPR, int NV, bool WIDE>
-__device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV],
-                                          bool passing) {
+template <typename T, int LPR, int NV, bool WIDE, bool PASSING>
+__device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV]) {
   if constexpr (WIDE) {
 #pragma unroll
     for (int g = 0; g < NV; ++g) {
       const int c = column<LPR, true>(lane, 8 * g);
-      if (c < width) store8(p + c, &v[8 * g], passing);
+      if (c < width) store8<PASSING>(p + c, &v[8 * g]);
     }
   } else {
 #pragma unroll
@@ -106,7 +105,7 @@ __device__ __forceinline__ void reduce_row(float& a, float& b, float* shared) {
   }
 }
 
-template <typename T, int LPR, int NV, bool WIDE>
+template <typename T, int LPR, int NV, bool WIDE, bool PASSING>
 __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const Norm p) {
   constexpr int THREADS = LPR > 256 ? LPR : 256;
   constexpr int ROWS = THREADS / LPR;  // rows of a workgroup
@@ -129,7 +128,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) g[e] = 1.0f;
     }
-    if (p.sum) store_row<T, LPR, NV, WIDE>((T*)p.sum + row * p.sum_stride, lane, p.width, s, p.passing);
+    if (p.sum) store_row<T, LPR, NV, WIDE, PASSING>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
     float square = 0.0f, most = 0.0f, check = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8 * NV; ++e) {
@@ -145,7 +144,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
       float y[8 * NV];
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) y[e] = s[e] * inv;
-      store_row<T, LPR, NV, WIDE>((T*)p.out + row * p.out_stride, lane, p.width, y, p.passing);
+      store_row<T, LPR, NV, WIDE, PASSING>((T*)p.out + row * p.out_stride, lane, p.width, y);
     }
     if (p.codes) {
       const bool finite = square < INFINITY && most < INFINITY;  // false for a NaN square
@@ -195,10 +194,13 @@ void launch(const Norm& p, bool wide, hipStream_t st) {
   // bound keeps threads below 2^32.
   const long long most = LPR <= 64 ? 4096 : 1 << 21;
   const unsigned blocks = (unsigned)(want < most ? want : most);
-  if (wide)
-    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true>), dim3(blocks), dim3(THREADS), 0, st, p);
+  constexpr bool MAY_PASS = sizeof(T) == 2 && LPR <= 64;
+  if (wide && MAY_PASS && p.passing)
+    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true, MAY_PASS>), dim3(blocks), dim3(THREADS), 0, st, p);
+  else if (wide)
+    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true, false>), dim3(blocks), dim3(THREADS), 0, st, p);
   else
-    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, false>), dim3(blocks), dim3(THREADS), 0, st, p);
+    hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, false, false>), dim3(blocks), dim3(THREADS), 0, st, p);
 }
 
 // As few lanes as hold the row with one granule each up to a wave (a wave

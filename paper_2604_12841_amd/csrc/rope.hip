@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const Rope p) {
         if (chunk * CP + k >= p.turned) o[a] = v[a], o[b] = v[b];
       }
       if constexpr (CP == 8) {
-        store8(oh + first, o, false);
-        store8(oh + second, o + 8, false);
+        store8(oh + first, o);
+        store8(oh + second, o + 8);
       } else {
         store1(oh + first, o[0]);
         store1(oh + second, o[1]);

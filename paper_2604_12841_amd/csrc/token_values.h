@@ -34,23 +34,26 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
 // anything else: it is stored past the caches, which leaves them, and the memory's time, to what is still read.
 constexpr long long PASSING_BYTES = 128ll << 20;
 
-__device__ __forceinline__ void store16(void* p, const uint4 w, bool passing) {
+template <bool PASSING>
+__device__ __forceinline__ void store16(void* p, const uint4 w) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-  if (passing)  // (written out: the compiler makes one ordinary store of the two branches)
-    asm volatile("global_store_dwordx4 %0, %1, off nt" ::"v"(p), "v"(__builtin_bit_cast(u32x4, w)));
+  if constexpr (PASSING)
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
   else
     *(uint4*)p = w;
 }
 
-__device__ __forceinline__ void store8(uint16_t* p, const float* v, bool passing) {
+template <bool PASSING = false>
+__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
   uint4 w;
   w.x = bf16_pack(v[0], v[1]), w.y = bf16_pack(v[2], v[3]);
   w.z = bf16_pack(v[4], v[5]), w.w = bf16_pack(v[6], v[7]);
-  store16(p, w, passing);
+  store16<PASSING>(p, w);
 }
 
 // (Never past the caches: each of the two stores covers half of every line, which the L2 has to put together.)
-__device__ __forceinline__ void store8(float* p, const float* v, bool) {
+template <bool PASSING = false>
+__device__ __forceinline__ void store8(float* p, const float* v) {
   *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
   *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }

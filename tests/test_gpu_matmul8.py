@@ -137,3 +137,25 @@ def test_refusals():
         pdx.matmul8(torch.zeros(1, K, dtype=torch.int8, device="cuda"), sa[:1], torch.zeros(1, K, dtype=torch.int8, device="cuda"), sw[:1],
                     out[:1, :1])
     assert e.value.status == pdx.PD_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_results_larger_than_the_caches(kind, out):
+    """Results that are stored past the caches are those of the rows one part at a time (sums do not depend on the tile
+    that a row is in: exact, or k by k in order)."""
+    M, N, K = 70000, 1032, 256
+    g = tc.gen(2)
+    a, w = codes(g, M, K, kind), codes(g, N, K, kind)
+    sa, sw, b = torch.rand(M, device="cuda"), torch.rand(N, device="cuda") / 1000, tc.normal(g, N)
+    whole = torch.empty(M, N, dtype=tc.DTYPES[out], device="cuda")
+    pdx.matmul8(a, sa, w, sw, whole, bias=b, act="gelu")
+    part = torch.empty(1000, N, dtype=tc.DTYPES[out], device="cuda")
+    for lo in (0, 33000, 69000):
+        pdx.matmul8(a[lo:lo + 1000], sa[lo:lo + 1000], w, sw, part, bias=b, act="gelu")
+        torch.cuda.synchronize()
+        want, size = tc.matmul64(a[lo:lo + 1000], sa[lo:lo + 1000], w, sw, b, "gelu")
+        for o in (part, whole[lo:lo + 1000]):
+            assert torch.all((o.double() - want).abs() <= tc.matmul_tolerance(want, size, b, kind == "int8", o.dtype, K))
+        if kind == "int8":
+            assert torch.equal(part, whole[lo:lo + 1000])

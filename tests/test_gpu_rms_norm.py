@@ -153,3 +153,19 @@ def test_refusals():
         assert e.value.status == pdx.PD_ERR_INVALID_ARG
     with pytest.raises(pdx.PredecoderError):  # rows of the output on top of each other
         pdx.rms_norm(x, out=torch.zeros(64, device="cuda").expand(4, 64))
+
+
+@pytest.mark.parametrize("width", [64, 512, 1024])
+def test_results_larger_than_the_caches(width):
+    """Results that are stored past the caches are the same as those of the rows one part at a time."""
+    rows = (129 << 20) // (2 * width)
+    g = tc.gen(width)
+    x, r = rows_of(g, rows, width, torch.bfloat16), rows_of(g, rows, width, torch.bfloat16)
+    whole = run(x, None, r, torch.float8_e4m3fn)
+    n = rows // 3
+    for lo in (0, n, 2 * n):
+        for a, b in zip(whole, run(x[lo:lo + n], None, r[lo:lo + n], torch.float8_e4m3fn)):
+            assert torch.equal(a[lo:lo + n].view(torch.uint8), b.view(torch.uint8))
+    s64, y = tc.norm64(x[-999:], r[-999:], None)
+    assert torch.all((whole[0][-999:].double() - s64).abs() <= (tc.U16 + tc.U32) * s64.abs())
+    assert torch.all((whole[1][-999:].double() - y).abs() <= (tc.U16 + tc.NORM_REL) * y.abs())
