@@ -130,12 +130,15 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
     }
     if (p.sum) store_row<T, LPR, NV, WIDE, PASSING>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
     float square = 0.0f, most = 0.0f, check = 0.0f;
+    float low[8 * NV];  // what the rounding of s gain lost
 #pragma unroll
     for (int e = 0; e < 8 * NV; ++e) {
       square = fmaf(s[e], s[e], square);
-      s[e] *= g[e];
-      most = fmaxf(most, fabsf(s[e]));  // drops NaN
-      check = fmaf(s[e], 0.0f, check);  // NaN from an infinite or NaN s gain
+      const float v = s[e] * g[e];
+      low[e] = fmaf(s[e], g[e], -v);
+      s[e] = v;
+      most = fmaxf(most, fabsf(v));  // drops NaN
+      check = fmaf(v, 0.0f, check);  // NaN from an infinite or NaN s gain
     }
     if (!(check == 0.0f)) most = INFINITY;
     reduce_row<LPR>(square, most, shared);
@@ -150,12 +153,19 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
       const bool finite = square < INFINITY && most < INFINITY;  // false for a NaN square
       // rows of tiny values are lifted by a power of two, so that Q / most stays finite
       const float lift = most < 0x1p-64f ? 0x1p64f : 1.0f;
-      const float q = finite && most > 0.0f ? p.qmax / (most * lift) : 0.0f;
+      // s gain and Q / most to twice the precision: a code then has the one rounding that the format makes, but for values
+      // within 2^-24 of halfway between two codes
+      const bool codes = finite && most > 0.0f;
+      const float big = most * lift, q = codes ? p.qmax / big : 0.0f;
+      const float q_low = fmaf(-q, big, p.qmax) * (q / p.qmax);
       if (lane == 0) p.scales[row] = finite ? most * inv / p.qmax : NAN;
       uint8_t* c = p.codes + row * p.codes_stride;
       float y[8 * NV];
 #pragma unroll
-      for (int e = 0; e < 8 * NV; ++e) y[e] = finite ? (s[e] * lift) * q : 0.0f;
+      for (int e = 0; e < 8 * NV; ++e) {
+        const float v = s[e] * lift;
+        y[e] = codes ? fmaf(v, q, fmaf(v, q_low, low[e] * lift * q)) : 0.0f;
+      }
       if constexpr (WIDE) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
