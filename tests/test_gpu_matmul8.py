@@ -60,7 +60,7 @@ def test_strides_and_alignment(M, N, K, kind, pad, shift, out_pad):
     check(M, N, K, kind, "fp32", False, "none", pad, shift, out_pad)
 
 
-@pytest.mark.parametrize("M,N", [(3, 5), (300, 512)])
+@pytest.mark.parametrize("M,N", [(3, 5), (300, 512), (4000, 640), (20000, 1032)])  # every kernel
 def test_no_sum(M, N):
     """K = 0: the activation of the bias."""
     bias = torch.linspace(-2, 2, N, device="cuda")
