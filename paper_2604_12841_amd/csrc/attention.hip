@@ -207,7 +207,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   // leave XCDs idle where items see unequal numbers of keys.
   unsigned item = ((blockIdx.x >> 3) / RUN * 8 + (blockIdx.x & 7)) * RUN + (blockIdx.x >> 3) % RUN;
   if (item >= p.items) return;
-  const int row_tile = item % p.row_tiles;
+  // (with rounds seen up to a row's own, later rows see more: they start first)
+  const int row_tile = p.causal ? p.row_tiles - 1 - (int)(item % p.row_tiles) : (int)(item % p.row_tiles);
   item /= p.row_tiles;
   const int split = item % p.splits;
   item /= p.splits;
