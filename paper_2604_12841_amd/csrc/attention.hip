@@ -38,6 +38,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 64;  // keys of a noted tile
+constexpr int SHORT = 4 * TILE;  // up to as many keys: no notes, their sites stay in LDS
 constexpr int RUN = 4;    // neighbouring work items of one XCD
 constexpr int FEW_SPLITS = 32;  // up to as many: a row's splits that saw nothing leave no result
 // tanh u for |u| <= 0.35 is u (TANH1 + u^2 (TANH3 + u^2 TANH5)) within 4.9e-7 (fitted for the least largest error)
@@ -197,8 +198,10 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   constexpr int NB = TK / 32;                 // blocks of 32 keys
   __shared__ __attribute__((aligned(16))) uint8_t lk[2][TK * DP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t lv[2][TK * DP * 2];
-  __shared__ uint4 ls[2][TK];  // ordered sites
-  __shared__ __attribute__((aligned(16))) uint32_t lb[2][TK];
+  // ordered sites and their bytes: with notes of the step's keys (at buf * TK); without, of all keys, or, if there are
+  // no sites, of the last tile's, for its end
+  __shared__ uint4 ls[SHORT];
+  __shared__ __attribute__((aligned(16))) uint32_t lb[SHORT];
   __shared__ int lq[4][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
 
@@ -340,17 +343,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         if (v_column < p.head_dim) send16(vs + key * p.v_t + v_column, lv[buf] + slot);
       }
     }
-    if (wave == 0 && lane < TK) {
-      if (notes) {
-        send16(ordered_sites + k0, 16u * lane, ls[buf]);
-      } else {
-        int4 s = make_int4(0, 0, 0, lane <= most_key ? 0 : -1);
-        if (sites && lane <= most_key) s = sites[k0 + lane];
-        ls[buf][lane] = ordered(s);
-        lb[buf][lane] = site_bytes(s);
-      }
-    }
-    if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0, 4u * lane, lb[buf]);
+    if (notes && wave == 0 && lane < TK) send16(ordered_sites + k0, 16u * lane, ls + buf * TK);
+    if (BIAS && notes && wave == NW - 1 && lane < TK) send4(bytes + k0, 4u * lane, lb + buf * TK);
   };
 
   f32x16 o[DP / 32];
@@ -373,6 +367,15 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) k_off[s] = k_place<DP>(lane & 31, 2 * s + half);
 
+  if (!notes) {
+    const int first = sites ? 0 : max(p.n_k - 1, 0) / TILE * TILE;
+    for (int key = tid; key < (sites ? SHORT : TILE); key += NT) {
+      int4 s = make_int4(0, 0, 0, first + key < p.n_k ? 0 : -1);
+      if (sites && key < p.n_k) s = sites[key];
+      ls[key] = ordered(s);
+      lb[key] = site_bytes(s);
+    }
+  }
   int tile = next_tile(), step = 0, buf = 0;
   Tile note = {};
   if (tile >= 0) {
@@ -391,6 +394,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
     }
     __builtin_amdgcn_sched_barrier(0);
 
+    const int at_step = notes ? buf * TK : (sites ? tile * TILE : 0) + step * TK;  // where the step's sites are
     if (!notes || meets(note, wv_min, wv_max, wt_max)) {
       f32x16 z[NB];
 #pragma unroll
@@ -434,8 +438,10 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
                 (!p.causal || note.tmax <= wt_min || note.tmax <= p.prefix_last) &&
                 (!BIAS || (w_bytes && (note.flags & BYTES) && (note.tmin >> 8) == (wt_min >> 8) &&
                            (note.tmax >> 8) == (wt_min >> 8)));
+      } else if (!sites) {
+        whole = (tile + 1) * TILE <= p.n_k;
       } else {
-        const uint4 s = ls[buf][lane & (TK - 1)];
+        const uint4 s = ls[at_step + (lane & (TK - 1))];
         const uint32_t t0 = (uint32_t)wt_min ^ 0x80000000u, seen_by_all = p.causal ? (uint32_t)max(wt_min, p.prefix_last) ^ 0x80000000u : ~0u;
         whole = w_plain && __all(s.w == (uint32_t)wv_min && s.x <= seen_by_all &&
                                  (!BIAS || ((s.x ^ t0) < 256u && (s.y ^ 0x80000000u) < 256u && (s.z ^ 0x80000000u) < 256u)));
@@ -447,7 +453,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             uint4 w = make_uint4(0, 0, 0, 0);
-            if constexpr (BIAS) w = *(const uint4*)&lb[buf][32 * n + 8 * g + 4 * half];
+            if constexpr (BIAS) w = *(const uint4*)&lb[at_step + 32 * n + 8 * g + 4 * half];
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -476,7 +482,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const uint4 key = ls[buf][32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
+            const uint4 key = ls[at_step + 32 * n + 8 * (e >> 2) + 4 * half + (e & 3)];
             uint32_t dist = 0;
             if constexpr (BIAS) dist = far_add(own.x, key.x, far_add(own.y, key.y, far_add(own.z, key.z, 0)));
             const float x = score(z[n][e], dist);
@@ -731,8 +737,8 @@ Plan plan_for(const pd_attention_args* a) {
   n.waves = rows <= 32 ? 1 : 10 * (full4 - full2) > full4 ? 2 : 4;
   n.row_tiles = (int)((rows + 32 * n.waves - 1) / (32 * n.waves));
   n.tiles = (int)(((long long)a->n_k + TILE - 1) / TILE);
-  // up to four tiles are read whole: the notes' launch would cost more than it saves
-  n.notes = a->k_sites && n.tiles > 4;
+  // a few tiles are read whole: the notes' launch would cost more than it saves
+  n.notes = a->k_sites && a->n_k > SHORT;
   const long long heads = (long long)a->kv_heads * a->batch, whole = n.row_tiles * heads;
   // Splits: to fill the card once (512 workgroups of four waves, or 2048 waves of few rows), down to 8 (2) tiles each;
   // and, while they keep 32 tiles, until there are eight times as many, which evens out rows that see unequal numbers of tiles.  A
