@@ -32,48 +32,63 @@ struct Norm {
   float* scales;
   long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
   int int8;
-  bool passing;  // bf16 sum and out, see token_values.h
+  bool passing;  // sum and out, see token_values.h
 };
 
-// The column of value e (0 .. 8 NV - 1) of a lane: granules of 8 neighbours,
-// or (rows without wide loads) one value in every LPR.
-template <int LPR, bool WIDE>
+// The column of value e (0 .. 8 NV - 1) of a lane: V neighbours (16 bytes of
+// the row's type, so that a wave's load or store covers whole lines), or
+// (rows without wide loads) one value in every LPR.
+template <int LPR, int V, bool WIDE>
 __device__ __forceinline__ int column(int lane, int e) {
-  return WIDE ? ((e >> 3) * LPR + lane) * 8 + (e & 7) : e * LPR + lane;
+  return WIDE ? (e / V * LPR + lane) * V + e % V : e * LPR + lane;
 }
 
-template <typename T, int LPR, int NV, bool WIDE>
+template <int V>
+__device__ __forceinline__ void load_some(const uint16_t* p, float* v) {
+  load16(p, v);
+}
+template <int V>
+__device__ __forceinline__ void load_some(const float* p, float* v) {
+  if constexpr (V == 8)
+    load8(p, v);
+  else
+    load16(p, v);
+}
+
+template <typename T, int LPR, int NV, int V, bool WIDE>
 __device__ __forceinline__ void load_row(const T* __restrict__ p, int lane, int width, float (&v)[8 * NV]) {
   if constexpr (WIDE) {
 #pragma unroll
-    for (int g = 0; g < NV; ++g) {
-      const int c = column<LPR, true>(lane, 8 * g);
-      float t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (c < width) load8(p + c, t);
+    for (int g = 0; g < 8 * NV / V; ++g) {
+      const int c = column<LPR, V, true>(lane, V * g);
+      float t[V];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * g + e] = t[e];
+      for (int e = 0; e < V; ++e) t[e] = 0.0f;
+      if (c < width) load_some<V>(p + c, t);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[V * g + e] = t[e];
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8 * NV; ++e) {
-      const int c = column<LPR, false>(lane, e);
+      const int c = column<LPR, V, false>(lane, e);
       v[e] = c < width ? load1(p + c) : 0.0f;
     }
   }
 }
 
-template <typename T, int LPR, int NV, bool WIDE, bool PASSING>
+template <typename T, int LPR, int NV, int V, bool WIDE, bool PASSING>
 __device__ __forceinline__ void store_row(T* __restrict__ p, int lane, int width, const float (&v)[8 * NV]) {
   if constexpr (WIDE) {
 #pragma unroll
-    for (int g = 0; g < NV; ++g) {
-      const int c = column<LPR, true>(lane, 8 * g);
-      if (c < width) store8<PASSING>(p + c, &v[8 * g]);
+    for (int g = 0; g < 8 * NV / V; ++g) {
+      const int c = column<LPR, V, true>(lane, V * g);
+      if (c < width) store16<PASSING>(p + c, &v[V * g]);
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8 * NV; ++e) {
-      const int c = column<LPR, false>(lane, e);
+      const int c = column<LPR, V, false>(lane, e);
       if (c < width) store1(p + c, v[e]);
     }
   }
@@ -109,26 +124,27 @@ template <typename T, int LPR, int NV, bool WIDE, bool PASSING>
 __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const Norm p) {
   constexpr int THREADS = LPR > 256 ? LPR : 256;
   constexpr int ROWS = THREADS / LPR;  // rows of a workgroup
+  constexpr int V = 16 / (int)sizeof(T);
   __shared__ float shared[LPR > 64 ? 2 * (LPR / 64) : 1];
   const int lane = threadIdx.x % LPR;
   for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / LPR; row < p.rows;
        row += (long long)gridDim.x * ROWS) {
     float s[8 * NV];
-    load_row<T, LPR, NV, WIDE>((const T*)p.x + row * p.x_stride, lane, p.width, s);
+    load_row<T, LPR, NV, V, WIDE>((const T*)p.x + row * p.x_stride, lane, p.width, s);
     if (p.residual) {
       float r[8 * NV];
-      load_row<T, LPR, NV, WIDE>((const T*)p.residual + row * p.residual_stride, lane, p.width, r);
+      load_row<T, LPR, NV, V, WIDE>((const T*)p.residual + row * p.residual_stride, lane, p.width, r);
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) s[e] += r[e];
     }
     float g[8 * NV];
     if (p.gain) {
-      load_row<float, LPR, NV, WIDE>(p.gain, lane, p.width, g);
+      load_row<float, LPR, NV, V, WIDE>(p.gain, lane, p.width, g);
     } else {
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) g[e] = 1.0f;
     }
-    if (p.sum) store_row<T, LPR, NV, WIDE, PASSING>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
+    if (p.sum) store_row<T, LPR, NV, V, WIDE, PASSING>((T*)p.sum + row * p.sum_stride, lane, p.width, s);
     float square = 0.0f, most = 0.0f, check = 0.0f;
     float low[8 * NV];  // what the rounding of s gain lost
 #pragma unroll
@@ -147,46 +163,47 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
       float y[8 * NV];
 #pragma unroll
       for (int e = 0; e < 8 * NV; ++e) y[e] = s[e] * inv;
-      store_row<T, LPR, NV, WIDE, PASSING>((T*)p.out + row * p.out_stride, lane, p.width, y);
+      store_row<T, LPR, NV, V, WIDE, PASSING>((T*)p.out + row * p.out_stride, lane, p.width, y);
     }
     if (p.codes) {
       const bool finite = square < INFINITY && most < INFINITY;  // false for a NaN square
-      // rows of tiny values are lifted by a power of two, so that Q / most stays finite
-      const float lift = most < 0x1p-64f ? 0x1p64f : 1.0f;
       // s gain and Q / most to twice the precision: a code then has the one rounding that the format makes, but for values
       // within 2^-24 of halfway between two codes
       const bool codes = finite && most > 0.0f;
-      const float big = most * lift, q = codes ? p.qmax / big : 0.0f;
+      float big = most;
+      if (big < 0x1p-64f) {  // rows of tiny values are lifted by a power of two, so that Q / most stays finite
+        big *= 0x1p64f;
+#pragma unroll
+        for (int e = 0; e < 8 * NV; ++e) s[e] *= 0x1p64f, low[e] *= 0x1p64f;
+      }
+      const float q = codes ? p.qmax / big : 0.0f;
       const float q_low = fmaf(-q, big, p.qmax) * (q / p.qmax);
       if (lane == 0) p.scales[row] = finite ? most * inv / p.qmax : NAN;
       uint8_t* c = p.codes + row * p.codes_stride;
       float y[8 * NV];
 #pragma unroll
-      for (int e = 0; e < 8 * NV; ++e) {
-        const float v = s[e] * lift;
-        y[e] = codes ? fmaf(v, q, fmaf(v, q_low, low[e] * lift * q)) : 0.0f;
-      }
+      for (int e = 0; e < 8 * NV; ++e) y[e] = codes ? fmaf(s[e], q, fmaf(s[e], q_low, low[e] * q)) : 0.0f;
       if constexpr (WIDE) {
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          const int at = column<LPR, true>(lane, 8 * n);
-          const float* v = &y[8 * n];
+        for (int n = 0; n < 8 * NV / V; ++n) {
+          const int at = column<LPR, V, true>(lane, V * n);
           if (at < p.width) {
-            uint2 w;
-            if (p.int8) {
-              w.x = int8_pack4(v[0], v[1], v[2], v[3]);
-              w.y = int8_pack4(v[4], v[5], v[6], v[7]);
-            } else {
-              w.x = e4m3_pack4(v[0], v[1], v[2], v[3]);
-              w.y = e4m3_pack4(v[4], v[5], v[6], v[7]);
+            uint32_t w[V / 4];
+#pragma unroll
+            for (int k = 0; k < V / 4; ++k) {
+              const float* v = &y[V * n + 4 * k];
+              w[k] = p.int8 ? int8_pack4(v[0], v[1], v[2], v[3]) : e4m3_pack4_within(v[0], v[1], v[2], v[3]);
             }
-            *(uint2*)(c + at) = w;
+            if constexpr (V == 8)
+              *(uint2*)(c + at) = make_uint2(w[0], w[1]);
+            else
+              *(uint32_t*)(c + at) = w[0];
           }
         }
       } else {
 #pragma unroll
         for (int e = 0; e < 8 * NV; ++e) {
-          const int at = column<LPR, false>(lane, e);
+          const int at = column<LPR, V, false>(lane, e);
           if (at < p.width) c[at] = (uint8_t)(p.int8 ? int8_pack4(y[e], 0, 0, 0) : e4m3_pack4(y[e], 0, 0, 0));
         }
       }
@@ -204,7 +221,7 @@ void launch(const Norm& p, bool wide, hipStream_t st) {
   // bound keeps threads below 2^32.
   const long long most = LPR <= 64 ? 4096 : 1 << 21;
   const unsigned blocks = (unsigned)(want < most ? want : most);
-  constexpr bool MAY_PASS = sizeof(T) == 2 && LPR <= 64;
+  constexpr bool MAY_PASS = LPR <= 64;
   if (wide && MAY_PASS && p.passing)
     hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, true, MAY_PASS>), dim3(blocks), dim3(THREADS), 0, st, p);
   else if (wide)

@@ -48,22 +48,43 @@ __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
   uint4 w;
   w.x = bf16_pack(v[0], v[1]), w.y = bf16_pack(v[2], v[3]);
   w.z = bf16_pack(v[4], v[5]), w.w = bf16_pack(v[6], v[7]);
-  store16<PASSING>(p, w);
+  store16<PASSING>((void*)p, w);
 }
 
-// (Never past the caches: each of the two stores covers half of every line, which the L2 has to put together.)
-template <bool PASSING = false>
 __device__ __forceinline__ void store8(float* p, const float* v) {
   *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
   *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// Four values rounded to the nearest integers (ties to even) within +-127, v0 in bits 0-7.
-__device__ __forceinline__ uint32_t int8_code(float v) {
-  return (uint32_t)(int)__builtin_rintf(__builtin_fminf(__builtin_fmaxf(v, -127.0f), 127.0f)) & 0xffu;
+// 16 bytes of values: eight bf16 or four fp32.
+__device__ __forceinline__ void load16(const uint16_t* p, float* v) { load8(p, v); }
+__device__ __forceinline__ void load16(const float* p, float* v) {
+  const float4 a = *(const float4*)p;
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
 }
+template <bool PASSING>
+__device__ __forceinline__ void store16(uint16_t* p, const float* v) {
+  store8<PASSING>(p, v);
+}
+template <bool PASSING>
+__device__ __forceinline__ void store16(float* p, const float* v) {
+  store16<PASSING>((void*)p, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                                        __float_as_uint(v[3])));
+}
+
+// Four values within +-127.4 rounded to the nearest integers (ties to even), v0 in bits 0-7: added to 3 2^22, a value's
+// integer is in the low bits of the sum.
 __device__ __forceinline__ uint32_t int8_pack4(float v0, float v1, float v2, float v3) {
-  return int8_code(v0) | int8_code(v1) << 8 | int8_code(v2) << 16 | int8_code(v3) << 24;
+  constexpr float SHIFT = 12582912.0f;
+  const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(v1 + SHIFT), __float_as_uint(v0 + SHIFT), 0x0c0c0400u);
+  const uint32_t b = __builtin_amdgcn_perm(__float_as_uint(v3 + SHIFT), __float_as_uint(v2 + SHIFT), 0x04000c0cu);
+  return a | b;
+}
+
+// Four values as E4M3 codes, within the format's range (+-464 rounds to +-448).
+__device__ __forceinline__ uint32_t e4m3_pack4_within(float v0, float v1, float v2, float v3) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v0, v1, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v2, v3, lo, true);
 }
 
 }  // namespace pd
