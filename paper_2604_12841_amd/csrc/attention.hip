@@ -752,7 +752,7 @@ Plan plan_for(const pd_attention_args* a) {
   if (splits < more) splits = more;
   if (splits > MOST_SPLITS) splits = MOST_SPLITS;
   const int dp = a->head_dim <= 32 ? 32 : a->head_dim <= 64 ? 64 : 128;
-  const long long most = (1ll << 30) / (heads * rows * dp * 4);  // 1 GB of workspace
+  const long long most = (1ll << 30) / (dp * 4) / heads / rows;  // 1 GB of workspace (the product could pass 64 bits)
   if (splits > most) splits = most;
   if (splits < 1) splits = 1;
   n.tiles_per_split = (int)((n.tiles + splits - 1) / splits);
@@ -787,7 +787,7 @@ pd_status check(const pd_attention_args* a, bool pointers) {
     // rows are counted in 32 bits, work items and rows of all heads by the launches (threads below 2^32)
     if ((long long)a->n_q * (a->heads / a->kv_heads) >= 1ll << 30) return PD_ERR_UNSUPPORTED;
     const Plan n = plan_for(a);
-    if (n.items >= 1ll << 24 || (n.splits > 1 && (long long)a->n_q * a->heads * a->batch >= 1ll << 24))
+    if (n.items > (1ll << 24) - 8 * RUN || (n.splits > 1 && (long long)a->n_q * a->heads * a->batch >= 1ll << 24))
       return PD_ERR_UNSUPPORTED;
   }
   if (!pointers || !a->batch || !a->heads || !a->n_q) return PD_OK;

@@ -127,3 +127,17 @@ def test_workspace_is_asked_for_before_the_call():
         assert attention(heads=8, n_q=1, n_k=100000, workspace=P + 4) == BAD
     assert tokens._functions().predecoder_attention_workspace(tokens.AttentionArgs(**(a | dict(head_dim=12)))) == 0
     assert tokens._functions().predecoder_attention_workspace(None) == 0
+
+
+def test_sizes_whose_products_pass_64_bits():
+    """kv_heads x batch x rows x bytes of a row = 2^64: refused, the plan's divisions included."""
+    many = dict(batch=32768, heads=32768, kv_heads=32768, head_dim=128, n_q=1 << 25, n_k=64)
+    assert attention(**many) == NO_FORM
+    assert tokens._functions().predecoder_attention_workspace(tokens.AttentionArgs(scale=0.1, **many)) == 0
+
+
+def test_work_items_are_counted_as_they_are_launched():
+    """4095 x 4097 = 2^24 - 1 items are launched as 2^24 workgroups of 256 threads: one thread too many for a grid."""
+    assert attention(batch=4097, heads=4095, kv_heads=4095, n_q=128, n_k=64) == NO_FORM
+    # (many heads, not many: the last size that has a form asks for its workspace and no less)
+    assert attention(batch=4096, heads=4095, kv_heads=4095, n_q=128, n_k=300, q_sites=P, k_sites=P, workspace=None) == BAD
