@@ -865,6 +865,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
     const float u = a->scale / a->cap, c = a->cap * LOG2E;
     p.small = 0.35f / fabsf(u);
     p.poly1 = c * u * TANH1, p.poly3 = c * u * u * u * TANH3, p.poly5 = c * u * u * u * u * u * TANH5;
+    if (!(fabsf(p.poly1) + fabsf(p.poly3) + fabsf(p.poly5) < INFINITY)) p.small = -1.0f;  // 0 x infinity
   } else {
     p.small = p.poly1 = p.poly3 = p.poly5 = 0.0f;
   }

@@ -248,3 +248,11 @@ def test_refusals():
         with pytest.raises(pdx.PredecoderError) as e:
             pdx.attention(t, t, t, torch.empty_like(t, memory_format=torch.contiguous_format))
         assert e.value.status == pdx.PD_ERR_UNSUPPORTED
+
+
+def test_scores_of_zero_under_a_tiny_cap():
+    """scale / cap so large that the small scores' polynomial has no coefficients: scores of zero are zero all the same."""
+    g = tc.gen(18)
+    q, k, v = qkv(g, 1, 70, 130, 2, 1, 64)
+    out, _ = check(torch.zeros_like(q), k, v, cap=1e-8, scale=1.0)
+    assert torch.isfinite(out).all()
