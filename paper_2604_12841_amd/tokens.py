@@ -201,6 +201,7 @@ def matmul8(a, a_scales, w, w_scales, out, bias=None, act="none", stream=None):
     pa, sa = _matrix(a, "a", (M, K), dt, dev)
     pw, sw = _matrix(w, "w", (N, K), dt, dev)
     po, so = _matrix(out, "out", (M, N), to, dev)
+    _need(not isinstance(act, str) or act in _ACTS, "act must be none, gelu or relu")
     code = _ACTS[act] if isinstance(act, str) else int(act)
     _call("predecoder_matmul8", _pack_matmul8(M, N, K, _CODES[dt], _VALUES[to], code, pa, sa,
                                               _vector(a_scales, "a_scales", M, dev), pw, sw,
