@@ -7,7 +7,8 @@
 // One pass: a row is read once into registers (by LPR lanes with NV granules
 // of 8 values each), both statistics -- the sum of s^2 and the largest
 // |s gain| -- come from there, and every output is written from there.  The
-// code needs no division by the norm: it cancels.  Bound by memory.
+// code needs no division by the norm: it cancels.  Bound by memory: 163072 x
+// 512 bf16 with a residual to a sum and E4M3 codes 103 us, 5.7 TB/s.
 #include <hip/hip_runtime.h>
 #include <math.h>
 

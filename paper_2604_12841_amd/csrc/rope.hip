@@ -9,7 +9,8 @@
 // A work item is (token, heads h, h + HS, ..., chunk of pairs): sine and
 // cosine are computed once for its heads, and neighbouring lanes hold
 // neighbouring chunks, then heads, so a wave reads whole lines.  Bound by
-// memory: each value is read and written once.
+// memory: each value is read and written once (163072 tokens x 10 heads x 64
+// bf16: 78 us, 5.4 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
