@@ -6,8 +6,7 @@
 // rounds what is left, and p lo is added, so the angle is as exact at round
 // 100000 as at round 1.
 //
-// A work item is (token, heads h, h + HS, ..., chunk of pairs): sine and
-// cosine are computed once for its heads, and neighbouring lanes hold
+// A work item is (token, head, chunk of pairs): neighbouring lanes hold
 // neighbouring chunks, then heads, so a wave reads whole lines.  Bound by
 // memory: each value is read and written once (163072 tokens x 10 heads x 64
 // bf16: 78 us, 5.4 TB/s).
@@ -26,7 +25,7 @@ constexpr int MAX_PAIRS = 128;
 struct Rope {
   long long tokens;
   int heads, pairs, turned, s0, s1;  // pairs [0, s0) turn with t, [s0, s1) with i, [s1, turned) with j
-  int head_split, chunks;
+  int chunks;
   float sign;
   const int4* sites;
   const void* x;
@@ -50,12 +49,12 @@ __device__ __forceinline__ void sincos_turns(float a, float& s, float& c) {
 // others half a head apart.
 template <typename T, int CP, bool INTER>
 __global__ void __launch_bounds__(256) rope_kernel(const Rope p) {
-  const long long items = p.tokens * p.head_split * p.chunks;
+  const long long items = p.tokens * p.heads * p.chunks;
   for (long long w = (long long)blockIdx.x * 256 + threadIdx.x; w < items; w += (long long)gridDim.x * 256) {
     const int chunk = (int)(w % p.chunks);
     const long long wt = w / p.chunks;
-    const int h0 = (int)(wt % p.head_split);
-    const long long token = wt / p.head_split;
+    const int h = (int)(wt % p.heads);
+    const long long token = wt / p.heads;
     const int4 at = p.sites[token];
     float c[CP], s[CP];
 #pragma unroll
@@ -66,42 +65,38 @@ __global__ void __launch_bounds__(256) rope_kernel(const Rope p) {
       sincos_turns<T>(turns, s[k], c[k]);
       s[k] *= p.sign;
     }
-    const T* x = (const T*)p.x + token * p.x_token;
-    T* out = (T*)p.out + token * p.out_token;
+    const T* x = (const T*)p.x + token * p.x_token + h * p.x_head;
+    T* out = (T*)p.out + token * p.out_token + h * p.out_head;
     const int first = INTER ? 2 * CP * chunk : CP * chunk;
     const int second = INTER ? first + CP : first + p.pairs;
-    for (int h = h0; h < p.heads; h += p.head_split) {
-      const T* xh = x + h * p.x_head;
-      T* oh = out + h * p.out_head;
-      float v[2 * CP], o[2 * CP];
-      if constexpr (CP == 8) {
-        load8(xh + first, v);
-        load8(xh + second, v + 8);
-      } else {
-        v[0] = load1(xh + first);
-        v[1] = load1(xh + second);
-      }
+    float v[2 * CP], o[2 * CP];
+    if constexpr (CP == 8) {
+      load8(x + first, v);
+      load8(x + second, v + 8);
+    } else {
+      v[0] = load1(x + first);
+      v[1] = load1(x + second);
+    }
 #pragma unroll
-      for (int k = 0; k < CP; ++k) {
-        const int a = INTER ? 2 * k : k, b = INTER ? 2 * k + 1 : k + CP;
-        o[a] = v[a] * c[k] - v[b] * s[k];
-        o[b] = v[b] * c[k] + v[a] * s[k];
-        if (chunk * CP + k >= p.turned) o[a] = v[a], o[b] = v[b];
-      }
-      if constexpr (CP == 8) {
-        store8(oh + first, o);
-        store8(oh + second, o + 8);
-      } else {
-        store1(oh + first, o[0]);
-        store1(oh + second, o[1]);
-      }
+    for (int k = 0; k < CP; ++k) {
+      const int a = INTER ? 2 * k : k, b = INTER ? 2 * k + 1 : k + CP;
+      o[a] = v[a] * c[k] - v[b] * s[k];
+      o[b] = v[b] * c[k] + v[a] * s[k];
+      if (chunk * CP + k >= p.turned) o[a] = v[a], o[b] = v[b];
+    }
+    if constexpr (CP == 8) {
+      store8(out + first, o);
+      store8(out + second, o + 8);
+    } else {
+      store1(out + first, o[0]);
+      store1(out + second, o[1]);
     }
   }
 }
 
 template <typename T, int CP>
 void launch(const Rope& p, bool interleaved, hipStream_t st) {
-  const long long items = p.tokens * p.head_split * p.chunks;
+  const long long items = p.tokens * p.heads * p.chunks;
   const long long want = (items + 255) / 256;
   const unsigned blocks = (unsigned)(want < (1 << 23) ? want : (1 << 23));  // threads stay below 2^32
   if (interleaved)
@@ -151,7 +146,6 @@ extern "C" pd_status predecoder_rope(void* hip_stream, const pd_rope_args* a) {
   };
   const bool wide = pairs % 8 == 0 && rows16(p.x, p.x_token, p.x_head) && rows16(p.out, p.out_token, p.out_head);
   p.chunks = wide ? pairs / 8 : pairs;
-  p.head_split = p.heads;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (a->dtype == PD_DTYPE_BF16) {
     if (wide)
