@@ -125,7 +125,9 @@ extern "C" pd_status predecoder_rope(void* hip_stream, const pd_rope_args* a) {
   const int elem = a->dtype == PD_DTYPE_BF16 ? 2 : 4;
   if ((uintptr_t)a->x % elem || (uintptr_t)a->out % elem) return PD_ERR_INVALID_ARG;
   if (a->head_dim > 2 * MAX_PAIRS) return PD_ERR_UNSUPPORTED;
-  if (a->tokens > (1ll << 40) || a->heads > (1 << 20)) return PD_ERR_UNSUPPORTED;  // 64-bit counts of work items
+  // work items are counted in 64 bits
+  if (a->tokens > (1ll << 40) || a->heads > (1 << 20) || a->tokens > (1ll << 62) / ((long long)a->heads * pairs))
+    return PD_ERR_UNSUPPORTED;
   Rope p;
   p.tokens = a->tokens, p.heads = a->heads, p.pairs = pairs, p.turned = (int)turned;
   p.s0 = a->sections[0], p.s1 = a->sections[0] + a->sections[1];

@@ -141,3 +141,7 @@ def test_work_items_are_counted_as_they_are_launched():
     assert attention(batch=4097, heads=4095, kv_heads=4095, n_q=128, n_k=64) == NO_FORM
     # (many heads, not many: the last size that has a form asks for its workspace and no less)
     assert attention(batch=4096, heads=4095, kv_heads=4095, n_q=128, n_k=300, q_sites=P, k_sites=P, workspace=None) == BAD
+
+
+def test_rotary_work_items_stay_within_64_bits():
+    assert rope(tokens=1 << 40, heads=1 << 20, head_dim=256) == NO_FORM
