@@ -9,7 +9,7 @@
 // A work item is (token, head, chunk of pairs): neighbouring lanes hold
 // neighbouring chunks, then heads, so a wave reads whole lines.  Bound by
 // memory: each value is read and written once (163072 tokens x 10 heads x 64
-// bf16: 78 us, 5.4 TB/s).
+// bf16: 77 us, 5.4 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
