@@ -156,7 +156,8 @@ pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
  * <= 64; |coordinate| < 2^29.
  * workspace: device memory of at least predecoder_attention_workspace(args)
  * bytes, 16-byte aligned (NULL if that is 0), not shared by calls that may
- * overlap. */
+ * overlap.
+ * Any finite cap >= 0 is taken (0: none): up to 64 within 1e-6 of the cap, above within 2^-20 of the score. */
 typedef struct pd_attention_args {
   int32_t batch, heads, kv_heads, head_dim;
   int32_t n_q, n_k; /* tokens of one batch entry */

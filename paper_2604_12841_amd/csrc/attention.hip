@@ -48,6 +48,14 @@ constexpr int RUN = 4;    // neighbouring work items of one XCD
 constexpr int FEW_SPLITS = 32;  // up to as many: a row's splits that saw nothing leave no result
 // tanh u for |u| <= 0.35 is u (TANH1 + u^2 (TANH3 + u^2 TANH5)) within 4.9e-7 (fitted for the least largest error)
 constexpr float TANH1 = 0.9999902f, TANH3 = -0.33268409f, TANH5 = 0.12248027f;
+// ... and u (1 + u^2 (TANH3R + u^2 (TANH5R + u^2 TANH7R))) within 4.2e-8 of itself (fitted for the least relative error)
+constexpr float TANH3R = -0.33332664f, TANH5R = 0.13299826f, TANH7R = -0.04914851f;
+
+// Forms of the cap.  CAP_NEAR is off by up to 1e-6 of the cap, however small the score: 6e-5 at the largest cap that
+// takes it, below what the probabilities' rounding moves.  CAP_FAR is off by 2^-20 of the score itself, for caps of any
+// size, and takes longer (16 volumes of 2548 tokens, 8 query and 2 key heads of 64: 445 us against 378).
+enum Cap { CAP_NONE, CAP_NEAR, CAP_FAR };
+constexpr float MOST_NEAR = 64.0f;
 
 // What a tile of keys holds: the range of volumes and of rounds over its tokens (vmin > vmax: none).
 struct Tile {
@@ -69,7 +77,8 @@ struct Attn {
   bool plain_rows;  // the keys of a tile lie within 32-bit offsets, and head_dim fills the rows in LDS
   float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
   float cap_a, cap_b;
-  float small, poly1, poly3, poly5;  // |q.k| <= small: z = x (poly1 + x^2 (poly3 + x^2 poly5)) is the cap
+  float unit, c0;  // CAP_FAR: scale / cap, and scale in log2 units
+  float small, poly1, poly3, poly5;  // |q.k| <= small (0.35 of the cap): CAP_NEAR's z = x (poly1 + x^2 (poly3 + x^2 poly5)) is the cap
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
@@ -194,7 +203,7 @@ __device__ __forceinline__ int v_place(int key, int g) {
   return key * (DP * 2) + ((g ^ turn) << 4);
 }
 
-template <int DP, int NW, bool CAP, bool BIAS>
+template <int DP, int NW, Cap CAP, bool BIAS>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW == 2 && DP < 128 ? 2 : 1) attention_kernel(const Attn p) {
   constexpr int TK = NW == 1 ? 32 : 64;       // keys of a step
   constexpr int NT = NW * 64, ROWS = NW * 32;
@@ -412,10 +421,41 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
           z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z[n], 0, 0, 0);
         }
       }
-      const float off = (CAP ? p.cap_b : 0.0f) - top, off_small = -top;
+      const float off = (CAP == CAP_NEAR ? p.cap_b : 0.0f) - top, off_small = -top;
+      // whether a score of the wave's tile exceeds 0.35 of the cap
+      auto large = [&] {
+        float size = 0.0f;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) size = fmaxf(fmaxf(size, fabsf(z[n][e])), fabsf(z[n][e + 1]));
+        return __any(size > p.small);
+      };
+      if constexpr (CAP == CAP_FAR) {
+        auto far_capped = [&](auto some_large) {
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = z[n][e], u = x * p.unit, w = u * u;
+              z[n][e] = x * p.c0 * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
+              if constexpr (some_large.value) {
+                const float part = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * p.c1));
+                z[n][e] = fabsf(x) <= p.small ? z[n][e] : fmaf(p.cap_a, part, p.cap_b);
+              }
+              if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four scores' parts in registers at a time
+            }
+        };
+        if (large())
+          far_capped(std::true_type());
+        else
+          far_capped(std::false_type());
+      }
       auto capped = [&](float x, float t) {
-        if constexpr (CAP)
+        if constexpr (CAP == CAP_NEAR)
           return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * p.c1)), t);
+        else if constexpr (CAP == CAP_FAR)
+          return x + t;
         else
           return fmaf(x, p.c1, t);
       };
@@ -469,13 +509,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
           }
       };
       if (whole) {
-        if constexpr (CAP) {
-          float size = 0.0f;
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) size = fmaxf(fmaxf(size, fabsf(z[n][e])), fabsf(z[n][e + 1]));
-          if (__any(size > p.small))
+        if constexpr (CAP == CAP_NEAR) {
+          if (large())
             scores(score_near);
           else
             scores(score_small);
@@ -821,20 +856,26 @@ extern "C" size_t predecoder_attention_workspace(const pd_attention_args* a) {
 
 namespace {
 
-template <int DP, int NW>
-void launch(const Attn& p, bool cap, bool bias, unsigned items, hipStream_t st) {
-  if (cap && bias)
-    hipLaunchKernelGGL((attention_kernel<DP, NW, true, true>), dim3(items), dim3(NW * 64), 0, st, p);
-  else if (cap)
-    hipLaunchKernelGGL((attention_kernel<DP, NW, true, false>), dim3(items), dim3(NW * 64), 0, st, p);
-  else if (bias)
-    hipLaunchKernelGGL((attention_kernel<DP, NW, false, true>), dim3(items), dim3(NW * 64), 0, st, p);
+template <int DP, int NW, Cap CAP>
+void launch_cap(const Attn& p, bool bias, unsigned items, hipStream_t st) {
+  if (bias)
+    hipLaunchKernelGGL((attention_kernel<DP, NW, CAP, true>), dim3(items), dim3(NW * 64), 0, st, p);
   else
-    hipLaunchKernelGGL((attention_kernel<DP, NW, false, false>), dim3(items), dim3(NW * 64), 0, st, p);
+    hipLaunchKernelGGL((attention_kernel<DP, NW, CAP, false>), dim3(items), dim3(NW * 64), 0, st, p);
+}
+
+template <int DP, int NW>
+void launch(const Attn& p, Cap cap, bool bias, unsigned items, hipStream_t st) {
+  if (cap == CAP_NONE)
+    launch_cap<DP, NW, CAP_NONE>(p, bias, items, st);
+  else if (cap == CAP_NEAR)
+    launch_cap<DP, NW, CAP_NEAR>(p, bias, items, st);
+  else
+    launch_cap<DP, NW, CAP_FAR>(p, bias, items, st);
 }
 
 template <int DP>
-void launch_width(const Attn& p, const Plan& n, bool cap, bool bias, hipStream_t st) {
+void launch_width(const Attn& p, const Plan& n, Cap cap, bool bias, hipStream_t st) {
   const unsigned blocks = (p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN);
   if (n.waves == 1)
     launch<DP, 1>(p, cap, bias, blocks, st);
@@ -865,16 +906,21 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.n_q = a->n_q, p.n_k = a->n_k, p.rows = a->n_q * p.group;
   p.items = (unsigned)n.items, p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
   p.prefix_last = a->prefix - 1, p.causal = a->causal;
-  p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / a->cap : a->scale * LOG2E;
+  const Cap cap = !(a->cap > 0.0f) ? CAP_NONE : a->cap <= MOST_NEAR ? CAP_NEAR : CAP_FAR;
+  // (caps past 2^126, whose double would leave the range, differ from it for scores that are themselves of such size alone)
+  const float most_cap = fminf(a->cap, 0x1p126f);
+  p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / most_cap : a->scale * LOG2E;
   if (a->cap > 0.0f) {
-    const float u = a->scale / a->cap, c = a->cap * LOG2E;
+    const float u = a->scale / most_cap, c = most_cap * LOG2E;
     p.small = 0.35f / fabsf(u);
     p.poly1 = c * u * TANH1, p.poly3 = c * u * u * u * TANH3, p.poly5 = c * u * u * u * u * u * TANH5;
-    if (!(fabsf(p.poly1) + fabsf(p.poly3) + fabsf(p.poly5) < INFINITY)) p.small = -1.0f;  // 0 x infinity
+    if (cap == CAP_NEAR && !(fabsf(p.poly1) + fabsf(p.poly3) + fabsf(p.poly5) < INFINITY))
+      p.small = -1.0f;  // 0 x infinity
   } else {
     p.small = p.poly1 = p.poly3 = p.poly5 = 0.0f;
   }
-  p.cap_a = -2.0f * a->cap * LOG2E, p.cap_b = a->cap * LOG2E;
+  p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
+  p.unit = a->cap > 0.0f ? a->scale / most_cap : 0.0f, p.c0 = a->scale * LOG2E;
   p.q = (const uint16_t*)a->q, p.k = (const uint16_t*)a->k, p.v = (const uint16_t*)a->v, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;
   p.k_b = a->k_batch_stride, p.k_t = a->k_token_stride, p.k_h = a->k_head_stride;
@@ -903,7 +949,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
     hipLaunchKernelGGL(attention_notes_kernel, dim3((unsigned)(n.tiles + 3) / 4, lists), dim3(256), 0, st, p.k_sites,
                        p.k_sites_b, p.n_k, p.tiles, notes, bytes, ordered_sites);
   }
-  const bool cap = a->cap > 0.0f, bias = a->slopes != nullptr;
+  const bool bias = a->slopes != nullptr;
   if (a->head_dim <= 32)
     launch_width<32>(p, n, cap, bias, st);
   else if (a->head_dim <= 64)
