@@ -24,6 +24,7 @@
 // 2548 tokens, 8 query and 2 key heads of 64, 379 us (561 TFLOP/s; vector units
 // 0.69, matrix units 0.24 busy).  One token against four caches of up to 39200:
 // 27.6 us, the keys' part at 3.6 TB/s.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -909,7 +910,9 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   const Cap cap = !(a->cap > 0.0f) ? CAP_NONE : a->cap <= MOST_NEAR ? CAP_NEAR : CAP_FAR;
   // (caps past 2^126, whose double would leave the range, differ from it for scores that are themselves of such size alone)
   const float most_cap = fminf(a->cap, 0x1p126f);
-  p.c1 = a->cap > 0.0f ? a->scale * 2.0f * LOG2E / most_cap : a->scale * LOG2E;
+  // kept finite, so that scores of zero stay zero; at the bounds any other score is past the cap, or past all of its row
+  auto finite = [](float c) { return fminf(fmaxf(c, -FLT_MAX), FLT_MAX); };
+  p.c1 = finite(a->cap > 0.0f ? a->scale * 2.0f * LOG2E / most_cap : a->scale * LOG2E);
   if (a->cap > 0.0f) {
     const float u = a->scale / most_cap, c = most_cap * LOG2E;
     p.small = 0.35f / fabsf(u);
@@ -920,7 +923,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
     p.small = p.poly1 = p.poly3 = p.poly5 = 0.0f;
   }
   p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
-  p.unit = a->cap > 0.0f ? a->scale / most_cap : 0.0f, p.c0 = a->scale * LOG2E;
+  p.unit = a->cap > 0.0f ? finite(a->scale / most_cap) : 0.0f, p.c0 = finite(a->scale * LOG2E);
   p.q = (const uint16_t*)a->q, p.k = (const uint16_t*)a->k, p.v = (const uint16_t*)a->v, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;
   p.k_b = a->k_batch_stride, p.k_t = a->k_token_stride, p.k_h = a->k_head_stride;

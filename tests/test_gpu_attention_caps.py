@@ -65,3 +65,12 @@ def test_scores_past_a_large_cap(nk):
     q, k, v = qkv(g, 1, 70, nk, 2, 2, 64, 1.5)
     check(q, k, v, cap=100.0, scale=20.0)
     check(q, k, v, cap=100.0, scale=-4.0)
+
+
+@pytest.mark.parametrize("cap,scale", [(1e-39, 1.0), (1e-30, 1e20), (0.0, 3e38), (50.0, 3e38), (100.0, 3e38)])
+@pytest.mark.parametrize("nk", [64, 130])
+def test_scores_of_zero_where_scale_and_cap_leave_the_range(cap, scale, nk):
+    """Scores of zero stay zero though scale / cap, or the scale in the softmax's units, is past the largest number."""
+    g = tc.gen(nk + 1)
+    q, k, v = qkv(g, 1, 70, nk, 2, 1, 64, 0.0)
+    assert torch.isfinite(check(q, k, v, cap=cap, scale=scale)).all()
