@@ -916,6 +916,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   if (a->cap > 0.0f) {
     const float u = a->scale / most_cap, c = most_cap * LOG2E;
     p.small = 0.35f / fabsf(u);
+    if (cap == CAP_NEAR) p.small = fminf(p.small, 0x1p60f);  // its polynomial takes the square
     p.poly1 = c * u * TANH1, p.poly3 = c * u * u * u * TANH3, p.poly5 = c * u * u * u * u * u * TANH5;
     if (cap == CAP_NEAR && !(fabsf(p.poly1) + fabsf(p.poly3) + fabsf(p.poly5) < INFINITY))
       p.small = -1.0f;  // 0 x infinity

@@ -74,3 +74,12 @@ def test_scores_of_zero_where_scale_and_cap_leave_the_range(cap, scale, nk):
     g = tc.gen(nk + 1)
     q, k, v = qkv(g, 1, 70, nk, 2, 1, 64, 0.0)
     assert torch.isfinite(check(q, k, v, cap=cap, scale=scale)).all()
+
+
+@pytest.mark.parametrize("cap", [30.0, 1e4])
+@pytest.mark.parametrize("nk", [64, 130])
+def test_products_whose_square_leaves_the_range(cap, nk):
+    """Usual scores of huge products and a tiny scale."""
+    g = tc.gen(nk + 2)
+    q, k, v = qkv(g, 1, 70, nk, 2, 1, 64, 1e10)
+    check(q, (1e10 * k.float()).to(torch.bfloat16), v, cap=cap, scale=2.0 ** -70)
