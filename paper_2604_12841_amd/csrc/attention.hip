@@ -253,7 +253,10 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
   // the last round that the row sees
   const uint32_t last = p.causal ? (uint32_t)max(at.x, p.prefix_last) ^ 0x80000000u : ~0u;
   const uint32_t at_bytes = site_bytes(at);
-  const float slope = BIAS ? p.slopes[head] * -LOG2E : 0.0f;
+  // Finite slopes past 2^94 leave a row its nearest tokens alone (negative ones its farthest), as 2^94 does, whose products
+  // with 2^24 (below) and with any distance stay finite.
+  float slope = BIAS ? p.slopes[head] : 0.0f;
+  if (fabsf(slope) < INFINITY) slope = fminf(fmaxf(slope * -LOG2E, -0x1p94f), 0x1p94f);
 
   // what this wave's rows see, and the workgroup's
   const int wv_min = wave_min(there ? at.w : INT_MAX), wv_max = wave_max(there ? at.w : -1);

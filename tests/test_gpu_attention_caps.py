@@ -83,3 +83,19 @@ def test_products_whose_square_leaves_the_range(cap, nk):
     g = tc.gen(nk + 2)
     q, k, v = qkv(g, 1, 70, nk, 2, 1, 64, 1e10)
     check(q, (1e10 * k.float()).to(torch.bfloat16), v, cap=cap, scale=2.0 ** -70)
+
+
+@pytest.mark.parametrize("slope", [1e32, 3.4e38])
+@pytest.mark.parametrize("cap", [0.0, 30.0, 1e4])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,T", [(5, 5), (7, 9)])
+def test_slopes_that_leave_the_nearest_token(slope, cap, causal, d, T):
+    """A finite slope of any size times a distance of zero is zero: every token sees itself alone."""
+    g = tc.gen(d)
+    sites = pdx.volume_sites(d, T)
+    n = sites.shape[0]
+    q, k, v = qkv(g, 1, n, n, 2, 2, 64, 1.5)
+    out = torch.full_like(q, 9.0)
+    pdx.attention(q, k, v, out, sites, sites, cap=cap, slopes=torch.full((2,), slope, device="cuda"), causal=causal)
+    torch.cuda.synchronize()
+    assert torch.equal(out, v)
