@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
                 (!BIAS || (w_bytes && (note.flags & BYTES) && (note.tmin >> 8) == (wt_min >> 8) &&
                            (note.tmax >> 8) == (wt_min >> 8)));
       } else if (!sites) {
-        whole = (tile + 1) * TILE <= p.n_k;
+        whole = p.n_k - tile * TILE >= TILE;
       } else {
         const uint4 s = ls[at_step + (lane & (TK - 1))];
         const uint32_t t0 = (uint32_t)wt_min ^ 0x80000000u, seen_by_all = p.causal ? (uint32_t)max(wt_min, p.prefix_last) ^ 0x80000000u : ~0u;
