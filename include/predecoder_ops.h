@@ -122,8 +122,9 @@ pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args* args);
  * and j (their sum may be less than head_dim / 2: the rest is copied); pair k of
  * a run of n turns by the angle  p base^(-k / n),  p the token's position on that axis:
  *   (u, v) -> (u cos - v sin, v cos + u sin)       (inverse: by the negative angle)
- * Angles are taken to 2^-24 of a turn up to |p| = 2^23.  out may be x itself
- * (same strides).  head_dim even, at most 256. */
+ * Angles are taken to 2^-24 of a turn up to |p| = 2^23 (base >= 1).  out is x
+ * itself (same strides) or does not overlap it; rows of out do not overlap each
+ * other.  head_dim even, at most 256. */
 typedef struct pd_rope_args {
   int64_t tokens;
   int32_t heads, head_dim;

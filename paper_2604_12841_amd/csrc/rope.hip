@@ -128,6 +128,11 @@ extern "C" pd_status predecoder_rope(void* hip_stream, const pd_rope_args* a) {
   // work items are counted in 64 bits
   if (a->tokens > (1ll << 40) || a->heads > (1 << 20) || a->tokens > (1ll << 62) / ((long long)a->heads * pairs))
     return PD_ERR_UNSUPPORTED;
+  // rows of out may not overlap, and out may be x only as it is
+  if (!rows_apart(a->head_dim, {{a->tokens, a->out_token_stride}, {a->heads, a->out_head_stride}})) return PD_ERR_INVALID_ARG;
+  if (a->out == a->x && ((a->tokens > 1 && a->out_token_stride != a->x_token_stride) ||
+                         (a->heads > 1 && a->out_head_stride != a->x_head_stride)))
+    return PD_ERR_INVALID_ARG;
   Rope p;
   p.tokens = a->tokens, p.heads = a->heads, p.pairs = pairs, p.turned = (int)turned;
   p.s0 = a->sections[0], p.s1 = a->sections[0] + a->sections[1];

@@ -1,14 +1,40 @@
 // token_values.h -- loads and stores of the token operators' values (bf16 as
 // uint16_t bit patterns, fp32) as fp32, one at a time or eight neighbours at
-// a time (16-byte aligned), and int8 codes.
+// a time (16-byte aligned), and int8 codes; on the host, the check of an
+// output's strides.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include "activation.h"
 
 namespace pd {
+
+// One axis of a tensor above its rows: its entries, and the values from one to the next.
+struct Axis {
+  long long size, stride;
+};
+
+// Whether rows of `width` values lie clear of each other, as an output's must: from the narrowest axis up, an axis steps
+// over all that lies within it.
+inline bool rows_apart(long long width, std::initializer_list<Axis> axes) {
+  Axis a[4];
+  int n = 0;
+  for (const Axis& x : axes)
+    if (x.size > 1) a[n++] = x;
+  auto step = [](const Axis& x) { return x.stride < 0 ? -(__int128)x.stride : (__int128)x.stride; };
+  std::sort(a, a + n, [&](const Axis& x, const Axis& y) { return step(x) < step(y); });
+  __int128 extent = width;
+  for (int k = 0; k < n; ++k) {
+    if (step(a[k]) < extent) return false;
+    extent += (a[k].size - 1) * step(a[k]);
+  }
+  return true;
+}
 
 __device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ __forceinline__ float load1(const float* p) { return *p; }

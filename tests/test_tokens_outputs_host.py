@@ -1,0 +1,25 @@
+"""Host-side checks of the token operators' outputs whose rows lie on each other: refused before any device call."""
+import ctypes
+
+import pytest
+
+import paper_2604_12841_amd as pdx
+from paper_2604_12841_amd import tokens
+
+P = 4096  # an aligned address that no call may touch
+BAD = pdx.PD_ERR_INVALID_ARG
+
+
+def rope(**kw):
+    a = dict(tokens=5, heads=3, head_dim=32, dtype=1, sections=(8, 4, 4), base=100.0, sites=P, x=2 * P, x_token_stride=96, x_head_stride=32, out=P,
+             out_token_stride=96, out_head_stride=32) | kw
+    a["sections"] = (ctypes.c_int32 * 3)(*a["sections"])
+    return tokens._functions().predecoder_rope(None, tokens.RopeArgs(**a))
+
+
+@pytest.mark.parametrize("kw", [dict(out_token_stride=0), dict(out_head_stride=0), dict(out_head_stride=31), dict(out_token_stride=95),
+                                dict(out_token_stride=-95), dict(out_token_stride=32, out_head_stride=159), dict(out_token_stride=-(1 << 63), tokens=1 << 30, out_head_stride=0),
+                                # x itself, under other strides
+                                dict(out=2 * P, out_token_stride=128), dict(out=2 * P, out_token_stride=32, out_head_stride=160)])
+def test_rotary_outputs_on_each_other(kw):
+    assert rope(**kw) == BAD
