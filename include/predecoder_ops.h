@@ -154,7 +154,7 @@ pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
  * the probabilities are rounded to bf16 for their product with v, their sum is not.
  * head_dim: a multiple of 8, at most 128; all rows (strides and addresses) of q,
  * k, v and out 16-byte aligned; heads a multiple of kv_heads, heads / kv_heads
- * <= 64; |coordinate| < 2^29.
+ * <= 64; |coordinate| < 2^29.  out overlaps no input, and its rows not each other.
  * workspace: device memory of at least predecoder_attention_workspace(args)
  * bytes, 16-byte aligned (NULL if that is 0), not shared by calls that may
  * overlap.

@@ -845,6 +845,9 @@ pd_status check(const pd_attention_args* a, bool pointers) {
       !rows16(a->v, a->v_batch_stride, a->v_token_stride, a->v_head_stride) ||
       !rows16(a->out, a->out_batch_stride, a->out_token_stride, a->out_head_stride))
     return PD_ERR_UNSUPPORTED;
+  // rows of out may not overlap
+  if (!rows_apart(a->head_dim, {{a->batch, a->out_batch_stride}, {a->n_q, a->out_token_stride}, {a->heads, a->out_head_stride}}))
+    return PD_ERR_INVALID_ARG;
   const size_t need = predecoder_attention_workspace(a);
   if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return PD_ERR_INVALID_ARG;
   return PD_OK;

@@ -23,3 +23,17 @@ def rope(**kw):
                                 dict(out=2 * P, out_token_stride=128), dict(out=2 * P, out_token_stride=32, out_head_stride=160)])
 def test_rotary_outputs_on_each_other(kw):
     assert rope(**kw) == BAD
+
+
+def attention(**kw):
+    a = dict(batch=2, heads=4, kv_heads=2, head_dim=64, n_q=4, n_k=9, scale=0.1)
+    for n in ("q", "k", "v", "out"):
+        a |= {n: P, n + "_batch_stride": 1024, n + "_token_stride": 256, n + "_head_stride": 64}
+    return tokens._functions().predecoder_attention(None, tokens.AttentionArgs(**(a | kw)))
+
+
+@pytest.mark.parametrize("kw", [dict(out_batch_stride=0), dict(out_token_stride=0), dict(out_head_stride=0), dict(out_head_stride=56),
+                                dict(out_token_stride=248), dict(out_token_stride=-248), dict(out_batch_stride=1016),
+                                dict(out_token_stride=64, out_head_stride=248), dict(out_batch_stride=256, out_token_stride=504)])
+def test_attention_outputs_on_each_other(kw):
+    assert attention(**kw) == BAD
