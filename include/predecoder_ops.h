@@ -94,7 +94,8 @@ pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* args);
  *   out[m][n] = act(a_scales[m] w_scales[n] sum_k a[m][k] w[n][k] + bias[n])
  * a: [M][K] codes of the tokens, w: [N][K] codes of the output channels, both of
  * codes_type; int8 sums are exact (K <= 131071), E4M3 sums fp32.  bias [N] or
- * NULL; act: pd_act; out bf16 or fp32 (out_dtype).  K = 0 gives act(bias). */
+ * NULL; act: pd_act (every one of NaN is NaN); out bf16 or fp32 (out_dtype).
+ * K = 0 gives act(bias). */
 typedef struct pd_matmul8_args {
   int64_t M;
   int32_t N, K;

@@ -130,6 +130,16 @@ __device__ __forceinline__ void wait_sent() {  // all but the last N loads are t
   asm volatile("" ::: "memory");
 }
 
+// The activation of a result, which keeps NaN: a row that the norm marked by its scale stays marked.  (The conv layers'
+// ReLU gives 0 for it.)
+template <int ACT>
+__device__ __forceinline__ float activated(float y) {
+  if constexpr (ACT == PD_ACT_RELU)
+    return y <= 0.0f ? 0.0f : y;
+  else
+    return act_fn<ACT>(y);
+}
+
 // The scales, bias, activation and rounding of a wave's blocks, 32 tokens at a time through LDS to whole lines.
 // acc[mb][nb]: tokens m0 + 32 mb, channels n0 + 32 nb on; sa: the scales of this lane's tokens; sw: the channels'
 // scales and, ws further, biases in LDS; `stage`: 4 KB of LDS of this wave's own.
@@ -157,7 +167,7 @@ __device__ __forceinline__ void finish(const Mm& p, typename Acc<SUM>::type (&ac
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            v[e] = act_fn<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * s[e], sa[mb], b[e]));
+            v[e] = activated<ACT>(fmaf((float)acc[mb][nb][4 * g + e] * s[e], sa[mb], b[e]));
           if constexpr (sizeof(T) == 2) {
             const int at = r * ROW + (((4 * q + g) ^ (r >> 1 & (GR - 1))) << 4) + 8 * half;
             *(uint2*)(stage + at) = make_uint2(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]));
