@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
     }
     if (!(check == 0.0f)) most = INFINITY;
     reduce_row<LPR>(square, most, shared);
-    const float inv = 1.0f / sqrtf(fmaf(square, p.inv_width, p.eps));
+    const float mean = fmaf(square, p.inv_width, p.eps);
+    const float inv = mean == 0.0f ? 0.0f : 1.0f / sqrtf(mean);  // (a row of zeros without an eps is zeros)
     if (p.out) {
       float y[8 * NV];
 #pragma unroll
