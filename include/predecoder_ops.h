@@ -143,6 +143,9 @@ typedef struct pd_rope_args {
 
 pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
 
+/* No prefix: causal attention sees a token's own and earlier rounds alone. */
+#define PD_PREFIX_NONE INT32_MIN
+
 /* ---- Attention ----
  *
  * For query token a of head h, and key token b of head h / (heads / kv_heads):
@@ -150,6 +153,8 @@ pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
  *   z -= slopes[h] (|t_a - t_b| + |i_a - i_b| + |j_a - j_b|)  if slopes is given
  *   out = sum_b softmax_b(z) v_b   over the visible tokens b:
  *     volume_a = volume_b >= 0, and with causal t_b <= t_a or t_b < prefix
+ * The prefix is all rounds below it, negative ones too: 0 is none where rounds
+ * count up from 0, PD_PREFIX_NONE is none everywhere.
  * Without sites (both NULL) every token is visible, and slopes, causal and
  * prefix must be unset.  A query that sees nothing gets zeros; keys and values at
  * invisible places do not reach the result, whatever they hold.  bf16 values;
@@ -165,7 +170,7 @@ typedef struct pd_attention_args {
   int32_t batch, heads, kv_heads, head_dim;
   int32_t n_q, n_k; /* tokens of one batch entry */
   float scale, cap;
-  int32_t causal, prefix; /* causal 0 or 1; prefix >= 0 rounds */
+  int32_t causal, prefix; /* causal 0 or 1; prefix >= 0, or PD_PREFIX_NONE */
   const void* q;
   int64_t q_batch_stride, q_token_stride, q_head_stride;
   const void* k;

@@ -73,7 +73,7 @@ struct Attn {
   int rows;  // n_q * group
   unsigned items;  // row_tiles * splits * kv_heads * batch
   int row_tiles, splits, tiles, tiles_per_split;
-  int prefix_last;  // prefix - 1
+  int prefix_last;  // prefix - 1; INT_MIN, below every round: none
   int causal;
   bool plain_rows;  // the keys of a tile lie within 32-bit offsets, and head_dim fills the rows in LDS
   float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
@@ -822,7 +822,8 @@ pd_status check(const pd_attention_args* a, bool pointers) {
   if (!a || a->batch < 0 || a->heads < 0 || a->kv_heads < 0 || a->n_q < 0 || a->n_k < 0) return PD_ERR_INVALID_ARG;
   if (a->head_dim < 1 || !(fabsf(a->scale) < INFINITY) || !(a->cap >= 0.0f) || !(a->cap < INFINITY))
     return PD_ERR_INVALID_ARG;
-  if (a->causal < 0 || a->causal > 1 || a->prefix < 0 || (a->prefix && !a->causal)) return PD_ERR_INVALID_ARG;
+  if (a->causal < 0 || a->causal > 1) return PD_ERR_INVALID_ARG;
+  if (a->prefix != PD_PREFIX_NONE && (a->prefix < 0 || (a->prefix && !a->causal))) return PD_ERR_INVALID_ARG;
   if (a->heads && (!a->kv_heads || a->heads % a->kv_heads)) return PD_ERR_INVALID_ARG;
   if (a->head_dim % 8 || a->head_dim > 128) return PD_ERR_UNSUPPORTED;
   if (a->heads && a->heads / a->kv_heads > 64) return PD_ERR_UNSUPPORTED;
@@ -912,7 +913,7 @@ extern "C" pd_status predecoder_attention(void* hip_stream, const pd_attention_a
   p.head_dim = a->head_dim;
   p.n_q = a->n_q, p.n_k = a->n_k, p.rows = a->n_q * p.group;
   p.items = (unsigned)n.items, p.row_tiles = n.row_tiles, p.splits = n.splits, p.tiles = n.tiles, p.tiles_per_split = n.tiles_per_split;
-  p.prefix_last = a->prefix - 1, p.causal = a->causal;
+  p.prefix_last = a->prefix == PD_PREFIX_NONE ? INT_MIN : a->prefix - 1, p.causal = a->causal;
   const Cap cap = !(a->cap > 0.0f) ? CAP_NONE : a->cap <= MOST_NEAR ? CAP_NEAR : CAP_FAR;
   // (caps past 2^126, whose double would leave the range, differ from it for scores that are themselves of such size alone)
   const float most_cap = fminf(a->cap, 0x1p126f);

@@ -18,6 +18,7 @@ __all__ = ["rms_norm", "matmul8", "rope", "attention", "attention_workspace", "v
            "CODES_E4M3", "CODES_INT8", "OPS_EXPORTS"]
 
 CODES_NONE, CODES_E4M3, CODES_INT8 = 0, 1, 2
+PREFIX_NONE = -(1 << 31)  # PD_PREFIX_NONE
 _ACTS = {"none": ACT_NONE, "gelu": ACT_GELU_TANH, "relu": ACT_RELU}
 _VALUES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32}
 _CODES = {torch.float8_e4m3fn: CODES_E4M3, torch.int8: CODES_INT8}
@@ -264,24 +265,26 @@ def _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, 
         pk, bk = _sites(k_sites, "k_sites", nk, dev, B)
     if scale is None:
         scale = D ** -0.5
-    return (B, H, Hk, D, nq, nk, scale, cap, bool(causal), int(prefix), *fields, pq, bq, pk, bk,
+    return (B, H, Hk, D, nq, nk, scale, cap, bool(causal),
+            PREFIX_NONE if prefix is None else int(prefix), *fields, pq, bq, pk, bk,
             _vector(slopes, "slopes", H, dev))
 
 
 def attention_workspace(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slopes=None, causal=False,
-                        prefix=0):
+                        prefix=None):
     """Bytes of workspace of attention() with these arguments."""
     a = _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix)
     return _by_bytes("predecoder_attention_workspace")(_pack_attention(*a, 0, 0))
 
 
-def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slopes=None, causal=False, prefix=0,
+def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slopes=None, causal=False, prefix=None,
               workspace=None, stream=None):
     """Attention of q [batch][n_q][heads][head_dim] over k, v [batch][n_k][kv_heads][head_dim] into out (bf16).
 
     Scores scale q.k (scale None: head_dim^-1/2), capped by cap tanh(. / cap) if cap > 0, minus slopes[head] times the L1 distance
-    of the sites; over the keys of the query's volume, with causal those of its own and earlier rounds or of rounds
-    below prefix.  sites: [n][4] for all batch entries or [batch][n][4].  workspace: a device tensor of at least
+    of the sites; over the keys of the query's volume, with causal those of its own and earlier rounds or, unless prefix
+    is None, of all rounds below prefix (for 0: the negative ones).  sites: [n][4] for all batch entries or
+    [batch][n][4].  workspace: a device tensor of at least
     attention_workspace() bytes (needed with a raw stream handle; otherwise allocated here)."""
     a = _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix)
     dev = q.get_device()
