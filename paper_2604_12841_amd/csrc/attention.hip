@@ -78,7 +78,6 @@ struct Attn {
   bool plain_rows;  // the keys of a tile lie within 32-bit offsets, and head_dim fills the rows in LDS
   float c1;    // log2 units: without a cap z = c1 x; with it z = cap_b + cap_a / (1 + 2^(c1 x))
   float cap_a, cap_b;
-  float unit, c0;  // CAP_FAR: scale / cap, and scale in log2 units
   float small, poly1, poly3, poly5;  // |q.k| <= small (0.35 of the cap): CAP_NEAR's z = x (poly1 + x^2 (poly3 + x^2 poly5)) is the cap
   const uint16_t* q;
   const uint16_t* k;
@@ -99,6 +98,7 @@ struct Attn {
   float4* part_o;
   int blocks, block_rows, part_c, part_r;
   float2* part_ml;    // [splits][batch][kv_heads][rows]: maximum (log2 units), sum
+  float unit, c0;  // CAP_FAR: scale / cap, and scale in log2 units
 };
 
 // A site as the kernel compares it: coordinates moved to unsigned numbers in the same order, volume -1 for no token.
