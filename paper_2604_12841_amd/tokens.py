@@ -6,6 +6,8 @@ enqueued on the current stream, or on `stream`.
 
 A token is one site of one round of a volume.  Its place is a row (t, i, j, volume) of an int32 tensor ("sites");
 volume < 0 marks a row that holds no token.
+
+The operators are for inference: a tensor that asks for a gradient is refused while gradients are recorded.
 """
 import ctypes
 import struct
@@ -136,12 +138,20 @@ def _index(t, what):
     return index
 
 
+def _lost_gradient(what):
+    """Refuses a tensor that asks for a gradient while gradients are recorded."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s asks for a gradient, which this operator does not give: call it under torch.no_grad()" % what)
+
+
 def _matrix(t, what, shape, dtype, index):
     """Pointer and row stride of a device matrix with contiguous rows; zeros for None."""
     if t is None:
         return 0, 0
     if t.get_device() != index:
         raise ValueError("%s must be a tensor on GPU %d" % (what, index))
+    if t.requires_grad:
+        _lost_gradient(what)
     if t.dtype != dtype:
         raise ValueError("%s has type %s, expected %s" % (what, t.dtype, dtype))
     if t.shape != shape:
@@ -158,6 +168,8 @@ def _vector(t, what, n, index):
         return 0
     if t.get_device() != index:
         raise ValueError("%s must be a tensor on GPU %d" % (what, index))
+    if t.requires_grad:
+        _lost_gradient(what)
     if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s must be a contiguous vector of %d float32 values" % (what, n))
     return t.data_ptr()
@@ -234,6 +246,10 @@ def rope(x, sites, out, sections, base=10000.0, interleaved=False, inverse=False
     _need(len(shape) == 3 and out.shape == shape, "x and out must be [tokens][heads][head_dim] of one shape")
     _need(dt in _VALUES and out.dtype == dt, "x and out must both be bfloat16 or both float32")
     _need(out.get_device() == dev, "x and out must be tensors on one GPU")
+    if x.requires_grad:
+        _lost_gradient("x")
+    if out.requires_grad:
+        _lost_gradient("out")
     n, H, D = shape
     xt, xh, x1 = x.stride()
     ot, oh, o1 = out.stride()
@@ -254,6 +270,8 @@ def _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, 
     for t, what, want in ((q, "q", shape), (k, "k", (B, nk, Hk, D)), (v, "v", (B, nk, Hk, D)), (out, "out", shape)):
         if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != want:
             raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(want)))
+        if t.requires_grad:
+            _lost_gradient(what)
         sb, st, sh, one = t.stride()
         if one != 1 and D > 1:
             raise ValueError("the rows of a head must be contiguous in %s" % what)
