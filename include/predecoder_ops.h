@@ -188,8 +188,9 @@ typedef struct pd_attention_args {
   size_t workspace_bytes;
 } pd_attention_args;
 
-/* Bytes of workspace that a call with these arguments uses (its pointers are
- * not read); 0 for invalid arguments. */
+/* Bytes of workspace that a call with these arguments uses; 0 for invalid ones.
+ * It goes by the sizes, by whether k_sites is NULL and by whether
+ * k_sites_batch_stride is 0: set those as in the call.  No pointer is followed. */
 size_t predecoder_attention_workspace(const pd_attention_args* args);
 
 pd_status predecoder_attention(void* hip_stream, const pd_attention_args* args);
