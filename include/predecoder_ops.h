@@ -164,7 +164,8 @@ pd_status predecoder_rope(void* hip_stream, const pd_rope_args* args);
  * Without sites (both NULL) every token is visible, and slopes, causal and
  * prefix must be unset.  A query that sees nothing gets zeros; keys and values at
  * invisible places do not reach the result, whatever they hold.  bf16 values;
- * the probabilities are rounded to bf16 for their product with v, their sum is not.
+ * the probabilities are rounded to bf16 for their product with v (2^-8 of each),
+ * and their fp32 sum is that of the rounded ones, so that the weights add up to one.
  * head_dim: a multiple of 8, at most 128; all rows (strides and addresses) of q,
  * k, v and out 16-byte aligned; heads a multiple of kv_heads, heads / kv_heads
  * <= 64; |coordinate| < 2^29.  out overlaps no input, and its rows not each other.

@@ -569,7 +569,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : NW ==
         }
         odd = __any((carry & 0x80008000u) != 0);
       }
-      // the probabilities in bf16, keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n, and their sum
+      // the probabilities in bf16, which the matrix instruction takes, keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n;
+      // and the sum of the rounded ones, with which equal values come out as they are
       uint4 pr[NB][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
