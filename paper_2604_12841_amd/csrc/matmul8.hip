@@ -530,7 +530,7 @@ extern "C" pd_status predecoder_matmul8(void* hip_stream, const pd_matmul8_args*
     return PD_ERR_INVALID_ARG;
   if (a->codes_type == PD_CODES_INT8 && a->K > 131071) return PD_ERR_UNSUPPORTED;  // |sum| <= 2^31 - 1
   // threads stay below 2^32
-  if (((a->M + 63) / 64) * (((long long)a->N + 63) / 64) >= (1ll << 24)) return PD_ERR_UNSUPPORTED;
+  if (a->M > (1ll << 30) || ((a->M + 63) / 64) * (((long long)a->N + 63) / 64) >= (1ll << 24)) return PD_ERR_UNSUPPORTED;
   Mm p;
   p.M = a->M, p.N = a->N, p.K = a->K;
   p.a = (const uint8_t*)a->a, p.w = (const uint8_t*)a->w;
