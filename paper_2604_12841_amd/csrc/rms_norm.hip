@@ -294,7 +294,7 @@ extern "C" pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* a
   if ((uintptr_t)a->x % elem || (uintptr_t)a->residual % elem || (uintptr_t)a->sum % elem ||
       (uintptr_t)a->out % elem || (uintptr_t)a->gain % 4 || (uintptr_t)a->scales % 4)
     return PD_ERR_INVALID_ARG;
-  if (a->width > 32768) return PD_ERR_UNSUPPORTED;
+  if (a->width > 32768 || a->rows > (1ll << 40)) return PD_ERR_UNSUPPORTED;  // values and work are counted in 64 bits
   Norm p;
   p.rows = a->rows;
   p.width = a->width;

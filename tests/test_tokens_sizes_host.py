@@ -15,3 +15,9 @@ def matmul(**kw):
 @pytest.mark.parametrize("M,N", [((1 << 63) - 1, 8), (1 << 62, (1 << 31) - 1), (1 << 56, 1 << 20), ((1 << 30) + 1, 1), (1 << 29, 256)])
 def test_products_of_too_many_tiles(M, N):
     assert matmul(M=M, N=N, out_stride=N) == pdx.PD_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,width", [((1 << 63) - 1, 64), (1 << 62, 32768), (1 << 50, 32768), ((1 << 40) + 1, 1)])
+def test_norms_of_too_many_rows(rows, width):
+    a = dict(rows=rows, width=width, dtype=1, codes_type=0, eps=1e-6, x=P, x_stride=width, out=P, out_stride=width)
+    assert tokens._functions().predecoder_rms_norm(None, tokens.NormArgs(**a)) == pdx.PD_ERR_UNSUPPORTED
