@@ -295,6 +295,14 @@ extern "C" pd_status predecoder_rms_norm(void* hip_stream, const pd_norm_args* a
       (uintptr_t)a->out % elem || (uintptr_t)a->gain % 4 || (uintptr_t)a->scales % 4)
     return PD_ERR_INVALID_ARG;
   if (a->width > 32768 || a->rows > (1ll << 40)) return PD_ERR_UNSUPPORTED;  // values and work are counted in 64 bits
+  // an output at an input's address is that input, row for row; two outputs do not share one
+  auto other_rows = [&](const void* out, long long out_stride, const void* in, long long in_stride) {
+    return out && out == in && a->rows > 1 && out_stride != in_stride;
+  };
+  if (other_rows(a->sum, a->sum_stride, a->x, a->x_stride) || other_rows(a->out, a->out_stride, a->x, a->x_stride) ||
+      other_rows(a->sum, a->sum_stride, a->residual, a->residual_stride) ||
+      other_rows(a->out, a->out_stride, a->residual, a->residual_stride) || (a->sum && a->sum == a->out))
+    return PD_ERR_INVALID_ARG;
   Norm p;
   p.rows = a->rows;
   p.width = a->width;

@@ -37,3 +37,15 @@ def attention(**kw):
                                 dict(out_token_stride=64, out_head_stride=248), dict(out_batch_stride=256, out_token_stride=504)])
 def test_attention_outputs_on_each_other(kw):
     assert attention(**kw) == BAD
+
+
+def norm(**kw):
+    a = dict(rows=4, width=64, dtype=1, codes_type=0, eps=1e-6, x=P, x_stride=64, out=2 * P, out_stride=64) | kw
+    return tokens._functions().predecoder_rms_norm(None, tokens.NormArgs(**a))
+
+
+@pytest.mark.parametrize("kw", [dict(out=P, out_stride=72), dict(x_stride=72, out=P), dict(sum=P, sum_stride=72), dict(residual=3 * P, residual_stride=72, sum=3 * P, sum_stride=64),
+                                dict(residual=3 * P, residual_stride=64, out=3 * P, out_stride=128), dict(sum=2 * P, sum_stride=64)])
+def test_norm_outputs_on_inputs_or_each_other(kw):
+    """An input under another stride, or one place for both outputs."""
+    assert norm(**kw) == BAD
