@@ -326,6 +326,7 @@ def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slo
 
 def volume_sites(d, T, volume=0, first_round=0, layout="plaquette", device="cuda"):
     """The sites of a volume's activations in memory order: [T H H][4], H = d + 1 (plaquette layout) or d (paper layout)."""
+    _need(layout in ("plaquette", "paper"), "layout must be plaquette or paper")
     H = d if layout == "paper" else d + 1
     t, i, j = torch.meshgrid(torch.arange(first_round, first_round + T, device=device), torch.arange(H, device=device),
                              torch.arange(H, device=device), indexing="ij")
