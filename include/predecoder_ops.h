@@ -66,10 +66,10 @@ typedef enum pd_codes { PD_CODES_NONE = 0, PD_CODES_E4M3 = 1, PD_CODES_INT8 = 2 
  *           one a row): scale = max |y| / 448 (E4M3) or / 127 (int8).  A row of
  *           zeros (s or s gain) has scale 0 and codes 0; a row whose sum of squares or
  *           whose s gain is not finite in fp32 has scale NaN and codes 0.
- * A row s of zeros has y 0, also for eps = 0.
- * y is computed from the unrounded s.  1 <= width <= 32768,
- * rows <= 2^40.  An output must be
- * one of the inputs itself (same address and stride) or not overlap them. */
+ * A row s of zeros has y 0, also for eps = 0; where the sum of squares alone is
+ * past fp32, y is 0.  y is computed from the unrounded s.
+ * 1 <= width <= 32768, rows <= 2^40.  An output must be one of the inputs itself
+ * (same address and stride) or not overlap them. */
 typedef struct pd_norm_args {
   int64_t rows;
   int32_t width;

@@ -5,25 +5,25 @@
 // One pass over the keys with the running maximum and sum of the softmax.  The
 // heads that share keys are rows of one query matrix: row r is token
 // r / group, head r % group of the key head's group.  A wave takes 32 rows, a
-// workgroup 32 or (four waves) 128, and tiles of keys come through LDS, two in
-// turn: the next one is on its way from memory to registers while this one
-// is worked on.  A wave computes the transposed scores K Q^T, so a lane holds
+// workgroup 32, 64 or 128 (one, two or four waves), and tiles of keys come
+// through LDS, two in turn: the next one is on its way there from memory while
+// this one is worked on.  A wave computes the transposed scores K Q^T, so a lane holds
 // half of the scores of one row (the other half of the wave the rest): maximum
 // and sum need one exchange.  The same registers, rounded to bf16, are the
 // right operand of out^T += V^T P^T, whose sum over keys may run in any order
 // as long as V follows it; V is read transposed from LDS.
 //
 // What to read: a short kernel notes for every tile of 64 keys which volumes
-// and rounds it holds.  A workgroup skips tiles that none of its rows sees, and
+// and rounds it holds (up to 256 keys are all read).  A workgroup skips tiles that none of its rows sees, and
 // tiles that all rows of a wave see whole need no mask.
 //
 // Few rows against many keys: the keys are split over workgroups, each
 // leaves its maximum, sum and unscaled result (fp32), and a last kernel joins them.
 //
 // Bound by vector instructions, 11.6 a score with cap and bias: 16 volumes of
-// 2548 tokens, 8 query and 2 key heads of 64, 379 us (561 TFLOP/s; vector units
+// 2548 tokens, 8 query and 2 key heads of 64, 389 us (546 TFLOP/s; vector units
 // 0.69, matrix units 0.24 busy).  One token against four caches of up to 39200:
-// 27.6 us, the keys' part at 3.6 TB/s.
+// 27.6 us, the keys' part at 3.5 TB/s.
 #include <float.h>
 #include <hip/hip_runtime.h>
 #include <limits.h>
@@ -54,7 +54,7 @@ constexpr float TANH3R = -0.33332664f, TANH5R = 0.13299826f, TANH7R = -0.0491485
 
 // Forms of the cap.  CAP_NEAR is off by up to 1e-6 of the cap, however small the score: 6e-5 at the largest cap that
 // takes it, below what the probabilities' rounding moves.  CAP_FAR is off by 2^-20 of the score itself, for caps of any
-// size, and takes longer (16 volumes of 2548 tokens, 8 query and 2 key heads of 64: 445 us against 378).
+// size, and takes 17 % longer (16 volumes of 2548 tokens, 8 query and 2 key heads of 64: 445 us against 379 in one run).
 enum Cap { CAP_NONE, CAP_NEAR, CAP_FAR };
 constexpr float MOST_NEAR = 64.0f;
 

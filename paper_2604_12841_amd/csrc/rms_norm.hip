@@ -8,7 +8,8 @@
 // of 8 values each), both statistics -- the sum of s^2 and the largest
 // |s gain| -- come from there, and every output is written from there.  The
 // code needs no division by the norm: it cancels.  Bound by memory: 163072 x
-// 512 bf16 with a residual to a sum and E4M3 codes 103 us, 5.7 TB/s.
+// 512 bf16 with a residual to a sum and E4M3 codes 104 us, 5.6 TB/s.  (Rows of more
+// than 8192 columns spill 14 to 71 registers: 4096 x 16384 bf16 173 us.)
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -229,8 +230,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
 template <typename T, int LPR, int NV, bool WIDE, bool PASSING>
 void launch_eps(const Norm& p, unsigned blocks, unsigned threads, hipStream_t st) {
   // Squares of values below 2^-45 lose bits, or all of them, that an eps below 2^-80 does not cover.  Finding the row's
-  // largest value first takes up to 3 % (163072 x 512 bf16 with residual to E4M3: 104 us against 102; 4096 x 16384: 177
-  // against 173).
+  // largest value first takes up to 3 % longer (bf16 with residual to E4M3: 163072 x 512 2 %, 4096 x 16384 3 %).
   if (p.eps < 0x1p-80f)
     hipLaunchKernelGGL((rms_norm_kernel<T, LPR, NV, WIDE, PASSING, true>), dim3(blocks), dim3(threads), 0, st, p);
   else

@@ -39,7 +39,7 @@ template <typename T>
 __device__ __forceinline__ void sincos_turns(float a, float& s, float& c) {
   if constexpr (sizeof(T) == 4) {
     sincospif(2.0f * a, &s, &c);
-  } else {  // the result is rounded to bf16
+  } else {  // within 2^-14, the result is rounded to bf16 (2^-8)
     s = __builtin_amdgcn_sinf(a);
     c = __builtin_amdgcn_cosf(a);
   }
