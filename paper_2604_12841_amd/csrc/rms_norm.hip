@@ -8,7 +8,7 @@
 // of 8 values each), both statistics -- the sum of s^2 and the largest
 // |s gain| -- come from there, and every output is written from there.  The
 // code needs no division by the norm: it cancels.  Bound by memory: 163072 x
-// 512 bf16 with a residual to a sum and E4M3 codes 104 us, 5.6 TB/s.  (Rows of more
+// 512 bf16 with a residual to a sum and E4M3 codes 103 us, 5.7 TB/s.  (Rows of more
 // than 8192 columns spill 14 to 71 registers: 4096 x 16384 bf16 173 us.)
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(LPR > 256 ? LPR : 256) rms_norm_kernel(const N
     if (!(check == 0.0f)) most = INFINITY;
     reduce_row<LPR>(square, most, shared);
     const float mean = fmaf(square, p.inv_width, eps);
-    const float inv = mean == 0.0f ? 0.0f : 1.0f / sqrtf(mean);  // (a row of zeros without an eps is zeros)
+    const float inv = TINY && mean == 0.0f ? 0.0f : 1.0f / sqrtf(mean);  // (a row of zeros without an eps is zeros)
     if (p.out) {
       float y[8 * NV];
 #pragma unroll
