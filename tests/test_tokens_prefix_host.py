@@ -2,7 +2,6 @@
 import os
 import re
 
-import paper_2604_12841_amd as pdx
 from conftest import ROOT
 from paper_2604_12841_amd import tokens
 
@@ -20,4 +19,3 @@ def test_no_prefix():
         assert workspace(prefix=bad) == 0  # refused
     text = open(os.path.join(ROOT, "include", "predecoder_ops.h")).read()
     assert re.search(r"#define PD_PREFIX_NONE INT32_MIN\b", text) and tokens.PREFIX_NONE == -(1 << 31)
-    assert pdx.PD_ERR_INVALID_ARG
