@@ -15,6 +15,16 @@
  *   predecoder_attention   grouped-head attention with capped scores, a distance
  *                          bias and masks by volume, round and prefix
  *
+ * and what a stream of rounds keeps of its past, with what reads it:
+ *
+ *   predecoder_cache_write, predecoder_cache_read
+ *                          keys and values in a ring of places, in 8 bits with a
+ *                          scale a row: quantised as they come, and read back
+ *   predecoder_attention8  predecoder_attention of new tokens over such a cache
+ *   predecoder_linear_attention
+ *                          linear attention with a decay for each head: a state of
+ *                          fixed size instead of a cache, whole rounds at a time
+ *
  * Types.  bf16 (PD_DTYPE_BF16) and fp32 (PD_DTYPE_FP32) values; 8-bit codes are
  * OCP E4M3 (the library's 8-bit format) or signed integers.  Sums, norms and
  * softmax statistics are fp32 (sums of int8 products: exact int32; of E4M3
@@ -202,6 +212,136 @@ typedef struct pd_attention_args {
 size_t predecoder_attention_workspace(const pd_attention_args* args);
 
 pd_status predecoder_attention(void* hip_stream, const pd_attention_args* args);
+
+/* ---- Cache of keys and values in 8 bits ----
+ *
+ * For each batch entry (a stream) a ring of `capacity` places; a place holds the
+ * keys and values of one token, and its site.  All three arrays are whole:
+ *   codes   [batch][2][kv_heads][capacity][head_dim], one byte each (0: keys, 1: values)
+ *   scales  [batch][2][kv_heads][capacity], fp32
+ *   sites   [batch][capacity]
+ * A row (the keys or values of one token and head) stands for code scale.  A place
+ * whose site has volume < 0 holds no token, and its codes and scales may be
+ * anything: a new cache needs its sites set so, and no more.
+ * head_dim: a multiple of 16, at most 128; codes and sites 16-byte aligned;
+ * batch, kv_heads <= 65535. */
+typedef struct pd_cache {
+  int32_t batch, kv_heads, head_dim, capacity;
+  int32_t codes_type; /* PD_CODES_E4M3 or PD_CODES_INT8 */
+  void* codes;
+  float* scales;
+  pd_site* sites;
+} pd_cache;
+
+/* Token m of entry b is at place (at[b] + m) mod capacity (at may be any number,
+ * negative ones too); tokens <= capacity, so that no place comes twice.
+ *
+ * Write: k and v [batch][tokens][kv_heads][head_dim] into the cache, with their
+ * sites.  scale = max |x| / 448 (E4M3) or / 127 (int8) in fp32, codes x / scale
+ * rounded once.  A row of zeros, or of values so small that its scale is 0, has
+ * scale 0 and codes 0; one with a value that is not finite has scale NaN and codes 0.
+ * Tokens of volume < 0 are left out: their places stay as they are.
+ * k, v and sites do not overlap the cache.
+ *
+ * Read: code scale, rounded to dtype, of those places into k and v; zeros where
+ * a place holds no token.  sites (may be NULL) gets the places' sites.  Rows of k and
+ * v do not overlap each other, nor the cache. */
+typedef struct pd_cache_args {
+  pd_cache cache;
+  int32_t tokens;
+  int32_t dtype;     /* of k and v: PD_DTYPE_BF16 or PD_DTYPE_FP32 */
+  const int64_t* at; /* [batch] */
+  void* k;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  void* v;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+  pd_site* sites; /* [batch][tokens], 16-byte aligned */
+  int64_t sites_batch_stride; /* in sites; write: 0: one list for all */
+} pd_cache_args;
+
+pd_status predecoder_cache_write(void* hip_stream, const pd_cache_args* args);
+pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args);
+
+/* ---- Attention over a cache in 8 bits ----
+ *
+ * What predecoder_attention computes (there: scores, cap, slopes, masks, prefix,
+ * queries that see nothing), of q over the tokens of a cache: keys and values are
+ * code scale, not rounded in between.  Scores, maximum and sum are fp32; a
+ * probability times a value's scale is rounded to bf16 (2^-8) for the product with the
+ * values' codes.  A visible row with scale NaN makes the result NaN; what invisible places
+ * hold does not reach it (but E4M3's NaN codes, which predecoder_cache_write never
+ * writes, may stand only where there is no token).
+ * q and out as there: bf16, all rows 16-byte aligned; heads a multiple of
+ * cache.kv_heads, heads / kv_heads <= 64; |coordinate| < 2^29.  q_sites is needed unless n_q
+ * is 0.  workspace as there.  A cap is met within 2^-20 of the score or of the cap. */
+typedef struct pd_attention8_args {
+  pd_cache cache;
+  int32_t heads, n_q;
+  float scale, cap;
+  int32_t causal, prefix; /* causal 0 or 1; prefix >= 0, or PD_PREFIX_NONE */
+  const void* q;
+  int64_t q_batch_stride, q_token_stride, q_head_stride;
+  void* out;
+  int64_t out_batch_stride, out_token_stride, out_head_stride;
+  const pd_site* q_sites; /* [batch][n_q], 16-byte aligned */
+  int64_t q_sites_batch_stride; /* in sites; 0: one list for all */
+  const float* slopes; /* [heads] or NULL */
+  void* workspace;
+  size_t workspace_bytes;
+} pd_attention8_args;
+
+/* Bytes of workspace that a call with these arguments uses; 0 for invalid ones.
+ * It goes by the sizes alone. */
+size_t predecoder_attention8_workspace(const pd_attention8_args* args);
+
+pd_status predecoder_attention8(void* hip_stream, const pd_attention8_args* args);
+
+/* ---- Linear attention with a decay ----
+ *
+ * The tokens of an entry come in rounds of per_round, token n in round
+ * t(n) = floor(n / per_round).  For each key head, with S_(-1) = state (NULL: zeros):
+ *   S_t = exp(-slope) S_(t-1) + sum over the tokens m of round t of k_m v_m^T
+ *   out_n = scale q_n S_t(n)       for every query head of the key head's group
+ * that is  scale sum over t(m) <= t(n) of exp(-slope (t(n) - t(m))) (q_n.k_m) v_m
+ * plus what the state brings: a token sees its whole round, as in causal attention.
+ * state_out (NULL: not asked for) gets S of the entry's last round; it may be
+ * state itself, or does not overlap it.  [batch][kv_heads][head_dim][head_dim]
+ * fp32, the key's channel first, whole.
+ * lengths [batch] (NULL: n for all): tokens of each entry, taken within 0 and n.  Rows of
+ * out behind them stay as they are, and what q, k and v hold there is not read; an
+ * entry of length 0 passes its state on.  A last round that is not whole counts
+ * as a round.
+ * slopes [kv_heads] (NULL: 0): the decay of a round; infinite: only its own round.
+ * bf16 q, k, v and out; sums and states fp32 (products of bf16 parts that hold 24
+ * bits of what is decayed), the weights of pairs inside a chunk and the state's part
+ * of a result taken to 16 bits or more, out rounded once.
+ * head_dim: a multiple of 8, at most 128; all rows 16-byte aligned; heads a multiple of
+ * kv_heads, heads / kv_heads <= 64.  out overlaps no input, its rows not each other.
+ * workspace as for attention. */
+typedef struct pd_linear_attention_args {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t n, per_round; /* per_round >= 1 */
+  float scale;
+  const void* q;
+  int64_t q_batch_stride, q_token_stride, q_head_stride;
+  const void* k;
+  int64_t k_batch_stride, k_token_stride, k_head_stride;
+  const void* v;
+  int64_t v_batch_stride, v_token_stride, v_head_stride;
+  void* out;
+  int64_t out_batch_stride, out_token_stride, out_head_stride;
+  const float* slopes;
+  const int32_t* lengths;
+  const float* state;
+  float* state_out;
+  void* workspace;
+  size_t workspace_bytes;
+} pd_linear_attention_args;
+
+/* Bytes of workspace, by the sizes alone; 0 for invalid arguments. */
+size_t predecoder_linear_attention_workspace(const pd_linear_attention_args* args);
+
+pd_status predecoder_linear_attention(void* hip_stream, const pd_linear_attention_args* args);
 
 #ifdef __cplusplus
 }

@@ -43,7 +43,8 @@ EXPORTS = ("predecoder_create", "predecoder_create_ex", "predecoder_run", "prede
            "predecoder_graph_destroy", "predecoder_run_static", "predecoder_peak_mfma", "predecoder_peak_copy")
 
 # The token operators (tokens.py): they work on torch tensors, so their module is loaded when one is first used.
-_TOKEN_OPS = ("rms_norm", "matmul8", "rope", "attention", "attention_workspace", "volume_sites")
+_TOKEN_OPS = ("rms_norm", "matmul8", "rope", "attention", "attention_workspace", "volume_sites", "new_cache", "cache_write",
+              "cache_read", "attention8", "attention8_workspace", "linear_attention", "linear_attention_workspace")
 __all__ += list(_TOKEN_OPS)
 
 

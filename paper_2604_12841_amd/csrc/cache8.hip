@@ -1,0 +1,228 @@
+// cache8.hip -- keys and values of tokens into a ring of places in 8 bits, and
+// back.
+//
+// A row is the keys or the values of one token and head: its scale is
+// max |x| / Q, its codes x / scale rounded to the format (Q its largest value).
+// Eight values a lane; as many lanes as hold a row (a power of two) find its
+// largest value among themselves.  A wave takes neighbouring tokens of one head,
+// whose rows lie one behind the other in the cache, so it writes whole lines.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "../../include/predecoder_ops.h"
+#include "cache8.h"
+
+namespace {
+
+using namespace pd;
+
+struct Cache8 {
+  int batch, kv_heads, head_dim, capacity, tokens;
+  unsigned token_blocks;
+  uint8_t* codes;
+  float* scales;
+  int4* sites;
+  const long long* at;
+  const void* x[2];  // k, v
+  void* y[2];
+  long long b_stride[2], t_stride[2], h_stride[2];
+  const int4* in_sites;
+  int4* out_sites;
+  long long sites_b;
+};
+
+// The place of token m: (at + m) mod capacity, m <= capacity.
+__device__ __forceinline__ int place_of(long long at, int m, int capacity) {
+  long long p = at % capacity;
+  if (p < 0) p += capacity;
+  p += m;
+  return (int)(p < capacity ? p : p - capacity);
+}
+
+// x / s to 23 bits, the last of which is set where more follow: another rounding, to fewer bits, is the only one.
+// r = 1 / s rounded.
+__device__ __forceinline__ float quotient_odd(float x, float s, float r) {
+  float t = x * r;
+  t = fmaf(fmaf(-t, s, x), r, t);  // rounded to nearest
+  const float rest = fmaf(-t, s, x);
+  const uint32_t u = __float_as_uint(t);
+  // an even t that the quotient is not: the neighbour on the quotient's side
+  const uint32_t side = (__float_as_uint(rest) ^ u) >> 31 ? u - 1 : u + 1;
+  return rest != 0.0f && !(u & 1) ? __uint_as_float(side) : t;
+}
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load_row8(const T* p, float* v) {
+  if constexpr (WIDE) {
+    load8(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = load1(p + e);
+  }
+}
+
+template <typename T, int LPR, bool INT8, bool WIDE>
+__global__ void __launch_bounds__(256) cache_write_kernel(const Cache8 p) {
+  constexpr int ROWS = 256 / LPR;
+  const unsigned group = blockIdx.x / p.token_blocks;
+  const int m = (int)(blockIdx.x % p.token_blocks) * ROWS + threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const int h = group % p.kv_heads, which = group / p.kv_heads % 2, b = group / p.kv_heads / 2;
+  const bool inside = m < p.tokens;
+  const int4 site = inside ? p.in_sites[b * p.sites_b + m] : make_int4(0, 0, 0, -1);
+  const bool there = site.w >= 0;
+  const bool mine = there && 8 * lane < p.head_dim;
+  float v[8] = {};
+  if (mine) load_row8<T, WIDE>((const T*)p.x[which] + b * p.b_stride[which] + m * p.t_stride[which] + h * p.h_stride[which] + 8 * lane, v);
+  float most = 0.0f;
+  bool finite = true;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    most = fmaxf(most, fabsf(v[e]));
+    finite = finite && fabsf(v[e]) < INFINITY;
+  }
+  if (!finite) most = INFINITY;
+#pragma unroll
+  for (int n = 1; n < LPR; n <<= 1) most = fmaxf(most, __shfl_xor(most, n));
+  if (!there) return;
+  const float scale = most < INFINITY ? most / (INT8 ? 127.0f : 448.0f) : NAN;
+  const int place = place_of(p.at[b], m, p.capacity);
+  const long long row = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity + place;
+  if (lane == 0) p.scales[row] = scale;
+  if (lane == 0 && which == 0 && h == 0) p.sites[(long long)b * p.capacity + place] = site;
+  if (!mine) return;
+  uint2 w = make_uint2(0, 0);
+  if (scale > 0.0f) {
+    // (rows of tiny values are lifted, so that the rest of a division is a number of the range)
+    const float lift = scale < 0x1p-60f ? 0x1p64f : 1.0f, s = scale * lift, r = 1.0f / s;
+    float c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = quotient_odd(v[e] * lift, s, r);
+    // (a scale of few bits, below the normal range, may be too small for its row)
+    const float q = INT8 ? 127.0f : 448.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = fminf(fmaxf(c[e], -q), q);
+    if constexpr (INT8)
+      w = make_uint2(int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7]));
+    else
+      w = make_uint2(e4m3_pack4_within(c[0], c[1], c[2], c[3]), e4m3_pack4_within(c[4], c[5], c[6], c[7]));
+  }
+  *(uint2*)(p.codes + row * p.head_dim + 8 * lane) = w;
+}
+
+// The values of eight codes.
+template <bool INT8>
+__device__ __forceinline__ void decode8(const uint2 w, float* v) {
+  const uint32_t u[2] = {w.x, w.y};
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    if constexpr (INT8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * n + e] = (float)(int8_t)(u[n] >> 8 * e);
+    } else {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(u[n], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u[n], true);
+      v[4 * n] = lo[0], v[4 * n + 1] = lo[1], v[4 * n + 2] = hi[0], v[4 * n + 3] = hi[1];
+    }
+  }
+}
+
+template <typename T, int LPR, bool INT8, bool WIDE>
+__global__ void __launch_bounds__(256) cache_read_kernel(const Cache8 p) {
+  constexpr int ROWS = 256 / LPR;
+  const unsigned group = blockIdx.x / p.token_blocks;
+  const int m = (int)(blockIdx.x % p.token_blocks) * ROWS + threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const int h = group % p.kv_heads, which = group / p.kv_heads % 2, b = group / p.kv_heads / 2;
+  if (m >= p.tokens) return;
+  const int place = place_of(p.at[b], m, p.capacity);
+  const int4 site = p.sites[(long long)b * p.capacity + place];
+  if (lane == 0 && which == 0 && h == 0 && p.out_sites) p.out_sites[b * p.sites_b + m] = site;
+  if (8 * lane >= p.head_dim) return;
+  float v[8] = {};
+  if (site.w >= 0) {
+    const long long row = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity + place;
+    const float scale = p.scales[row];
+    decode8<INT8>(*(const uint2*)(p.codes + row * p.head_dim + 8 * lane), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= scale;
+  }
+  T* y = (T*)p.y[which] + b * p.b_stride[which] + m * p.t_stride[which] + h * p.h_stride[which] + 8 * lane;
+  if constexpr (WIDE) {
+    store8(y, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) store1(y + e, v[e]);
+  }
+}
+
+template <typename T, bool INT8, bool WIDE>
+void launch(const Cache8& p, bool write, long long groups, hipStream_t st) {
+  auto go = [&](auto lanes) {
+    constexpr int LPR = decltype(lanes)::value;
+    if (write)
+      hipLaunchKernelGGL((cache_write_kernel<T, LPR, INT8, WIDE>), dim3((unsigned)(groups * p.token_blocks)), dim3(256), 0, st, p);
+    else
+      hipLaunchKernelGGL((cache_read_kernel<T, LPR, INT8, WIDE>), dim3((unsigned)(groups * p.token_blocks)), dim3(256), 0, st, p);
+  };
+  if (p.head_dim <= 32)
+    go(std::integral_constant<int, 4>());
+  else if (p.head_dim <= 64)
+    go(std::integral_constant<int, 8>());
+  else
+    go(std::integral_constant<int, 16>());
+}
+
+pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
+  if (!a) return PD_ERR_INVALID_ARG;
+  const pd_status ok = check_cache(a->cache, false);
+  if (ok != PD_OK) return ok;
+  const pd_cache& c = a->cache;
+  if (a->tokens < 0 || a->tokens > c.capacity) return PD_ERR_INVALID_ARG;
+  if (a->dtype != PD_DTYPE_BF16 && a->dtype != PD_DTYPE_FP32) return PD_ERR_INVALID_ARG;
+  if (!c.batch || !c.kv_heads || !a->tokens) return PD_OK;
+  const int lanes = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : 16, rows = 256 / lanes;
+  const long long groups = 2ll * c.batch * c.kv_heads, blocks = (a->tokens + rows - 1) / rows;
+  if (groups * blocks >= 1ll << 24) return PD_ERR_UNSUPPORTED;  // threads below 2^32
+  if (check_cache(c, true) != PD_OK || !a->at || (uintptr_t)a->at % 8 || !a->k || !a->v || (write && !a->sites)) return PD_ERR_INVALID_ARG;
+  const int elem = a->dtype == PD_DTYPE_BF16 ? 2 : 4;
+  if ((uintptr_t)a->k % elem || (uintptr_t)a->v % elem || (uintptr_t)a->sites % 16) return PD_ERR_INVALID_ARG;
+  if (!write) {
+    if (!rows_apart(c.head_dim, {{c.batch, a->k_batch_stride}, {a->tokens, a->k_token_stride}, {c.kv_heads, a->k_head_stride}}) ||
+        !rows_apart(c.head_dim, {{c.batch, a->v_batch_stride}, {a->tokens, a->v_token_stride}, {c.kv_heads, a->v_head_stride}}) || a->k == a->v)
+      return PD_ERR_INVALID_ARG;
+    if (a->sites && !rows_apart(a->tokens, {{c.batch, a->sites_batch_stride}})) return PD_ERR_INVALID_ARG;
+  }
+  Cache8 p;
+  p.batch = c.batch, p.kv_heads = c.kv_heads, p.head_dim = c.head_dim, p.capacity = c.capacity, p.tokens = a->tokens;
+  p.token_blocks = (unsigned)blocks;
+  p.codes = (uint8_t*)c.codes, p.scales = c.scales, p.sites = (int4*)c.sites, p.at = (const long long*)a->at;
+  p.x[0] = p.y[0] = a->k, p.x[1] = p.y[1] = a->v;
+  p.b_stride[0] = a->k_batch_stride, p.t_stride[0] = a->k_token_stride, p.h_stride[0] = a->k_head_stride;
+  p.b_stride[1] = a->v_batch_stride, p.t_stride[1] = a->v_token_stride, p.h_stride[1] = a->v_head_stride;
+  p.in_sites = (const int4*)a->sites, p.out_sites = (int4*)a->sites, p.sites_b = a->sites_batch_stride;
+  bool wide = true;
+  for (int n = 0; n < 2; ++n)
+    wide = wide && (uintptr_t)p.x[n] % 16 == 0 && p.b_stride[n] * elem % 16 == 0 && p.t_stride[n] * elem % 16 == 0 && p.h_stride[n] * elem % 16 == 0;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  auto go = [&](auto type, auto int8) {
+    using T = decltype(type);
+    if (wide)
+      launch<T, decltype(int8)::value, true>(p, write, groups, st);
+    else
+      launch<T, decltype(int8)::value, false>(p, write, groups, st);
+  };
+  const bool int8 = c.codes_type == PD_CODES_INT8, bf16 = a->dtype == PD_DTYPE_BF16;
+  if (bf16 && int8)
+    go(uint16_t(), std::true_type());
+  else if (bf16)
+    go(uint16_t(), std::false_type());
+  else if (int8)
+    go(float(), std::true_type());
+  else
+    go(float(), std::false_type());
+  return hipGetLastError() == hipSuccess ? PD_OK : PD_ERR_DEVICE;
+}
+
+}  // namespace
+
+extern "C" pd_status predecoder_cache_write(void* hip_stream, const pd_cache_args* args) { return run(hip_stream, args, true); }
+
+extern "C" pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args) { return run(hip_stream, args, false); }

@@ -16,7 +16,8 @@ import torch
 
 from . import (ACT_GELU_TANH, ACT_NONE, ACT_RELU, DTYPE_BF16, DTYPE_FP32, PD_OK, PredecoderError, lib)
 
-__all__ = ["rms_norm", "matmul8", "rope", "attention", "attention_workspace", "volume_sites", "CODES_NONE",
+__all__ = ["rms_norm", "matmul8", "rope", "attention", "attention_workspace", "volume_sites", "new_cache", "cache_write",
+           "cache_read", "attention8", "attention8_workspace", "linear_attention", "linear_attention_workspace", "CODES_NONE",
            "CODES_E4M3", "CODES_INT8", "OPS_EXPORTS"]
 
 CODES_NONE, CODES_E4M3, CODES_INT8 = 0, 1, 2
@@ -27,7 +28,8 @@ _CODES = {torch.float8_e4m3fn: CODES_E4M3, torch.int8: CODES_INT8}
 
 # Every symbol declared in include/predecoder_ops.h.
 OPS_EXPORTS = ("predecoder_rms_norm", "predecoder_matmul8", "predecoder_rope", "predecoder_attention_workspace",
-               "predecoder_attention")
+               "predecoder_attention", "predecoder_cache_write", "predecoder_cache_read", "predecoder_attention8_workspace",
+               "predecoder_attention8", "predecoder_linear_attention_workspace", "predecoder_linear_attention")
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -62,6 +64,35 @@ class AttentionArgs(ctypes.Structure):
                 ("slopes", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+# pd_cache, as the first member of the structures that hold one
+_CACHE = [("batch", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("capacity", _i32), ("codes_type", _i32), ("codes", _vp),
+          ("scales", _vp), ("cache_sites", _vp)]
+
+
+class CacheArgs(ctypes.Structure):
+    _fields_ = _CACHE + [("tokens", _i32), ("dtype", _i32), ("at", _vp)] + \
+               [f for n in "kv" for f in ((n, _vp), (n + "_batch_stride", _i64), (n + "_token_stride", _i64),
+                                          (n + "_head_stride", _i64))] + \
+               [("sites", _vp), ("sites_batch_stride", _i64)]
+
+
+class Attention8Args(ctypes.Structure):
+    _fields_ = _CACHE + [("heads", _i32), ("n_q", _i32), ("scale", _f32), ("cap", _f32), ("causal", _i32), ("prefix", _i32)] + \
+               [f for n in ("q", "out") for f in ((n, _vp), (n + "_batch_stride", _i64), (n + "_token_stride", _i64),
+                                                  (n + "_head_stride", _i64))] + \
+               [("q_sites", _vp), ("q_sites_batch_stride", _i64), ("slopes", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class LinearAttentionArgs(ctypes.Structure):
+    _fields_ = [("batch", _i32), ("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("n", _i32), ("per_round", _i32),
+                ("scale", _f32)] + \
+               [f for n in ("q", "k", "v", "out") for f in ((n, _vp), (n + "_batch_stride", _i64), (n + "_token_stride", _i64),
+                                                            (n + "_head_stride", _i64))] + \
+               [("slopes", _vp), ("lengths", _vp), ("state", _vp), ("state_out", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _fn = None
 
 
@@ -71,11 +102,14 @@ def _functions():
     if _fn is None:
         L = lib()
         for name, args in (("predecoder_rms_norm", NormArgs), ("predecoder_matmul8", Matmul8Args),
-                           ("predecoder_rope", RopeArgs), ("predecoder_attention", AttentionArgs)):
+                           ("predecoder_rope", RopeArgs), ("predecoder_attention", AttentionArgs),
+                           ("predecoder_cache_write", CacheArgs), ("predecoder_cache_read", CacheArgs),
+                           ("predecoder_attention8", Attention8Args), ("predecoder_linear_attention", LinearAttentionArgs)):
             f = getattr(L, name)
             f.argtypes, f.restype = [_vp, ctypes.POINTER(args)], _i32
-        L.predecoder_attention_workspace.argtypes = [ctypes.POINTER(AttentionArgs)]
-        L.predecoder_attention_workspace.restype = ctypes.c_size_t
+            if name + "_workspace" in OPS_EXPORTS:
+                f = getattr(L, name + "_workspace")
+                f.argtypes, f.restype = [ctypes.POINTER(args)], ctypes.c_size_t
         _fn = L
     return _fn
 
@@ -93,6 +127,7 @@ def _packer(args):
 
 _pack_norm, _pack_matmul8 = _packer(NormArgs), _packer(Matmul8Args)
 _pack_rope, _pack_attention = _packer(RopeArgs), _packer(AttentionArgs)
+_pack_cache, _pack_attention8, _pack_linear = _packer(CacheArgs), _packer(Attention8Args), _packer(LinearAttentionArgs)
 _fast = {}
 
 
@@ -101,7 +136,7 @@ def _by_bytes(name):
     f = _fast.get(name)
     if f is None:
         f = lib()[name]
-        work = name == "predecoder_attention_workspace"
+        work = name.endswith("_workspace")
         f.argtypes = [ctypes.c_char_p] if work else [_vp, ctypes.c_char_p]
         f.restype = ctypes.c_size_t if work else _i32
         _fast[name] = f
@@ -260,6 +295,27 @@ def rope(x, sites, out, sections, base=10000.0, interleaved=False, inverse=False
           stream, dev)
 
 
+def _call_with_workspace(name, pack, a, q, workspace, stream):
+    """Calls `name` with the packed arguments `a`, a workspace and its size; the workspace is the caller's or allocated here."""
+    dev = q.get_device()
+    ptr = 0
+    if workspace is not None:
+        _need(workspace.get_device() == dev and workspace.is_contiguous(),
+              "workspace must be a contiguous tensor on the GPU of q")
+        ptr, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = _by_bytes(name + "_workspace")(pack(*a, 0, 0))
+        if need:
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            else:
+                _need(isinstance(stream, torch.cuda.Stream), "a raw stream handle needs a workspace from the caller")
+                with torch.cuda.stream(stream):  # its memory goes back to the stream that uses it
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            ptr = workspace.data_ptr()
+    _call(name, pack(*a, ptr, need), stream, dev)
+
+
 def _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix):
     """The arguments of predecoder_attention for these tensors, without a workspace."""
     _need(q.dim() == 4 and k.dim() == 4, "q and k must be [batch][tokens][heads][head_dim]")
@@ -305,23 +361,168 @@ def attention(q, k, v, out, q_sites=None, k_sites=None, scale=None, cap=0.0, slo
     [batch][n][4].  workspace: a device tensor of at least
     attention_workspace() bytes (needed with a raw stream handle; otherwise allocated here)."""
     a = _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix)
-    dev = q.get_device()
-    ptr = 0
-    if workspace is not None:
-        _need(workspace.get_device() == dev and workspace.is_contiguous(),
-              "workspace must be a contiguous tensor on the GPU of q")
-        ptr, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    else:
-        need = _by_bytes("predecoder_attention_workspace")(_pack_attention(*a, 0, 0))
-        if need:
-            if stream is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            else:
-                _need(isinstance(stream, torch.cuda.Stream), "a raw stream handle needs a workspace from the caller")
-                with torch.cuda.stream(stream):  # its memory goes back to the stream that uses it
-                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            ptr = workspace.data_ptr()
-    _call("predecoder_attention", _pack_attention(*a, ptr, need), stream, dev)
+    _call_with_workspace("predecoder_attention", _pack_attention, a, q, workspace, stream)
+
+
+def new_cache(batch, capacity, kv_heads, head_dim, codes="e4m3", device="cuda"):
+    """An empty cache (codes, scales, sites) for `batch` streams of `capacity` tokens, in 8 bits ("e4m3" or "int8")."""
+    _need(codes in ("e4m3", "int8"), "codes must be e4m3 or int8")
+    sites = torch.zeros(batch, capacity, 4, dtype=torch.int32, device=device)
+    sites[..., 3] = -1
+    dtype = torch.int8 if codes == "int8" else torch.float8_e4m3fn
+    return (torch.zeros(batch, 2, kv_heads, capacity, head_dim, dtype=torch.int8, device=device).view(dtype),
+            torch.zeros(batch, 2, kv_heads, capacity, device=device), sites)
+
+
+def _cache_args(cache, index):
+    """The members of pd_cache for (codes, scales, sites)."""
+    codes, scales, sites = cache
+    shape, dt = codes.shape, codes.dtype
+    if len(shape) != 5 or shape[1] != 2 or dt not in _CODES:
+        raise ValueError("the cache's codes must be float8_e4m3fn or int8 [batch][2][kv_heads][capacity][head_dim]")
+    B, _, Hk, cap, D = shape
+    if scales.shape != (B, 2, Hk, cap) or scales.dtype != torch.float32 or sites.shape != (B, cap, 4) or sites.dtype != torch.int32:
+        raise ValueError("the cache's scales must be float32 %s and its sites int32 %s" % ((B, 2, Hk, cap), (B, cap, 4)))
+    if codes.get_device() != index or scales.get_device() != index or sites.get_device() != index:
+        raise ValueError("the cache must be on GPU %d" % index)
+    if not (codes.is_contiguous() and scales.is_contiguous() and sites.is_contiguous()):
+        raise ValueError("the cache's tensors must be contiguous")
+    if scales.requires_grad:
+        _lost_gradient("the cache's scales")
+    return B, Hk, D, cap, _CODES[dt], codes.data_ptr(), scales.data_ptr(), sites.data_ptr()
+
+
+def _cache_call(name, cache, at, k, v, sites, stream):
+    _need(k.dim() == 4, "k and v must be [batch][tokens][kv_heads][head_dim]")
+    shape, dt, dev = k.shape, k.dtype, _index(k, "k")
+    _need(dt in _VALUES, "k and v must be bfloat16 or float32")
+    c = _cache_args(cache, dev)
+    B, n, Hk, D = shape
+    if (B, Hk, D) != c[:3]:
+        raise ValueError("k has shape %s, and the cache %s" % (tuple(shape), tuple(cache[0].shape)))
+    if at.get_device() != dev or at.dtype != torch.int64 or at.shape != (B,) or not at.is_contiguous():
+        raise ValueError("at must be a contiguous vector of %d int64 values on GPU %d" % (B, dev))
+    fields = []
+    for t, what in ((k, "k"), (v, "v")):
+        if t.get_device() != dev or t.dtype != dt or t.shape != shape:
+            raise ValueError("%s must be a %s tensor %s on GPU %d" % (what, dt, tuple(shape), dev))
+        if t.requires_grad:
+            _lost_gradient(what)
+        sb, st, sh, one = t.stride()
+        if one != 1 and D > 1:
+            raise ValueError("the rows of a head must be contiguous in %s" % what)
+        fields += (t.data_ptr(), sb, st, sh)
+    ps = bs = 0
+    if sites is not None:
+        ps, bs = _sites(sites, "sites", n, dev, B)
+        if name == "predecoder_cache_read":
+            _need(sites.shape == (B, n, 4), "sites must be [batch][tokens][4]")
+    _call(name, _pack_cache(*c, n, _VALUES[dt], at.data_ptr(), *fields, ps, bs), stream, dev)
+
+
+def cache_write(cache, at, k, v, sites, stream=None):
+    """Keys and values of new tokens, k and v [batch][tokens][kv_heads][head_dim] (bf16 or float32), into a cache in 8 bits.
+
+    cache: (codes [batch][2][kv_heads][capacity][head_dim] float8_e4m3fn or int8, scales [batch][2][kv_heads][capacity],
+    sites [batch][capacity][4]), as new_cache() makes it.  Token m of entry b goes to place (at[b] + m) mod capacity (at: int64 on
+    the GPU), with its site ([tokens][4] for all entries or [batch][tokens][4]); a token of volume < 0 leaves its place as it is."""
+    _need(sites is not None, "sites must be given")
+    _cache_call("predecoder_cache_write", cache, at, k, v, sites, stream)
+
+
+def cache_read(cache, at, k, v, sites=None, stream=None):
+    """Keys and values of the places from at[b] on, code scale rounded, into k and v [batch][tokens][kv_heads][head_dim] (bf16
+    or float32), and their sites into `sites` [batch][tokens][4] if given.  Places that hold no token give zeros."""
+    _cache_call("predecoder_cache_read", cache, at, k, v, sites, stream)
+
+
+def _attention8_args(q, cache, out, q_sites, scale, cap, slopes, causal, prefix):
+    _need(q.dim() == 4, "q must be [batch][tokens][heads][head_dim]")
+    shape, dev = q.shape, _index(q, "q")
+    B, nq, H, D = shape
+    c = _cache_args(cache, dev)
+    if B != c[0] or D != c[2]:
+        raise ValueError("q has shape %s, and the cache %s" % (tuple(shape), tuple(cache[0].shape)))
+    fields = []
+    for t, what in ((q, "q"), (out, "out")):
+        if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != shape:
+            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(shape)))
+        if t.requires_grad:
+            _lost_gradient(what)
+        sb, st, sh, one = t.stride()
+        if one != 1 and D > 1:
+            raise ValueError("the rows of a head must be contiguous in %s" % what)
+        fields += (t.data_ptr(), sb, st, sh)
+    pq, bq = _sites(q_sites, "q_sites", nq, dev, B)
+    return (*c, H, nq, D ** -0.5 if scale is None else scale, cap, bool(causal), PREFIX_NONE if prefix is None else int(prefix), *fields, pq, bq,
+            _vector(slopes, "slopes", H, dev))
+
+
+def attention8_workspace(q, cache, out, q_sites, scale=None, cap=0.0, slopes=None, causal=False, prefix=None):
+    """Bytes of workspace of attention8() with these arguments."""
+    a = _attention8_args(q, cache, out, q_sites, scale, cap, slopes, causal, prefix)
+    return _by_bytes("predecoder_attention8_workspace")(_pack_attention8(*a, 0, 0))
+
+
+def attention8(q, cache, out, q_sites, scale=None, cap=0.0, slopes=None, causal=False, prefix=None, workspace=None, stream=None):
+    """attention() of q [batch][n_q][heads][head_dim] over the tokens of a cache in 8 bits (see cache_write()) into out (bf16).
+
+    A query of volume a sees the cache's places of volume a, with causal those of its own and earlier rounds or, unless prefix is
+    None, of all rounds below prefix.  The other arguments are attention()'s; workspace: attention8_workspace() bytes."""
+    a = _attention8_args(q, cache, out, q_sites, scale, cap, slopes, causal, prefix)
+    _call_with_workspace("predecoder_attention8", _pack_attention8, a, q, workspace, stream)
+
+
+def _linear_args(q, k, v, out, slopes, per_round, lengths, state, state_out, scale):
+    _need(q.dim() == 4 and k.dim() == 4, "q and k must be [batch][tokens][heads][head_dim]")
+    shape, dev = q.shape, _index(q, "q")
+    B, n, H, D = shape
+    Hk = k.shape[2]
+    fields = []
+    for t, what, want in ((q, "q", shape), (k, "k", (B, n, Hk, D)), (v, "v", (B, n, Hk, D)), (out, "out", shape)):
+        if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != want:
+            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(want)))
+        if t.requires_grad:
+            _lost_gradient(what)
+        sb, st, sh, one = t.stride()
+        if one != 1 and D > 1:
+            raise ValueError("the rows of a head must be contiguous in %s" % what)
+        fields += (t.data_ptr(), sb, st, sh)
+    pl = 0
+    if lengths is not None:
+        if lengths.get_device() != dev or lengths.dtype != torch.int32 or lengths.shape != (B,) or not lengths.is_contiguous():
+            raise ValueError("lengths must be a contiguous vector of %d int32 values on GPU %d" % (B, dev))
+        pl = lengths.data_ptr()
+    states = []
+    for t, what in ((state, "state"), (state_out, "state_out")):
+        if t is None:
+            states.append(0)
+            continue
+        if t.get_device() != dev or t.dtype != torch.float32 or t.shape != (B, Hk, D, D) or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous float32 tensor %s on GPU %d" % (what, (B, Hk, D, D), dev))
+        if t.requires_grad:
+            _lost_gradient(what)
+        states.append(t.data_ptr())
+    return (B, H, Hk, D, n, per_round, D ** -0.5 if scale is None else scale, *fields, _vector(slopes, "slopes", Hk, dev), pl, *states)
+
+
+def linear_attention_workspace(q, k, v, out, slopes=None, per_round=1, lengths=None, state=None, state_out=None, scale=None):
+    """Bytes of workspace of linear_attention() with these arguments."""
+    a = _linear_args(q, k, v, out, slopes, per_round, lengths, state, state_out, scale)
+    return _by_bytes("predecoder_linear_attention_workspace")(_pack_linear(*a, 0, 0))
+
+
+def linear_attention(q, k, v, out, slopes=None, per_round=1, lengths=None, state=None, state_out=None, scale=None, workspace=None,
+                     stream=None):
+    """Linear attention with a decay, over rounds of per_round tokens: out_n = scale q_n S_t(n) with
+    S_t = exp(-slope) S_(t-1) + the sum of k_m v_m^T over the tokens of round t.
+
+    q, out [batch][n][heads][head_dim], k, v [batch][n][kv_heads][head_dim] (bf16); slopes [kv_heads] (None: no decay); scale None:
+    head_dim^-1/2.  state (None: zeros) is S before the first round, state_out gets S after the last
+    ([batch][kv_heads][head_dim][head_dim] float32, may be state).  lengths [batch] (int32 on the GPU): tokens of each entry; rows
+    of out behind them stay as they are.  workspace: linear_attention_workspace() bytes."""
+    a = _linear_args(q, k, v, out, slopes, per_round, lengths, state, state_out, scale)
+    _call_with_workspace("predecoder_linear_attention", _pack_linear, a, q, workspace, stream)
 
 
 def volume_sites(d, T, volume=0, first_round=0, layout="plaquette", device="cuda"):

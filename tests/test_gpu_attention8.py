@@ -1,0 +1,179 @@
+"""GPU: attention over a cache in 8 bits against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import memory_cases as mc
+import paper_2604_12841_amd as pdx
+import token_cases as tc
+
+pytestmark = pytest.mark.gpu
+
+
+def places_of(g, B, n, volumes, most_round, holes):
+    s = torch.randint(0, 9, (B, n, 4), generator=g, device="cuda", dtype=torch.int32)
+    s[..., 0] = torch.randint(0, most_round, (B, n), generator=g, device="cuda", dtype=torch.int32)
+    s[..., 3] = torch.randint(0, volumes, (B, n), generator=g, device="cuda", dtype=torch.int32)
+    if holes:
+        s[..., 3] = torch.where(torch.rand(B, n, generator=g, device="cuda") < holes, -1, s[..., 3])
+    return s
+
+
+def check(q, cache, q_sites, **kw):
+    a = dict(scale=q.shape[-1] ** -0.5, cap=0.0, slopes=None, causal=False, prefix=None) | kw
+    B, n, H, D = q.shape
+    whole = torch.full((B, n, H, D + 8), 7.0, device="cuda", dtype=torch.bfloat16)
+    out = whole[..., :D]
+    pdx.attention8(q, cache, out, q_sites, **a)
+    torch.cuda.synchronize()
+    a["prefix"] = -(1 << 31) if a["prefix"] is None else a["prefix"]
+    want, bound = mc.attention8_reference(q, cache, q_sites, **a)
+    assert torch.all(whole[..., D:] == 7.0)
+    assert torch.equal(out.isnan(), want.isnan())
+    off = (out.double() - want).abs()
+    assert torch.all((off <= bound) | want.isnan()), float((off / bound).nan_to_num(0).amax())
+    return out
+
+
+CASES = [  # B, n_q, capacity, heads, kv_heads, D
+    (1, 1, 1, 1, 1, 16), (1, 1, 63, 4, 4, 32), (2, 1, 300, 8, 2, 64), (1, 36, 720, 4, 4, 32), (2, 7, 129, 6, 3, 48), (1, 33, 64, 2, 1, 128),
+    (3, 1, 5000, 8, 2, 64), (1, 130, 1027, 4, 1, 96), (2, 5, 2049, 2, 2, 128), (1, 65, 65, 8, 8, 80), (1, 1, 20000, 16, 1, 128), (2, 196, 590, 8, 2, 64)]
+
+
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("B,n,capacity,H,Hk,D", CASES)
+def test_over_a_cache(codes, B, n, capacity, H, Hk, D):
+    g = tc.gen(n * 1000 + capacity)
+    k_sites = places_of(g, B, capacity, 2, 12, 0.1)
+    cache = mc.filled_cache(g, B, capacity, Hk, D, codes, k_sites)
+    q = (1.5 * tc.normal(g, B, n, H, D)).to(torch.bfloat16)
+    q_sites = places_of(g, B, n, 2, 12, 0.1)
+    slopes = torch.exp2(-8.0 * (torch.arange(H, device="cuda") + 1.0) / H)
+    check(q, cache, q_sites)
+    check(q, cache, q_sites, cap=20.0, slopes=slopes, causal=True, prefix=2)
+    check(q, cache, q_sites, cap=300.0, causal=True)
+    check(q, cache, q_sites, slopes=-slopes, scale=0.05)
+
+
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,H,Hk,D", [(1, 4, 2, 64), (40, 4, 2, 64), (3, 2, 2, 128), (130, 2, 1, 32)])
+def test_volumes_apart(codes, n, H, Hk, D):
+    """Volumes in runs: whole tiles that a query does not see, empty runs, volumes that no key has."""
+    g = tc.gen(n + D)
+    B, capacity = 2, 1500
+    k_sites = places_of(g, B, capacity, 1, 40, 0)
+    at = torch.arange(capacity, device="cuda", dtype=torch.int32)
+    k_sites[..., 3] = at // 300
+    k_sites[..., 0] = at // 36
+    k_sites[:, 500:900, 3] = -1
+    cache = mc.filled_cache(g, B, capacity, Hk, D, codes, k_sites)
+    q = tc.normal(g, B, n, H, D).to(torch.bfloat16)
+    q_sites = places_of(g, B, n, 7, 45, 0)
+    check(q, cache, q_sites, causal=True, cap=30.0)
+    check(q, cache, q_sites)
+    q_sites[..., 3] = 2  # its places 600 to 899 are empty
+    q_sites[1, :, 3] = -1
+    out = check(q, cache, q_sites)
+    assert torch.all(out == 0)
+    q_sites[0, :, 3] = 4
+    q_sites[0, :, 0] = torch.arange(n, device="cuda", dtype=torch.int32) % 3 + 32  # rounds 33 on hold the volume's keys
+    check(q, cache, q_sites, causal=True)
+
+
+def test_what_is_masked_does_not_reach_the_result():
+    """NaN scales of rows that a query does not see, at tokens of other volumes and later rounds; visible ones give NaN."""
+    g = tc.gen(77)
+    k_sites = places_of(g, 1, 700, 2, 20, 0)
+    for which in (0, 1):
+        cache = mc.filled_cache(g, 1, 700, 2, 64, "e4m3", k_sites)
+        cache[1][:, which, :, :] = torch.where((k_sites[..., 3] == 1) | (k_sites[..., 0] > 10), math.nan, cache[1][:, which])
+        for n in (1, 50):
+            q = tc.normal(g, 1, n, 4, 64).to(torch.bfloat16)
+            q_sites = places_of(g, 1, n, 1, 11, 0)
+            out = check(q, cache, q_sites, causal=True)
+            assert torch.isfinite(out).all()
+            q_sites[..., 0] = 19
+            assert check(q, cache, q_sites, causal=True).isnan().all()
+
+
+def test_scores_of_any_size():
+    g = tc.gen(5)
+    k_sites = places_of(g, 1, 400, 1, 9, 0)
+    cache = mc.filled_cache(g, 1, 400, 1, 64, "int8", k_sites)
+    for n in (1, 40):
+        q = (30.0 * tc.normal(g, 1, n, 2, 64)).to(torch.bfloat16)
+        q_sites = places_of(g, 1, n, 1, 9, 0)
+        check(q, cache, q_sites)
+        check(q, cache, q_sites, cap=5.0)
+        check(q, cache, q_sites, cap=1e4)
+        check(q, cache, q_sites, scale=0.0)
+        check(q, cache, q_sites, scale=-1.0)
+        check(q, cache, q_sites, slopes=torch.tensor([1e4, 0.0], device="cuda"))
+    cache[1][:, 0] *= 2.0 ** 40  # keys, and queries to match
+    check((q * 2.0 ** -40).to(torch.bfloat16), cache, q_sites)
+
+
+def test_equal_values_come_out():
+    """Where all values are one row the result is that row, whatever the scores."""
+    g = tc.gen(6)
+    for codes in ("e4m3", "int8"):
+        cache = mc.filled_cache(g, 1, 900, 1, 64, codes, places_of(g, 1, 900, 1, 9, 0))
+        cache[0][:, 1] = cache[0][:, 1, :, :1].clone().expand(1, 1, 900, 64) if codes == "int8" else cache[0].view(torch.uint8)[:, 1, :, :1].clone().expand(
+            1, 1, 900, 64).contiguous().view(torch.float8_e4m3fn)
+        cache[1][:, 1] = 0.25
+        for n in (1, 70):
+            q = tc.normal(g, 1, n, 3, 64).to(torch.bfloat16)
+            out = check(q, cache, places_of(g, 1, n, 1, 9, 0))
+            v = mc.by_token(cache)[1][0, 0, 0]
+            assert torch.all((out.double() - v).abs() <= 2 * tc.U16 * v.abs())
+
+
+def test_many_lists_streams_and_workspaces():
+    g = tc.gen(8)
+    B, capacity = 3, 4000
+    cache = mc.filled_cache(g, B, capacity, 2, 64, "e4m3", places_of(g, B, capacity, 1, 50, 0.2))
+    q = tc.normal(g, B, 2, 8, 64).to(torch.bfloat16)
+    one = places_of(g, 1, 2, 1, 50, 0)[0]
+    a, b, c = (torch.empty_like(q) for _ in range(3))
+    pdx.attention8(q, cache, a, one, causal=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    pdx.attention8(q, cache, b, one.expand(B, 2, 4).contiguous(), causal=True, stream=s)
+    need = pdx.attention8_workspace(q, cache, c, one)
+    w = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    pdx.attention8(q, cache, c, one, causal=True, workspace=w, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_nothing_to_do():
+    cache = pdx.new_cache(1, 0, 2, 64)
+    q = torch.ones(1, 3, 4, 64, device="cuda", dtype=torch.bfloat16)
+    out = torch.full_like(q, 3.0)
+    sites = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    pdx.attention8(q, cache, out, sites)
+    torch.cuda.synchronize()
+    assert torch.all(out == 0)
+    pdx.attention8(q, pdx.new_cache(1, 500, 2, 64), out.fill_(3.0), sites)
+    torch.cuda.synchronize()
+    assert torch.all(out == 0)
+    pdx.attention8(q[:, :0], pdx.new_cache(1, 500, 2, 64), out[:, :0], sites[:0])
+
+
+def test_refusals():
+    cache = pdx.new_cache(2, 100, 2, 64)
+    q = torch.zeros(2, 3, 4, 64, device="cuda", dtype=torch.bfloat16)
+    sites = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    good = dict(q=q, cache=cache, out=torch.empty_like(q), q_sites=sites)
+    for bad in (dict(q=q.float()), dict(q=q[:1]), dict(out=q[:, :2]), dict(q_sites=sites[:2]), dict(q_sites=sites.cpu()), dict(q=q[..., :32], out=q[..., 32:]),
+                dict(slopes=torch.zeros(3, device="cuda")), dict(cache=(cache[0], cache[1], cache[2].long())), dict(out=torch.empty_like(q).requires_grad_())):
+        with pytest.raises(ValueError):
+            pdx.attention8(**(good | bad))
+    for bad in (dict(scale=math.nan), dict(cap=-1.0), dict(cap=math.inf), dict(prefix=3), dict(out=q), dict(causal=True, prefix=-2)):
+        with pytest.raises(pdx.PredecoderError) as e:
+            pdx.attention8(**(good | bad))
+        assert e.value.status == pdx.PD_ERR_INVALID_ARG
+    q = torch.zeros(2, 3, 3, 64, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(pdx.PredecoderError):
+        pdx.attention8(q, cache, torch.empty_like(q), sites)
