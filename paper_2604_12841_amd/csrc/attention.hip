@@ -30,17 +30,12 @@
 #include <math.h>
 
 #include "../../include/predecoder_ops.h"
+#include "lds_tiles.h"
 #include "token_values.h"
 
 namespace {
 
 using namespace pd;
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 64;  // keys of a noted tile
@@ -165,43 +160,6 @@ __global__ void __launch_bounds__(256) attention_notes_kernel(const int4* __rest
   if (lane == 0) notes[at] = t;
   bytes[at * TILE + lane] = site_bytes(s);
   ordered_sites[at * TILE + lane] = ordered(s);
-}
-
-// Send 16 (4) bytes a lane from memory to LDS at `to` (the same in all lanes) + 16 (4) times the lane; lanes that do
-// not take part leave their place as it is.  Complete after sent().  Written out rather than with the builtin, for
-// which the compiler waits before any later LDS read, of the other buffer too; no register is an output.  (The wait
-// states are those that the load needs after writes of m0 and, by vector instructions, of its scalar base.)
-__device__ __forceinline__ uint32_t lds_byte(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-__device__ __forceinline__ void send16(const void* from, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte(to)), "v"(from));
-}
-__device__ __forceinline__ void send16(const void* base, uint32_t at, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
-}
-__device__ __forceinline__ void send4(const void* base, uint32_t at, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
-}
-__device__ __forceinline__ void sent() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-  asm volatile("" ::: "memory");
-}
-
-// LDS byte of granule g (8 values) of a key's row.  Rows are not padded; which
-// granule lies where is turned by the key, so that the 16 lanes that are
-// served together fall on different banks: K is read 32 keys at a
-// time, one granule each, V four keys at a time, two granules each.
-template <int DP>
-__device__ __forceinline__ int k_place(int key, int g) {
-  const int turn = DP == 128 ? key & 15 : DP == 64 ? (key >> 1) & 7 : (key >> 2) & 3;
-  return key * (DP * 2) + ((g ^ turn) << 4);
-}
-template <int DP>
-__device__ __forceinline__ int v_place(int key, int g) {
-  const int turn = DP == 128 ? (key & 3) << 2 : DP == 64 ? ((key >> 1) & 1) << 2 : 0;
-  return key * (DP * 2) + ((g ^ turn) << 4);
 }
 
 template <int DP, int NW, Cap CAP, bool BIAS>

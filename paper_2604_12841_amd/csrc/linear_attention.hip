@@ -3,20 +3,45 @@
 //   S_t = exp(-slope) S_(t-1) + sum over the tokens m of round t of k_m v_m^T
 //   out_n = scale q_n S_t(n)
 //
-// The recurrent form: a workgroup holds the columns of S of one batch entry and
-// key head, a thread some rows of one column.
+// Chunked form.  S stays in registers, in blocks of 32 x 32 over the waves of a
+// workgroup; tiles of 64 tokens of K and V come through LDS, two in turn, and
+// S += K^T V with both operands read transposed.  As the right operand of
+// out^T = S^T q^T a copy of S goes to LDS, in two bf16 parts (16 bits).
+//   Wide rounds (more than 32 tokens): S takes a whole round in, then the round's
+//   queries read it: no token sees a part of a round, so there are no pairs.
+//   Narrow rounds: a tile holds as many whole rounds as fit.  Its queries read S from
+//   before the tile, decayed, and the tile's keys in pairs:
+//   out_i = w^(t_i + 1) q_i S + sum over t_j <= t_i of w^(t_i - t_j) (q_i.k_j) v_j;
+//   then S = w^R S + sum of w^(R - 1 - t_j) k_j v_j^T.  The weighted keys are split into three bf16 parts (24
+//   bits), weighted pairs into two.
+//
+// Few entries and heads against many rounds: the rounds are cut into segments.
+// A first pass leaves each segment's own S, a scan turns them into the S that
+// each segment starts from, and the last pass runs the segments side by side.
+//
+// Recurrent form (one token an entry): S is read, updated, multiplied by q and
+// written by threads that hold four columns of some rows.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
 #include "../../include/predecoder_ops.h"
+#include "lds_tiles.h"
 #include "token_values.h"
 
 namespace {
 
 using namespace pd;
 
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int TILE = 64;  // tokens
+constexpr int NARROW = 32;  // a round of up to as many tokens shares its tile with others
+
 struct Linear {
   int batch, heads, kv_heads, group, head_dim, n, per_round;
+  int tile_rounds;  // narrow rounds: of a tile
+  int tile_tokens;  // narrow rounds: tile_rounds per_round; else TILE
+  int segments;
+  int segment_rounds;  // narrow rounds: a multiple of tile_rounds
   float scale;
   const uint16_t* q;
   const uint16_t* k;
@@ -27,51 +52,490 @@ struct Linear {
   const int* lengths;
   const float* state;
   float* state_out;
+  float* starts;  // [batch][kv_heads][segments][head_dim][head_dim]
 };
 
-// A workgroup of 16 x 16 threads: thread (r, c) holds rows r + 16 n of column c of sixteen.
-__global__ void __launch_bounds__(256) linear_simple_kernel(const Linear p) {
-  __shared__ float part[16][17];
-  const int r = threadIdx.x >> 4, c = threadIdx.x & 15, D = p.head_dim;
-  const int kvh = blockIdx.y % p.kv_heads, b = blockIdx.y / p.kv_heads, col = blockIdx.x * 16 + c;
-  const int len = p.lengths ? min(max(p.lengths[b], 0), p.n) : p.n;
-  const float fade = p.slopes ? expf(-p.slopes[kvh]) : 1.0f;
-  const long long at = (long long)blockIdx.y * D * D;
-  float s[8];
+__device__ __forceinline__ int length_of(const Linear& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.n) : p.n; }
+
+// exp(-slope rounds) as a sum of two numbers: a decay is applied once a round, and what its rounding loses would add up.
+struct Fade {
+  float hi, lo;
+};
+__device__ __forceinline__ Fade fade_of(const Linear& p, int kvh, int rounds) {
+  const double f = p.slopes && rounds ? exp(-(double)p.slopes[kvh] * rounds) : 1.0;
+  Fade r;
+  r.hi = (float)f;
+  r.lo = fabsf(r.hi) < INFINITY ? (float)(f - (double)r.hi) : 0.0f;
+  return r;
+}
+__device__ __forceinline__ float faded(float s, Fade f, float add) { return fmaf(s, f.hi, fmaf(s, f.lo, add)); }
+
+// Splits v into bf16 parts: v = hi + lo to 16 bits.
+__device__ __forceinline__ float bf16_of(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = bf16_pack(a, b);
+  lo = bf16_pack(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+}
+
+template <int DP>
+struct Shape {
+  static constexpr int KB = DP / 32;                               // blocks of 32 channels
+  static constexpr int NW = DP == 32 ? 1 : DP == 64 ? 4 : 8;       // waves
+  static constexpr int NBW = KB * KB / NW;                         // blocks of S of a wave
+  static constexpr int NT = NW * 64;
+};
+
+// PAIRS: narrow rounds.  OUT: the results of a segment from the S that it starts from; otherwise its own S.
+template <int DP, bool PAIRS, bool OUT>
+__global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
+  using Sh = Shape<DP>;
+  constexpr int KB = Sh::KB, NW = Sh::NW, NBW = Sh::NBW, NT = Sh::NT;
+  constexpr int G = TILE * (DP / 8) / NT;  // granules of K (and of V) that a thread stages
+  constexpr int KEYS = NT / (DP / 8);      // tokens from one of them to the next
+  // parts that the columns of a block of results are dealt to waves in (narrow rounds: few rows, and many waves)
+  constexpr int MS = PAIRS ? (KB < NW / 2 ? KB : NW > 1 ? NW / 2 : 1) : KB / 2 > 1 ? KB / 2 : 1, MB = KB / MS;
+  __shared__ __attribute__((aligned(16))) uint8_t lk[2][TILE * DP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * DP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? DP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
+  __shared__ __attribute__((aligned(16))) float lt[PAIRS ? TILE : 4];   // round of a tile's token
+  __shared__ __attribute__((aligned(16))) float lw[PAIRS ? TILE : 4];   // what its key counts for after the tile
+  __shared__ float lp[PAIRS ? TILE + 1 : 1];                            // decay over that many rounds
+  __shared__ int odd_flag[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  const int segment = blockIdx.x % p.segments, kvh = blockIdx.x / p.segments % p.kv_heads, b = blockIdx.x / p.segments / p.kv_heads;
+  const int D = p.head_dim, len = length_of(p, b);
+  const long long first = (long long)segment * p.segment_rounds * p.per_round;  // tokens of this segment
+  const long long last = min((long long)len, first + (long long)p.segment_rounds * p.per_round);
+  const long long state_at = (long long)(b * p.kv_heads + kvh) * D * D;
+  float* const own = p.starts + (state_at * p.segments + (long long)segment * D * D);
+  const int dkb = wave % KB, dvb = wave / KB * NBW;
+
+  f32x16 S[NBW];
+  {
+    const float* from = !OUT ? nullptr : p.segments > 1 ? own : p.state ? p.state + state_at : nullptr;
 #pragma unroll
-  for (int m = 0; m < 8; ++m) s[m] = p.state && r + 16 * m < D && col < D ? p.state[at + (r + 16 * m) * D + col] : 0.0f;
-  for (long long n00 = 0; n00 < len; n00 += p.per_round) {
-    const int n0 = (int)n00;
-    const int n1 = (int)min((long long)len, (long long)n0 + p.per_round);
+    for (int j = 0; j < NBW; ++j)
 #pragma unroll
-    for (int m = 0; m < 8; ++m) s[m] *= fade;
-    for (int n = n0; n < n1; ++n) {
-      const uint16_t* k = p.k + b * p.k_b + n * p.k_t + kvh * p.k_h;
-      const float v = col < D ? load1(p.v + b * p.v_b + n * p.v_t + kvh * p.v_h + col) : 0.0f;
-#pragma unroll
-      for (int m = 0; m < 8; ++m)
-        if (r + 16 * m < D) s[m] = fmaf(load1(k + r + 16 * m), v, s[m]);
-    }
-    for (int n = n0; n < n1; ++n)
-      for (int g = 0; g < p.group; ++g) {
-        const int h = kvh * p.group + g;
-        const uint16_t* q = p.q + b * p.q_b + n * p.q_t + h * p.q_h;
-        float sum = 0.0f;
-#pragma unroll
-        for (int m = 0; m < 8; ++m)
-          if (r + 16 * m < D) sum = fmaf(load1(q + r + 16 * m), s[m], sum);
-        part[r][c] = sum;
-        __syncthreads();
-        if (r == 0 && col < D) {
-          for (int m = 1; m < 16; ++m) sum += part[m][c];
-          store1(p.out + b * p.o_b + n * p.o_t + h * p.o_h + col, sum * p.scale);
-        }
-        __syncthreads();
+      for (int e = 0; e < 16; ++e) {
+        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = 32 * (dvb + j) + (lane & 31);
+        S[j][e] = from && dk < D && dv < D ? from[dk * D + dv] : 0.0f;
       }
   }
+  auto store_state = [&](float* to) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m)
-    if (p.state_out && r + 16 * m < D && col < D) p.state_out[at + (r + 16 * m) * D + col] = s[m];
+    for (int j = 0; j < NBW; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = 32 * (dvb + j) + (lane & 31);
+        if (dk < D && dv < D) to[dk * D + dv] = S[j][e];
+      }
+  };
+  // Slopes past 2^60 leave a row its own round, as 2^60 does; zero rounds stay 0.  (Taken here: with a choice between
+  // matrix instructions and the first reader of their result the compiler leaves too little time on the shorter way.)
+  const float slope = p.slopes ? fminf(fmaxf(p.slopes[kvh] * -LOG2E, -0x1p60f), 0x1p60f) : 0.0f;
+  const Fade fade = fade_of(p, kvh, PAIRS ? p.tile_rounds : 1);
+
+  const uint16_t* kb = p.k + b * p.k_b + kvh * p.k_h;
+  const uint16_t* vb = p.v + b * p.v_b + kvh * p.v_h;
+  // columns past head_dim stay the zeros that they are set to here
+  if (D < DP)
+    for (int c = tid; c < TILE * (DP / 8); c += NT)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) *(uint4*)(lk[n] + c * 16) = *(uint4*)(lv[n] + c * 16) = make_uint4(0, 0, 0, 0);
+  if constexpr (PAIRS) {
+    for (int i = tid; i <= TILE; i += NT) lp[i] = p.slopes && i ? (float)exp(-(double)p.slopes[kvh] * i) : 1.0f;
+    for (int i = tid; i < TILE; i += NT) lt[i] = (float)(i / p.per_round);
+  }
+  if (tid < 2) odd_flag[tid] = 0;
+  __syncthreads();
+  // the keys' weights in a tile of so many rounds
+  auto weigh = [&](int rounds) {
+    for (int i = tid; i < TILE; i += NT) lw[i] = lp[max(rounds - 1 - (int)lt[i], 0)];
+  };
+
+  // Staging, straight into LDS: granule slots tid + n NT.  Tokens past the tile's end repeat its last.
+  const int key0 = tid / (DP / 8), slot0 = tid % (DP / 8);
+  auto load_tile = [&](int buf, long long at, int valid) {
+#pragma unroll
+    for (int n = 0; n < G; ++n) {
+      const int key = key0 + n * KEYS, slot = (n * NT + wave * 64) * 16;
+      const long long token = at + min(key, valid - 1);
+      const int kc = (slot0 ^ (k_place<DP>(key, 0) >> 4) % (DP / 8)) * 8, vc = (slot0 ^ (v_place<DP>(key, 0) >> 4) % (DP / 8)) * 8;
+      if (kc < D) send16(kb + token * p.k_t + kc, lk[buf] + slot);
+      if (vc < D) send16(vb + token * p.v_t + vc, lv[buf] + slot);
+    }
+  };
+  // notes an infinity or a NaN in V, once this thread's granules have landed
+  auto note_odd = [&](int buf) {
+    uint32_t carry = 0;
+#pragma unroll
+    for (int n = 0; n < G; ++n) {
+      const uint4 w = *(const uint4*)(lv[buf] + (tid + n * NT) * 16);
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) carry |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
+    }
+    if (carry & 0x80008000u) odd_flag[buf] = 1;
+  };
+
+  // LDS places of this lane's transposed operands: four tokens from 4 half on, and eight on from there
+  const int vkey = (lane & 15) >> 2, vgran = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), vbyte = (lane & 1) * 8;
+  const int k_tr[2] = {k_place<DP>(vkey + 4 * half, 4 * dkb + vgran) + vbyte, k_place<DP>(vkey + 4 * half + 8, 4 * dkb + vgran) + vbyte};
+  auto v_tr = [&](int block, int hi) { return v_place<DP>(vkey, 4 * block + vgran) + vbyte + (4 * half + 8 * hi) * DP * 2; };
+  auto columns = [&](const uint8_t* f, const uint8_t* g) {
+    return __builtin_shufflevector(read_columns(f), read_columns(g), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // token 16 s + 4 half + {0 .. 3, 8 .. 11} of elements 0 .. 7
+  auto token_of = [&](int s, int e) { return 16 * s + 4 * half + (e & 3) + 8 * (e >> 2); };
+
+  // S = fade S + K^T V over the tile's tokens
+  auto update = [&](int buf, int valid, bool begins, Fade f) {
+    if (begins) {
+#pragma unroll
+      for (int j = 0; j < NBW; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[j][e] = faded(S[j][e], f, 0.0f);
+    }
+#pragma unroll
+    for (int s = 0; s < TILE / 16; ++s) {
+      if (16 * s >= valid) break;
+      s16x8 a = columns(lk[buf] + k_tr[0] + 16 * s * DP * 2, lk[buf] + k_tr[1] + 16 * s * DP * 2);
+      s16x8 v[NBW];
+#pragma unroll
+      for (int j = 0; j < NBW; ++j) v[j] = columns(lv[buf] + v_tr(dvb + j, 0) + 16 * s * DP * 2, lv[buf] + v_tr(dvb + j, 1) + 16 * s * DP * 2);
+      if (16 * s + 16 > valid) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool in = token_of(s, e) < valid;
+          a[e] = in ? a[e] : 0;
+#pragma unroll
+          for (int j = 0; j < NBW; ++j) v[j][e] = in ? v[j][e] : 0;
+        }
+      }
+      if constexpr (PAIRS) {
+        const float4 w0 = *(const float4*)&lw[16 * s + 4 * half], w1 = *(const float4*)&lw[16 * s + 4 * half + 8];
+        const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        uint32_t part[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = bf16_of((uint16_t)a[2 * e]) * w[2 * e], y = bf16_of((uint16_t)a[2 * e + 1]) * w[2 * e + 1];
+          part[0][e] = bf16_pack(x, y);
+          const float x1 = x - __uint_as_float(part[0][e] << 16), y1 = y - __uint_as_float(part[0][e] & 0xffff0000u);
+          split2(x1, y1, part[1][e], part[2][e]);
+        }
+#pragma unroll
+        for (int n = 2; n >= 0; --n)
+#pragma unroll
+          for (int j = 0; j < NBW; ++j)
+            S[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8, make_uint4(part[n][0], part[n][1], part[n][2], part[n][3])), __builtin_bit_cast(bf16x8, v[j]), S[j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NBW; ++j)
+          S[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, v[j]), S[j], 0, 0, 0);
+      }
+    }
+  };
+  auto share_state = [&] {
+#pragma unroll
+    for (int j = 0; j < NBW; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint2 hi, lo;
+        split2(S[j][4 * g], S[j][4 * g + 1], hi.x, lo.x);
+        split2(S[j][4 * g + 2], S[j][4 * g + 3], hi.y, lo.y);
+        const int at = k_place<DP>(32 * (dvb + j) + (lane & 31), 4 * dkb + g) + 8 * half;
+        *(uint2*)(ls[0] + at) = hi;
+        *(uint2*)(ls[OUT ? 1 : 0] + at) = lo;
+      }
+  };
+
+  // The results of the queries of tokens at .. at + tokens - 1: rows token * group + head.
+  auto results = [&](int buf, long long at, int tokens) {
+    const int rows = tokens * p.group, blocks = (rows + 31) / 32;
+#pragma unroll 1
+    for (int unit = wave; unit < blocks * MS; unit += NW) {
+      const int m0 = unit % MS * MB, row = unit / MS * 32 + (lane & 31);
+      const int r = min(row, rows - 1), i = r / p.group, head = kvh * p.group + r % p.group;
+      const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
+      bf16x8 fq[DP / 16];
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) {
+        const int d = 16 * s + 8 * half;
+        const uint4 w = d < D ? *(const uint4*)(q + d) : make_uint4(0, 0, 0, 0);
+        fq[s] = __builtin_bit_cast(bf16x8, w);
+      }
+      f32x16 o[MB];
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[m][e] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          const int f = k_place<DP>(32 * (m0 + m) + (lane & 31), 2 * s + half);
+          const uint4 lo = *(const uint4*)(ls[OUT ? 1 : 0] + f), hi = *(const uint4*)(ls[0] + f);
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), fq[s], o[m], 0, 0, 0);
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), fq[s], o[m], 0, 0, 0);
+        }
+      if constexpr (PAIRS) {
+        const float ti = lt[i], before = lp[(int)ti + 1];
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[m][e] *= before;
+        const bool odd = odd_flag[buf] != 0;
+#pragma unroll 1
+        for (int n = 0; n < 2; ++n) {
+          if (32 * n >= tokens) break;
+          f32x16 z;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < DP / 16; ++s) {
+            const uint4 w = *(const uint4*)(lk[buf] + k_place<DP>(lane & 31, 2 * s + half) + 32 * n * DP * 2);
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z, 0, 0, 0);
+          }
+          uint32_t seen = 0;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float4 t = *(const float4*)&lt[32 * n + 8 * g + 4 * half];
+            const float tj[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float far = ti - tj[e];
+              const bool in = far >= 0.0f && 32 * n + 8 * g + 4 * half + e < tokens;
+              z[4 * g + e] = in ? z[4 * g + e] * __builtin_amdgcn_exp2f(slope * far) : 0.0f;
+              seen |= (uint32_t)in << (4 * g + e);
+            }
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (32 * n + 16 * s >= tokens) break;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2(z[8 * s + 2 * e], z[8 * s + 2 * e + 1], hi[e], lo[e]);
+            const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+            const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+              const int step = (32 * n + 16 * s) * DP * 2;
+              s16x8 v = columns(lv[buf] + v_tr(m0 + m, 0) + step, lv[buf] + v_tr(m0 + m, 1) + step);
+              if (odd) {
+                // 0 x infinity: values that are not finite count as 0, and then make the rows that see them NaN
+                s16x8 there, ones;
+                f32x16 count;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) count[e] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  there[e] = (v[e] & 0x7f80) == 0x7f80 ? 0x3f80 : 0;
+                  v[e] = there[e] ? 0 : v[e];
+                  ones[e] = seen >> (8 * s + e) & 1 ? 0x3f80 : 0;
+                }
+                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, there), __builtin_bit_cast(bf16x8, ones), count, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[m][e] = count[e] != 0.0f ? NAN : o[m][e];
+              }
+              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pl, o[m], 0, 0, 0);
+              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), ph, o[m], 0, 0, 0);
+            }
+          }
+        }
+      }
+      if (row < rows) {
+        uint16_t* out = p.out + b * p.o_b + (at + i) * p.o_t + head * p.o_h;
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int d = 32 * (m0 + m) + 8 * g + 4 * half;
+            if (d < D) {
+              uint2 w;
+              w.x = bf16_pack(o[m][4 * g] * p.scale, o[m][4 * g + 1] * p.scale);
+              w.y = bf16_pack(o[m][4 * g + 2] * p.scale, o[m][4 * g + 3] * p.scale);
+              *(uint2*)(out + d) = w;
+            }
+          }
+      }
+    }
+  };
+
+  // The tiles: [at, at + valid).  Wide rounds: a tile does not cross a round's end.
+  auto tile_end = [&](long long at, long long round_end) { return (int)(min(min(at + (PAIRS ? p.tile_tokens : TILE), round_end), last) - at); };
+  long long at = first, round_end = PAIRS ? last : first + p.per_round;
+  int buf = 0, valid = 0;
+  if (at < last) {
+    valid = tile_end(at, round_end);
+    load_tile(0, at, valid);
+  }
+  if constexpr (PAIRS) {
+    weigh(min(p.tile_rounds, (valid + p.per_round - 1) / p.per_round));
+    if constexpr (OUT) share_state();
+  }
+  sent();
+  if constexpr (PAIRS && OUT) note_odd(0);
+  __syncthreads();
+  long long round_at = at;
+  while (at < last) {
+    const long long next = at + valid;
+    const bool ends = PAIRS || next == round_end || next == last;
+    const bool begins = PAIRS || at == round_at;
+    long long next_end = round_end;
+    if (!PAIRS && next == round_end) next_end += p.per_round;
+    int next_valid = 0;
+    if (next < last) {
+      next_valid = tile_end(next, next_end);
+      load_tile(buf ^ 1, next, next_valid);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PAIRS) {
+      const int rounds = (valid + p.per_round - 1) / p.per_round;
+      if constexpr (OUT) results(buf, at, valid);
+      update(buf, valid, true, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
+      sent();
+      __syncthreads();  // S, the weights and this tile are read
+      if (next < last) {
+        if (OUT && tid == 0) odd_flag[buf] = 0;
+        if constexpr (OUT) {
+          note_odd(buf ^ 1);
+          share_state();
+        }
+        const int next_rounds = (next_valid + p.per_round - 1) / p.per_round;
+        if (next_rounds != rounds) weigh(next_rounds);
+      }
+      __syncthreads();
+    } else {
+      update(buf, valid, begins, fade);
+      if (OUT && ends) share_state();
+      sent();
+      __syncthreads();
+      if (OUT && ends) {
+        results(buf, round_at, (int)(next - round_at));
+        __syncthreads();
+      }
+    }
+    if (!PAIRS && ends) round_at = next;
+    at = next, valid = next_valid, round_end = next_end, buf ^= 1;
+  }
+  if constexpr (!OUT)
+    store_state(own);
+  else if (p.segments == 1 && p.state_out)
+    store_state(p.state_out + state_at);
+}
+
+// The S that each segment starts from, in the place of its own, and the last one.  A thread an element of S.
+__global__ void __launch_bounds__(256) linear_scan_kernel(const Linear p) {
+  const long long size = (long long)p.head_dim * p.head_dim;
+  const int blocks = (int)((size + 255) / 256);
+  const int bh = blockIdx.x / blocks, kvh = bh % p.kv_heads, b = bh / p.kv_heads;
+  const long long i = (long long)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  if (i >= size) return;
+  const int len = length_of(p, b);
+  const int rounds = (int)(((long long)len + p.per_round - 1) / p.per_round);
+  const int whole = rounds / p.segment_rounds, rest = rounds % p.segment_rounds;
+  const Fade fade = fade_of(p, kvh, p.segment_rounds);
+  float s = p.state ? p.state[bh * size + i] : 0.0f;
+  float* at = p.starts + bh * p.segments * size + i;
+#pragma unroll 8
+  for (int n = 0; n < whole; ++n) {
+    const float own = at[n * size];
+    at[n * size] = s;
+    s = faded(s, fade, own);
+  }
+  if (rest) {
+    const float own = at[whole * size];
+    at[whole * size] = s;
+    s = faded(s, fade_of(p, kvh, rest), own);
+  }
+  if (p.state_out) p.state_out[bh * size + i] = s;
+}
+
+// One token an entry: thread (r, c) holds columns 4 c .. 4 c + 3 of rows r + ROWS n.
+template <int DP>
+__global__ void __launch_bounds__(256) linear_token_kernel(const Linear p) {
+  constexpr int COLS = DP / 4, ROWS = 256 / COLS, N = DP / ROWS;
+  __shared__ float4 part[ROWS][COLS];
+  const int tid = threadIdx.x, c = tid % COLS, r = tid / COLS, D = p.head_dim;
+  const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads;
+  const long long at = (long long)blockIdx.x * D * D;
+  const bool token = length_of(p, b) > 0;
+  const bool col = 4 * c < D;
+  float4 s[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    s[n] = p.state && col && r + ROWS * n < D ? *(const float4*)(p.state + at + (r + ROWS * n) * D + 4 * c) : make_float4(0, 0, 0, 0);
+  if (token) {
+    const Fade fade = fade_of(p, kvh, 1);
+    const uint16_t* k = p.k + b * p.k_b + kvh * p.k_h;
+    float v[4] = {};
+    if (col) {
+      const uint2 w = *(const uint2*)(p.v + b * p.v_b + kvh * p.v_h + 4 * c);
+      v[0] = bf16_of(w.x & 0xffff), v[1] = bf16_of(w.x >> 16), v[2] = bf16_of(w.y & 0xffff), v[3] = bf16_of(w.y >> 16);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float x = r + ROWS * n < D ? load1(k + r + ROWS * n) : 0.0f;
+      s[n].x = faded(s[n].x, fade, x * v[0]), s[n].y = faded(s[n].y, fade, x * v[1]);
+      s[n].z = faded(s[n].z, fade, x * v[2]), s[n].w = faded(s[n].w, fade, x * v[3]);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (p.state_out && col && r + ROWS * n < D) *(float4*)(p.state_out + at + (r + ROWS * n) * D + 4 * c) = s[n];
+  if (!token) return;
+  for (int g = 0; g < p.group; ++g) {
+    const int h = kvh * p.group + g;
+    const uint16_t* q = p.q + b * p.q_b + h * p.q_h;
+    float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float x = r + ROWS * n < D ? load1(q + r + ROWS * n) : 0.0f;
+      o.x = fmaf(x, s[n].x, o.x), o.y = fmaf(x, s[n].y, o.y), o.z = fmaf(x, s[n].z, o.z), o.w = fmaf(x, s[n].w, o.w);
+    }
+    __syncthreads();
+    part[r][c] = o;
+    __syncthreads();
+    if (r == 0 && col) {
+      for (int n = 1; n < ROWS; ++n) {
+        const float4 w = part[n][c];
+        o.x += w.x, o.y += w.y, o.z += w.z, o.w += w.w;
+      }
+      uint2 w;
+      w.x = bf16_pack(o.x * p.scale, o.y * p.scale), w.y = bf16_pack(o.z * p.scale, o.w * p.scale);
+      *(uint2*)(p.out + b * p.o_b + h * p.o_h + 4 * c) = w;
+    }
+  }
+}
+
+// How a call runs.
+struct Plan {
+  bool pairs;
+  int tile_rounds, tile_tokens, segments, segment_rounds;
+  size_t bytes;
+  long long items;
+};
+
+Plan plan_for(const pd_linear_attention_args* a) {
+  Plan n = {};
+  n.pairs = a->per_round <= NARROW;
+  n.tile_rounds = n.pairs ? TILE / a->per_round : 1;
+  n.tile_tokens = n.pairs ? n.tile_rounds * a->per_round : TILE;
+  const long long rounds = ((long long)a->n + a->per_round - 1) / a->per_round, heads = std::max(1ll, (long long)a->batch * a->kv_heads);
+  // Segments, to fill the card, while each holds tokens whose reading outweighs its state's (written, read twice and written by the scan).
+  const long long fill = a->head_dim <= 32 ? 4096 : a->head_dim <= 64 ? 768 : 256;
+  const long long most = (long long)a->n / (4 * a->head_dim < 256 ? 256 : 4 * a->head_dim);
+  long long segments = (fill + heads - 1) / heads;
+  if (segments > most) segments = most;
+  if (segments < 1 || 2 * heads > fill) segments = 1;
+  long long each = rounds ? (rounds + segments - 1) / segments : 1;
+  each = (each + n.tile_rounds - 1) / n.tile_rounds * n.tile_rounds;
+  n.segment_rounds = (int)(each < INT32_MAX - 64 ? each : INT32_MAX - 64);
+  n.segments = rounds ? (int)((rounds + n.segment_rounds - 1) / n.segment_rounds) : 1;
+  n.bytes = n.segments > 1 ? (size_t)heads * n.segments * a->head_dim * a->head_dim * 4 : 0;
+  n.items = heads * n.segments;
+  return n;
 }
 
 bool rows16(const void* p, long long b, long long t, long long h) {
@@ -84,7 +548,9 @@ pd_status check(const pd_linear_attention_args* a, bool pointers) {
   if (a->heads && (!a->kv_heads || a->heads % a->kv_heads)) return PD_ERR_INVALID_ARG;
   if (a->head_dim % 8 || a->head_dim > 128) return PD_ERR_UNSUPPORTED;
   if (a->heads && a->heads / a->kv_heads > 64) return PD_ERR_UNSUPPORTED;
-  if ((long long)a->kv_heads * a->batch > 65535) return PD_ERR_UNSUPPORTED;
+  // work items, and the scan's, are counted by the launches (threads below 2^32)
+  if ((__int128)a->kv_heads * a->batch >= 1ll << 17 || plan_for(a).items >= 1ll << 22) return PD_ERR_UNSUPPORTED;
+  if ((__int128)a->n * (a->kv_heads ? a->heads / a->kv_heads : 1) >= 1ll << 30) return PD_ERR_UNSUPPORTED;  // rows, in 32 bits
   if (!pointers || !a->batch || !a->heads) return PD_OK;
   if ((uintptr_t)a->slopes % 4 || (uintptr_t)a->lengths % 4 || (uintptr_t)a->state % 16 || (uintptr_t)a->state_out % 16) return PD_ERR_INVALID_ARG;
   if (!a->n) return PD_OK;
@@ -96,12 +562,38 @@ pd_status check(const pd_linear_attention_args* a, bool pointers) {
     return PD_ERR_UNSUPPORTED;
   if (!rows_apart(a->head_dim, {{a->batch, a->out_batch_stride}, {a->n, a->out_token_stride}, {a->heads, a->out_head_stride}}))
     return PD_ERR_INVALID_ARG;
+  const size_t need = plan_for(a).bytes;
+  if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return PD_ERR_INVALID_ARG;
   return PD_OK;
+}
+
+template <int DP>
+void launch(const Linear& p, bool pairs, hipStream_t st) {
+  const unsigned heads = (unsigned)(p.batch * p.kv_heads);
+  if (p.n == 1) {
+    hipLaunchKernelGGL(linear_token_kernel<DP>, dim3(heads), dim3(256), 0, st, p);
+    return;
+  }
+  const dim3 grid(heads * p.segments), threads(Shape<DP>::NT);
+  if (p.segments > 1) {
+    if (pairs)
+      hipLaunchKernelGGL((linear_kernel<DP, true, false>), grid, threads, 0, st, p);
+    else
+      hipLaunchKernelGGL((linear_kernel<DP, false, false>), grid, threads, 0, st, p);
+    hipLaunchKernelGGL(linear_scan_kernel, dim3(heads * ((p.head_dim * p.head_dim + 255) / 256)), dim3(256), 0, st, p);
+  }
+  if (pairs)
+    hipLaunchKernelGGL((linear_kernel<DP, true, true>), grid, threads, 0, st, p);
+  else
+    hipLaunchKernelGGL((linear_kernel<DP, false, true>), grid, threads, 0, st, p);
 }
 
 }  // namespace
 
-extern "C" size_t predecoder_linear_attention_workspace(const pd_linear_attention_args* a) { return 0; }
+extern "C" size_t predecoder_linear_attention_workspace(const pd_linear_attention_args* a) {
+  if (check(a, false) != PD_OK || !a->batch || !a->heads) return 0;
+  return plan_for(a).bytes;
+}
 
 extern "C" pd_status predecoder_linear_attention(void* hip_stream, const pd_linear_attention_args* a) {
   const pd_status ok = check(a, true);
@@ -116,7 +608,15 @@ extern "C" pd_status predecoder_linear_attention(void* hip_stream, const pd_line
   p.v_b = a->v_batch_stride, p.v_t = a->v_token_stride, p.v_h = a->v_head_stride;
   p.o_b = a->out_batch_stride, p.o_t = a->out_token_stride, p.o_h = a->out_head_stride;
   p.slopes = a->slopes, p.lengths = a->lengths, p.state = a->state, p.state_out = a->state_out;
-  hipLaunchKernelGGL(linear_simple_kernel, dim3((a->head_dim + 15) / 16, (unsigned)(a->kv_heads * a->batch)), dim3(256), 0,
-                     (hipStream_t)hip_stream, p);
+  const Plan n = plan_for(a);
+  p.tile_rounds = n.tile_rounds, p.tile_tokens = n.tile_tokens, p.segments = n.segments, p.segment_rounds = n.segment_rounds;
+  p.starts = (float*)a->workspace;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  if (a->head_dim <= 32)
+    launch<32>(p, n.pairs, st);
+  else if (a->head_dim <= 64)
+    launch<64>(p, n.pairs, st);
+  else
+    launch<128>(p, n.pairs, st);
   return hipGetLastError() == hipSuccess ? PD_OK : PD_ERR_DEVICE;
 }
