@@ -29,6 +29,9 @@ __device__ __forceinline__ void send16(const void* base, uint32_t at, const void
 __device__ __forceinline__ void send4(const void* base, uint32_t at, const void* to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte(to)), "v"(at), "s"(base));
 }
+__device__ __forceinline__ void send4at(const void* from, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(lds_byte(to)), "v"(from));
+}
 __device__ __forceinline__ void sent() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
