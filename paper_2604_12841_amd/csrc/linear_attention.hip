@@ -87,13 +87,13 @@ struct Shape {
 
 // PAIRS: narrow rounds.  OUT: the results of a segment from the S that it starts from; otherwise its own S.
 template <int DP, bool PAIRS, bool OUT>
-__global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
+__global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel(const Linear p) {
   using Sh = Shape<DP>;
   constexpr int KB = Sh::KB, NW = Sh::NW, NBW = Sh::NBW, NT = Sh::NT;
   constexpr int G = TILE * (DP / 8) / NT;  // granules of K (and of V) that a thread stages
   constexpr int KEYS = NT / (DP / 8);      // tokens from one of them to the next
   // parts that the columns of a block of results are dealt to waves in (narrow rounds: few rows, and many waves)
-  constexpr int MS = PAIRS ? (KB < NW / 2 ? KB : NW > 1 ? NW / 2 : 1) : KB / 2 > 1 ? KB / 2 : 1, MB = KB / MS;
+  constexpr int MS = PAIRS ? (KB < NW / 2 ? KB : NW > 1 ? NW / 2 : 1) : 1, MB = KB / MS;
   __shared__ __attribute__((aligned(16))) uint8_t lk[2][TILE * DP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * DP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? DP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
@@ -118,7 +118,8 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = 32 * (dvb + j) + (lane & 31);
-        S[j][e] = from && dk < D && dv < D ? from[dk * D + dv] : 0.0f;
+        S[j][e] = from ? from[min(dk, D - 1) * D + min(dv, D - 1)] : 0.0f;
+        if (dk >= D || dv >= D) S[j][e] = 0.0f;
       }
   }
   auto store_state = [&](float* to) {
@@ -161,8 +162,13 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
       const int key = key0 + n * KEYS, slot = (n * NT + wave * 64) * 16;
       const long long token = at + min(key, valid - 1);
       const int kc = (slot0 ^ (k_place<DP>(key, 0) >> 4) % (DP / 8)) * 8, vc = (slot0 ^ (v_place<DP>(key, 0) >> 4) % (DP / 8)) * 8;
-      if (kc < D) send16(kb + token * p.k_t + kc, lk[buf] + slot);
-      if (vc < D) send16(vb + token * p.v_t + vc, lv[buf] + slot);
+      if (D == DP) {
+        send16(kb + token * p.k_t + kc, lk[buf] + slot);
+        send16(vb + token * p.v_t + vc, lv[buf] + slot);
+      } else {
+        if (kc < D) send16(kb + token * p.k_t + kc, lk[buf] + slot);
+        if (vc < D) send16(vb + token * p.v_t + vc, lv[buf] + slot);
+      }
     }
   };
   // notes an infinity or a NaN in V, once this thread's granules have landed
@@ -196,7 +202,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) S[j][e] = faded(S[j][e], f, 0.0f);
     }
-#pragma unroll
+#pragma unroll 1
     for (int s = 0; s < TILE / 16; ++s) {
       if (16 * s >= valid) break;
       s16x8 a = columns(lk[buf] + k_tr[0] + 16 * s * DP * 2, lk[buf] + k_tr[1] + 16 * s * DP * 2);
@@ -250,28 +256,46 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
       }
   };
 
-  // The results of the queries of tokens at .. at + tokens - 1: rows token * group + head.
+  // The results of the queries of tokens at .. at + tokens - 1: rows token * group + head, 32 of them a unit.  The
+  // queries of a wave's next unit are on their way while it works on one; fetch() sends for those of the first.
+  uint4 next_q[DP / 16];
+  auto place_of = [&](int unit, int tokens, int& row, int& i, int& head) {
+    row = unit / MS * 32 + (lane & 31);
+    const int r = min(row, tokens * p.group - 1);
+    i = r / p.group, head = kvh * p.group + r % p.group;
+  };
+  auto fetch_unit = [&](long long at, int tokens, int unit) {
+    int row, i, head;
+    place_of(unit, tokens, row, i, head);
+    const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      // (past head_dim anything of the row will do: S and the keys are 0 there)
+      next_q[s] = *(const uint4*)(q + min(16 * s + 8 * half, D - 8));
+    }
+  };
+  auto units_of = [&](int tokens) { return (tokens * p.group + 31) / 32 * MS; };
+  auto fetch = [&](long long at, int tokens) {
+    if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
+  };
   auto results = [&](int buf, long long at, int tokens) {
-    const int rows = tokens * p.group, blocks = (rows + 31) / 32;
+    const int rows = tokens * p.group, units = units_of(tokens);
 #pragma unroll 1
-    for (int unit = wave; unit < blocks * MS; unit += NW) {
-      const int m0 = unit % MS * MB, row = unit / MS * 32 + (lane & 31);
-      const int r = min(row, rows - 1), i = r / p.group, head = kvh * p.group + r % p.group;
-      const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
+    for (int unit = wave; unit < units; unit += NW) {
+      int row, i, head;
+      place_of(unit, tokens, row, i, head);
+      const int m0 = unit % MS * MB;
       bf16x8 fq[DP / 16];
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s) {
-        const int d = 16 * s + 8 * half;
-        const uint4 w = d < D ? *(const uint4*)(q + d) : make_uint4(0, 0, 0, 0);
-        fq[s] = __builtin_bit_cast(bf16x8, w);
-      }
+      for (int s = 0; s < DP / 16; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
+      if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
       f32x16 o[MB];
 #pragma unroll
       for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[m][e] = 0.0f;
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s)
+      for (int s = 0; s < DP / 16; ++s) {
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           const int f = k_place<DP>(32 * (m0 + m) + (lane & 31), 2 * s + half);
@@ -279,6 +303,8 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
           o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), fq[s], o[m], 0, 0, 0);
           o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), fq[s], o[m], 0, 0, 0);
         }
+        if (s & 1) __builtin_amdgcn_sched_barrier(0);  // two steps' parts of S in registers at a time
+      }
       if constexpr (PAIRS) {
         const float ti = lt[i], before = lp[(int)ti + 1];
 #pragma unroll
@@ -372,7 +398,10 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
   }
   if constexpr (PAIRS) {
     weigh(min(p.tile_rounds, (valid + p.per_round - 1) / p.per_round));
-    if constexpr (OUT) share_state();
+    if constexpr (OUT) {
+      if (at < last) fetch(at, valid);
+      share_state();
+    }
   }
   sent();
   if constexpr (PAIRS && OUT) note_odd(0);
@@ -392,7 +421,10 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (PAIRS) {
       const int rounds = (valid + p.per_round - 1) / p.per_round;
-      if constexpr (OUT) results(buf, at, valid);
+      if constexpr (OUT) {
+        results(buf, at, valid);
+        if (next < last) fetch(next, next_valid);
+      }
       update(buf, valid, true, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
       sent();
       __syncthreads();  // S, the weights and this tile are read
@@ -407,6 +439,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT) linear_kernel(const Linear p) {
       }
       __syncthreads();
     } else {
+      if (OUT && ends) fetch(round_at, (int)(next - round_at));
       update(buf, valid, begins, fade);
       if (OUT && ends) share_state();
       sent();
@@ -438,11 +471,18 @@ __global__ void __launch_bounds__(256) linear_scan_kernel(const Linear p) {
   const Fade fade = fade_of(p, kvh, p.segment_rounds);
   float s = p.state ? p.state[bh * size + i] : 0.0f;
   float* at = p.starts + bh * p.segments * size + i;
-#pragma unroll 8
-  for (int n = 0; n < whole; ++n) {
-    const float own = at[n * size];
-    at[n * size] = s;
-    s = faded(s, fade, own);
+  // (loads of several segments together: a store after each would hold the next one back)
+  constexpr int BATCH = 16;
+  for (int n0 = 0; n0 < whole; n0 += BATCH) {
+    float own[BATCH];
+#pragma unroll
+    for (int n = 0; n < BATCH; ++n) own[n] = n0 + n < whole ? at[(n0 + n) * size] : 0.0f;
+#pragma unroll
+    for (int n = 0; n < BATCH; ++n)
+      if (n0 + n < whole) {
+        at[(n0 + n) * size] = s;
+        s = faded(s, fade, own[n]);
+      }
   }
   if (rest) {
     const float own = at[whole * size];
