@@ -22,6 +22,7 @@
 // Recurrent form (one token an entry): S is read, updated, multiplied by q and
 // written by threads that hold four columns of some rows.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 
 #include "../../include/predecoder_ops.h"
@@ -33,13 +34,12 @@ namespace {
 using namespace pd;
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int TILE = 64;  // tokens
 constexpr int NARROW = 32;  // a round of up to as many tokens shares its tile with others
 
 struct Linear {
   int batch, heads, kv_heads, group, head_dim, n, per_round;
   int tile_rounds;  // narrow rounds: of a tile
-  int tile_tokens;  // narrow rounds: tile_rounds per_round; else TILE
+  int tile_tokens;  // narrow rounds: tile_rounds per_round; else a tile's
   int segments;
   int segment_rounds;  // narrow rounds: a multiple of tile_rounds
   float scale;
@@ -77,32 +77,37 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
   lo = bf16_pack(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
 }
 
+// A workgroup holds all rows of S (the key's channels, padded to DP) and VP of its columns (the value's channels).
 template <int DP>
 struct Shape {
-  static constexpr int KB = DP / 32;                               // blocks of 32 channels
-  static constexpr int NW = DP == 32 ? 1 : DP == 64 ? 4 : 8;       // waves
-  static constexpr int NBW = KB * KB / NW;                         // blocks of S of a wave
+  static constexpr int VP = DP == 128 ? 64 : DP;
+  static constexpr int TILE = DP == 128 ? 48 : 64;      // tokens: two workgroups' tiles and S fit a CU's LDS
+  static constexpr int KB = DP / 32, VB = VP / 32;      // blocks of 32 channels
+  static constexpr int NW = DP == 32 ? 1 : 4;           // waves
+  static constexpr int NBW = KB * VB / NW;              // blocks of S of a wave
   static constexpr int NT = NW * 64;
 };
 
 // PAIRS: narrow rounds.  OUT: the results of a segment from the S that it starts from; otherwise its own S.
 template <int DP, bool PAIRS, bool OUT>
-__global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel(const Linear p) {
+__global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p) {
   using Sh = Shape<DP>;
-  constexpr int KB = Sh::KB, NW = Sh::NW, NBW = Sh::NBW, NT = Sh::NT;
-  constexpr int G = TILE * (DP / 8) / NT;  // granules of K (and of V) that a thread stages
-  constexpr int KEYS = NT / (DP / 8);      // tokens from one of them to the next
+  constexpr int VP = Sh::VP, TILE = Sh::TILE, KB = Sh::KB, VB = Sh::VB, NW = Sh::NW, NBW = Sh::NBW, NT = Sh::NT;
   // parts that the columns of a block of results are dealt to waves in (narrow rounds: few rows, and many waves)
-  constexpr int MS = PAIRS ? (KB < NW / 2 ? KB : NW > 1 ? NW / 2 : 1) : 1, MB = KB / MS;
+  constexpr int MS = PAIRS ? VB : 1, MB = VB / MS;
   __shared__ __attribute__((aligned(16))) uint8_t lk[2][TILE * DP * 2];
-  __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * DP * 2];
-  __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? DP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
-  __shared__ __attribute__((aligned(16))) float lt[PAIRS ? TILE : 4];   // round of a tile's token
+  __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * VP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? VP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
+  __shared__ __attribute__((aligned(16))) float lt[PAIRS ? 64 : 4];   // round of a tile's token
   __shared__ __attribute__((aligned(16))) float lw[PAIRS ? TILE : 4];   // what its key counts for after the tile
   __shared__ float lp[PAIRS ? TILE + 1 : 1];                            // decay over that many rounds
   __shared__ int odd_flag[2];
+  __shared__ __attribute__((aligned(16))) uint8_t lo[OUT ? NW : 1][OUT ? 32 * 64 : 16];  // 32 columns of a unit's results
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int segment = blockIdx.x % p.segments, kvh = blockIdx.x / p.segments % p.kv_heads, b = blockIdx.x / p.segments / p.kv_heads;
+  // (workgroups are dealt to the eight XCDs in turn: the two that share a segment's queries and keys go to one, for its L2)
+  const int item = VP == DP ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7), v0 = VP == DP ? 0 : VP * ((blockIdx.x >> 3) & 1);
+  if (item >= p.batch * p.kv_heads * p.segments) return;
+  const int segment = item % p.segments, kvh = item / p.segments % p.kv_heads, b = item / p.segments / p.kv_heads;
   const int D = p.head_dim, len = length_of(p, b);
   const long long first = (long long)segment * p.segment_rounds * p.per_round;  // tokens of this segment
   const long long last = min((long long)len, first + (long long)p.segment_rounds * p.per_round);
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
     for (int j = 0; j < NBW; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = 32 * (dvb + j) + (lane & 31);
+        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = v0 + 32 * (dvb + j) + (lane & 31);
         S[j][e] = from ? from[min(dk, D - 1) * D + min(dv, D - 1)] : 0.0f;
         if (dk >= D || dv >= D) S[j][e] = 0.0f;
       }
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
     for (int j = 0; j < NBW; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = 32 * (dvb + j) + (lane & 31);
+        const int dk = 32 * dkb + 8 * (e >> 2) + 4 * half + (e & 3), dv = v0 + 32 * (dvb + j) + (lane & 31);
         if (dk < D && dv < D) to[dk * D + dv] = S[j][e];
       }
   };
@@ -139,13 +144,13 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
   const uint16_t* kb = p.k + b * p.k_b + kvh * p.k_h;
   const uint16_t* vb = p.v + b * p.v_b + kvh * p.v_h;
   // columns past head_dim stay the zeros that they are set to here
-  if (D < DP)
-    for (int c = tid; c < TILE * (DP / 8); c += NT)
-#pragma unroll
-      for (int n = 0; n < 2; ++n) *(uint4*)(lk[n] + c * 16) = *(uint4*)(lv[n] + c * 16) = make_uint4(0, 0, 0, 0);
+  if (D < DP) {
+    for (int c = tid; c < 2 * TILE * (DP / 8); c += NT) *(uint4*)(lk[0] + c * 16) = make_uint4(0, 0, 0, 0);
+    for (int c = tid; c < 2 * TILE * (VP / 8); c += NT) *(uint4*)(lv[0] + c * 16) = make_uint4(0, 0, 0, 0);
+  }
   if constexpr (PAIRS) {
     for (int i = tid; i <= TILE; i += NT) lp[i] = p.slopes && i ? (float)exp(-(double)p.slopes[kvh] * i) : 1.0f;
-    for (int i = tid; i < TILE; i += NT) lt[i] = (float)(i / p.per_round);
+    for (int i = tid; i < 64; i += NT) lt[i] = (float)(i / p.per_round);
   }
   if (tid < 2) odd_flag[tid] = 0;
   __syncthreads();
@@ -155,27 +160,29 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
   };
 
   // Staging, straight into LDS: granule slots tid + n NT.  Tokens past the tile's end repeat its last.
-  const int key0 = tid / (DP / 8), slot0 = tid % (DP / 8);
   auto load_tile = [&](int buf, long long at, int valid) {
+    auto send = [&](auto width, const uint16_t* rows, long long stride, uint8_t* to, int first, auto place) {
+      constexpr int GR = decltype(width)::value / 8;  // granules of a row
 #pragma unroll
-    for (int n = 0; n < G; ++n) {
-      const int key = key0 + n * KEYS, slot = (n * NT + wave * 64) * 16;
-      const long long token = at + min(key, valid - 1);
-      const int kc = (slot0 ^ (k_place<DP>(key, 0) >> 4) % (DP / 8)) * 8, vc = (slot0 ^ (v_place<DP>(key, 0) >> 4) % (DP / 8)) * 8;
-      if (D == DP) {
-        send16(kb + token * p.k_t + kc, lk[buf] + slot);
-        send16(vb + token * p.v_t + vc, lv[buf] + slot);
-      } else {
-        if (kc < D) send16(kb + token * p.k_t + kc, lk[buf] + slot);
-        if (vc < D) send16(vb + token * p.v_t + vc, lv[buf] + slot);
+      for (int n = 0; n < (TILE * GR + NT - 1) / NT; ++n) {
+        if (n * NT + wave * 64 >= TILE * GR) break;
+        const int slot = tid + n * NT, key = slot / GR, c = first + (slot % GR ^ (place(key) >> 4) % GR) * 8;
+        const uint16_t* const from = rows + (at + min(key, valid - 1)) * stride + c;
+        if (D == DP)
+          send16(from, to + (n * NT + wave * 64) * 16);
+        else if (c < D)
+          send16(from, to + (n * NT + wave * 64) * 16);
       }
-    }
+    };
+    send(std::integral_constant<int, DP>(), kb, p.k_t, lk[buf], 0, [](int key) { return k_place<DP>(key, 0); });
+    send(std::integral_constant<int, VP>(), vb, p.v_t, lv[buf], v0, [](int key) { return v_place<VP>(key, 0); });
   };
   // notes an infinity or a NaN in V, once this thread's granules have landed
   auto note_odd = [&](int buf) {
     uint32_t carry = 0;
 #pragma unroll
-    for (int n = 0; n < G; ++n) {
+    for (int n = 0; n < (TILE * (VP / 8) + NT - 1) / NT; ++n) {
+      if (n * NT + wave * 64 >= TILE * (VP / 8)) break;
       const uint4 w = *(const uint4*)(lv[buf] + (tid + n * NT) * 16);
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -187,7 +194,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
   // LDS places of this lane's transposed operands: four tokens from 4 half on, and eight on from there
   const int vkey = (lane & 15) >> 2, vgran = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), vbyte = (lane & 1) * 8;
   const int k_tr[2] = {k_place<DP>(vkey + 4 * half, 4 * dkb + vgran) + vbyte, k_place<DP>(vkey + 4 * half + 8, 4 * dkb + vgran) + vbyte};
-  auto v_tr = [&](int block, int hi) { return v_place<DP>(vkey, 4 * block + vgran) + vbyte + (4 * half + 8 * hi) * DP * 2; };
+  auto v_tr = [&](int block, int hi) { return v_place<VP>(vkey, 4 * block + vgran) + vbyte + (4 * half + 8 * hi) * VP * 2; };
   auto columns = [&](const uint8_t* f, const uint8_t* g) {
     return __builtin_shufflevector(read_columns(f), read_columns(g), 0, 1, 2, 3, 4, 5, 6, 7);
   };
@@ -202,13 +209,13 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
 #pragma unroll
         for (int e = 0; e < 16; ++e) S[j][e] = faded(S[j][e], f, 0.0f);
     }
-#pragma unroll 1
+#pragma unroll(OUT ? 1 : 2)
     for (int s = 0; s < TILE / 16; ++s) {
       if (16 * s >= valid) break;
       s16x8 a = columns(lk[buf] + k_tr[0] + 16 * s * DP * 2, lk[buf] + k_tr[1] + 16 * s * DP * 2);
       s16x8 v[NBW];
 #pragma unroll
-      for (int j = 0; j < NBW; ++j) v[j] = columns(lv[buf] + v_tr(dvb + j, 0) + 16 * s * DP * 2, lv[buf] + v_tr(dvb + j, 1) + 16 * s * DP * 2);
+      for (int j = 0; j < NBW; ++j) v[j] = columns(lv[buf] + v_tr(dvb + j, 0) + 16 * s * VP * 2, lv[buf] + v_tr(dvb + j, 1) + 16 * s * VP * 2);
       if (16 * s + 16 > valid) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -258,11 +265,17 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
 
   // The results of the queries of tokens at .. at + tokens - 1: rows token * group + head, 32 of them a unit.  The
   // queries of a wave's next unit are on their way while it works on one; fetch() sends for those of the first.
+  int unit = 0;  // this wave's next
   uint4 next_q[DP / 16];
+  // (a division by the group: of the unit's first row, the same for all lanes, and of less than 128 by a product)
+  const int group_part = 65536 / p.group + 1;
+  auto token_at = [&](int unit, int lane_row, int& i, int& head) {
+    const int first = unit / MS * 32, from = first / p.group, x = first - from * p.group + lane_row, more = x * group_part >> 16;
+    i = from + more, head = kvh * p.group + x - more * p.group;
+  };
   auto place_of = [&](int unit, int tokens, int& row, int& i, int& head) {
     row = unit / MS * 32 + (lane & 31);
-    const int r = min(row, tokens * p.group - 1);
-    i = r / p.group, head = kvh * p.group + r % p.group;
+    token_at(unit, min(lane & 31, tokens * p.group - 1 - unit / MS * 32), i, head);
   };
   auto fetch_unit = [&](long long at, int tokens, int unit) {
     int row, i, head;
@@ -276,12 +289,14 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
   };
   auto units_of = [&](int tokens) { return (tokens * p.group + 31) / 32 * MS; };
   auto fetch = [&](long long at, int tokens) {
+    unit = wave;
     if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
   };
-  auto results = [&](int buf, long long at, int tokens) {
+  // `most` of them
+  auto results = [&](int buf, long long at, int tokens, int most) {
     const int rows = tokens * p.group, units = units_of(tokens);
 #pragma unroll 1
-    for (int unit = wave; unit < units; unit += NW) {
+    for (int done = 0; done < most && unit < units; ++done, unit += NW) {
       int row, i, head;
       place_of(unit, tokens, row, i, head);
       const int m0 = unit % MS * MB;
@@ -289,21 +304,31 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
       if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
+      __builtin_amdgcn_sched_barrier(0);
       f32x16 o[MB];
 #pragma unroll
       for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[m][e] = 0.0f;
+      // (the parts of S are read a step ahead of the products that take them)
+      uint4 part[2][MB][2];
+      auto read_parts = [&](int s) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) part[s & 1][m][n] = *(const uint4*)(ls[OUT ? n : 0] + k_place<DP>(32 * (m0 + m) + (lane & 31), 2 * s + half));
+      };
+      read_parts(0);
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) {
+        if (s + 1 < DP / 16) read_parts(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int m = 0; m < MB; ++m) {
-          const int f = k_place<DP>(32 * (m0 + m) + (lane & 31), 2 * s + half);
-          const uint4 lo = *(const uint4*)(ls[OUT ? 1 : 0] + f), hi = *(const uint4*)(ls[0] + f);
-          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), fq[s], o[m], 0, 0, 0);
-          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), fq[s], o[m], 0, 0, 0);
-        }
-        if (s & 1) __builtin_amdgcn_sched_barrier(0);  // two steps' parts of S in registers at a time
+        for (int n = 1; n >= 0; --n)
+#pragma unroll
+          for (int m = 0; m < MB; ++m)
+            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, part[s & 1][m][n]), fq[s], o[m], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (PAIRS) {
         const float ti = lt[i], before = lp[(int)ti + 1];
@@ -320,7 +345,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
           for (int e = 0; e < 16; ++e) z[e] = 0.0f;
 #pragma unroll
           for (int s = 0; s < DP / 16; ++s) {
-            const uint4 w = *(const uint4*)(lk[buf] + k_place<DP>(lane & 31, 2 * s + half) + 32 * n * DP * 2);
+            const uint4 w = *(const uint4*)(lk[buf] + k_place<DP>(min(32 * n + (lane & 31), TILE - 1), 2 * s + half));
             z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z, 0, 0, 0);
           }
           uint32_t seen = 0;
@@ -346,7 +371,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
             const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
             for (int m = 0; m < MB; ++m) {
-              const int step = (32 * n + 16 * s) * DP * 2;
+              const int step = (32 * n + 16 * s) * VP * 2;
               s16x8 v = columns(lv[buf] + v_tr(m0 + m, 0) + step, lv[buf] + v_tr(m0 + m, 1) + step);
               if (odd) {
                 // 0 x infinity: values that are not finite count as 0, and then make the rows that see them NaN
@@ -370,26 +395,33 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
           }
         }
       }
-      if (row < rows) {
-        uint16_t* out = p.out + b * p.o_b + (at + i) * p.o_t + head * p.o_h;
+      // Lanes hold 8 bytes of a row here and there: through LDS, 32 columns at a time, they get 16 bytes each of whole pieces.
 #pragma unroll
-        for (int m = 0; m < MB; ++m)
+      for (int m = 0; m < MB; ++m) {
+        auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int d = 32 * (m0 + m) + 8 * g + 4 * half;
-            if (d < D) {
-              uint2 w;
-              w.x = bf16_pack(o[m][4 * g] * p.scale, o[m][4 * g + 1] * p.scale);
-              w.y = bf16_pack(o[m][4 * g + 2] * p.scale, o[m][4 * g + 3] * p.scale);
-              *(uint2*)(out + d) = w;
-            }
-          }
+        for (int g = 0; g < 4; ++g) {
+          uint2 w;
+          w.x = bf16_pack(o[m][4 * g] * p.scale, o[m][4 * g + 1] * p.scale);
+          w.y = bf16_pack(o[m][4 * g + 2] * p.scale, o[m][4 * g + 3] * p.scale);
+          *(uint2*)(granule(lane & 31, g) + 8 * half) = w;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int r = lane / 4 + 16 * n, rr = unit / MS * 32 + r, d = v0 + 32 * (m0 + m) + 8 * (lane & 3);
+          const uint4 w = *(const uint4*)granule(r, lane & 3);
+          int ri, rh;
+          token_at(unit, r, ri, rh);
+          if (rr < rows && d < D) *(uint4*)(p.out + b * p.o_b + (at + ri) * p.o_t + rh * p.o_h + d) = w;
+        }
+        __builtin_amdgcn_wave_barrier();
       }
     }
   };
 
   // The tiles: [at, at + valid).  Wide rounds: a tile does not cross a round's end.
-  auto tile_end = [&](long long at, long long round_end) { return (int)(min(min(at + (PAIRS ? p.tile_tokens : TILE), round_end), last) - at); };
+  auto tile_end = [&](long long at, long long round_end) { return (int)(min(min(at + p.tile_tokens, round_end), last) - at); };
   long long at = first, round_end = PAIRS ? last : first + p.per_round;
   int buf = 0, valid = 0;
   if (at < last) {
@@ -407,6 +439,8 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
   if constexpr (PAIRS && OUT) note_odd(0);
   __syncthreads();
   long long round_at = at;
+  long long due_at = at;  // wide rounds: the tokens whose results are to come from the S in LDS
+  int due = 0;
   while (at < last) {
     const long long next = at + valid;
     const bool ends = PAIRS || next == round_end || next == last;
@@ -422,7 +456,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
     if constexpr (PAIRS) {
       const int rounds = (valid + p.per_round - 1) / p.per_round;
       if constexpr (OUT) {
-        results(buf, at, valid);
+        results(buf, at, valid, INT_MAX);
         if (next < last) fetch(next, next_valid);
       }
       update(buf, valid, true, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
@@ -439,19 +473,25 @@ __global__ void __launch_bounds__(Shape<DP>::NT, DP == 64 ? 3 : 2) linear_kernel
       }
       __syncthreads();
     } else {
-      if (OUT && ends) fetch(round_at, (int)(next - round_at));
       update(buf, valid, begins, fade);
-      if (OUT && ends) share_state();
+      if constexpr (OUT) {
+        // a share of the round before's results with each tile of this one
+        const int left = (int)((min(round_end, last) - at + p.tile_tokens - 1) / p.tile_tokens), mine = (units_of(due) - unit + NW - 1) / NW;
+        if (mine > 0) results(buf, due_at, due, (mine + left - 1) / left);
+        if (ends) {
+          __syncthreads();  // S of the round before is read
+          share_state();
+          due_at = round_at, due = (int)(next - round_at);
+          fetch(due_at, due);
+        }
+      }
       sent();
       __syncthreads();
-      if (OUT && ends) {
-        results(buf, round_at, (int)(next - round_at));
-        __syncthreads();
-      }
     }
     if (!PAIRS && ends) round_at = next;
     at = next, valid = next_valid, round_end = next_end, buf ^= 1;
   }
+  if constexpr (OUT && !PAIRS) results(buf, due_at, due, INT_MAX);
   if constexpr (!OUT)
     store_state(own);
   else if (p.segments == 1 && p.state_out)
@@ -560,15 +600,16 @@ struct Plan {
 Plan plan_for(const pd_linear_attention_args* a) {
   Plan n = {};
   n.pairs = a->per_round <= NARROW;
-  n.tile_rounds = n.pairs ? TILE / a->per_round : 1;
-  n.tile_tokens = n.pairs ? n.tile_rounds * a->per_round : TILE;
+  const int tile = a->head_dim <= 64 ? 64 : Shape<128>::TILE;
+  n.tile_rounds = n.pairs ? tile / a->per_round : 1;
+  n.tile_tokens = n.pairs ? n.tile_rounds * a->per_round : tile;
   const long long rounds = ((long long)a->n + a->per_round - 1) / a->per_round, heads = std::max(1ll, (long long)a->batch * a->kv_heads);
   // Segments, to fill the card, while each holds tokens whose reading outweighs its state's (written, read twice and written by the scan).
-  const long long fill = a->head_dim <= 32 ? 4096 : a->head_dim <= 64 ? 768 : 256;
+  const long long fill = a->head_dim <= 32 ? 2048 : a->head_dim <= 64 ? 512 : 256;
   const long long most = (long long)a->n / (4 * a->head_dim < 256 ? 256 : 4 * a->head_dim);
-  long long segments = (fill + heads - 1) / heads;
+  long long segments = fill / heads;
   if (segments > most) segments = most;
-  if (segments < 1 || 2 * heads > fill) segments = 1;
+  if (segments < 1) segments = 1;
   long long each = rounds ? (rounds + segments - 1) / segments : 1;
   each = (each + n.tile_rounds - 1) / n.tile_rounds * n.tile_rounds;
   n.segment_rounds = (int)(each < INT32_MAX - 64 ? each : INT32_MAX - 64);
@@ -614,7 +655,8 @@ void launch(const Linear& p, bool pairs, hipStream_t st) {
     hipLaunchKernelGGL(linear_token_kernel<DP>, dim3(heads), dim3(256), 0, st, p);
     return;
   }
-  const dim3 grid(heads * p.segments), threads(Shape<DP>::NT);
+  const unsigned items = heads * p.segments;
+  const dim3 grid(Shape<DP>::VP == DP ? items : (items + 7) / 8 * 16), threads(Shape<DP>::NT);
   if (p.segments > 1) {
     if (pairs)
       hipLaunchKernelGGL((linear_kernel<DP, true, false>), grid, threads, 0, st, p);
