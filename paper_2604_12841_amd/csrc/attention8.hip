@@ -42,7 +42,7 @@ struct Attn8 {
   int causal, prefix_last;  // prefix - 1; INT_MIN, below every round: none
   // a score of product x and key scale s, in log2 units: s factor x, or with the cap, for u = s factor x:
   // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for |u| <= 0.35 a polynomial
-  float factor, cap_a, cap_b;
+  float factor, cap_a, cap_b, poly1, poly3, poly5;
   const uint16_t* q;
   uint16_t* out;
   long long q_b, q_t, q_h, o_b, o_t, o_h;
@@ -69,6 +69,13 @@ __device__ __forceinline__ int v8_place(int key, int g) {
   return key * DP + ((g ^ turn) << 4);
 }
 
+// V for few rows: 16 keys of 32 lanes, one granule each.
+template <int DP>
+__device__ __forceinline__ int vf_place(int key, int g) {
+  const int turn = DP == 128 ? ((key >> 1) & 3) | (key >> 2 & 4) : DP == 64 ? ((key >> 2) & 1) | (key >> 3 & 2) : (key >> 4) & 1;
+  return key * DP + ((g ^ turn) << 4);
+}
+
 // Eight codes as bf16, exactly.
 template <bool INT8>
 __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
@@ -89,6 +96,57 @@ __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
 }
 
+// A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u.
+// TIER: |u| is at most TIERS[TIER], or 2: anything.
+constexpr float TIERS[2] = {0.35f, 1.0f};
+// tanh u for |u| <= 1 is u (M1 + u^2 (M3 + ...)) within 2.1e-7 (fitted for the least largest error)
+constexpr float M1 = 0.9999961853f, M3 = -0.3332305849f, M5 = 0.1324913949f, M7 = -0.0508833490f, M9 = 0.0160305836f, M11 = -0.0028102861f;
+template <Cap CAP, int TIER>
+__device__ __forceinline__ float score8(const Attn8& p, float u, float t) {
+  if constexpr (CAP == CAP_NONE) return u + t;
+  const float w = u * u;
+  if constexpr (CAP == CAP_NEAR) {
+    if constexpr (TIER == 0) return fmaf(u, fmaf(w, fmaf(w, p.poly5, p.poly3), p.poly1), t);
+    if constexpr (TIER == 1) return fmaf(u * p.cap_b, fmaf(w, fmaf(w, fmaf(w, fmaf(w, fmaf(w, M11, M9), M7), M5), M3), M1), t);
+    return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b + t);
+  }
+  float x = u * p.cap_b * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
+  if constexpr (TIER > 0)
+    x = fabsf(u) <= 0.35f ? x : fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b);
+  return x + t;
+}
+// Calls f with the tier of a wave's largest |u|.
+template <Cap CAP, typename F>
+__device__ __forceinline__ void with_tier(float size, F&& f) {
+  if constexpr (CAP == CAP_NONE) {
+    f(std::integral_constant<int, 0>());
+  } else {
+    if (!__any(!(size <= TIERS[0])))
+      f(std::integral_constant<int, 0>());
+    else if (CAP == CAP_NEAR && !__any(!(size <= TIERS[1])))
+      f(std::integral_constant<int, 1>());
+    else
+      f(std::integral_constant<int, 2>());
+  }
+}
+// The distance's part of a score: dist < 2^10 as an fp16 number below the normal range is dist 2^-24, which the mixed
+// multiply-add takes as it is.
+__device__ __forceinline__ float near_part(uint32_t bytes, uint32_t at_bytes, float slope24, float t) {
+  return fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)__builtin_amdgcn_sad_u8(bytes, at_bytes, 0)), slope24, t);
+}
+__device__ __forceinline__ uint32_t distance(const int4 a, const int4 k) {
+  const uint32_t sign = 0x80000000u;
+  return far_add((uint32_t)a.x ^ sign, (uint32_t)k.x ^ sign, far_add((uint32_t)a.y ^ sign, (uint32_t)k.y ^ sign, far_add((uint32_t)a.z ^ sign, (uint32_t)k.z ^ sign, 0)));
+}
+// A byte mask of four keys from their bits.
+__device__ __forceinline__ uint32_t byte_mask(uint32_t bits) { return ((bits & 15) * 0x00204081u & 0x01010101u) * 255u; }
+
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+__device__ __forceinline__ i32x2 read_byte_columns(const uint8_t* f) {
+  typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)f);
+}
+
 // A tile of keys in LDS.
 template <int DP>
 struct alignas(16) KeyTile {
@@ -96,41 +154,360 @@ struct alignas(16) KeyTile {
   int4 sites[TILE];
   float ks[TILE], vs[TILE];  // scales
 };
-// What follows from them: ks factor, and site_bytes.
+// What follows from the sites and scales: ks factor, vs (0 where there is no token), and site_bytes.
 struct alignas(16) KeyNotes {
-  float f[TILE];
+  float f[TILE], v[TILE];
   uint32_t bytes[TILE];
 };
 
-// FEW: the waves share the rows and take tiles in turn.
-template <int DP, bool FEW, bool INT8, Cap CAP>
-__global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
-  constexpr int NT = FEW ? 64 : NW * 64;  // threads that stage a tile
-  constexpr int GR = DP / 16;             // granules of a row
-  constexpr int G = TILE * GR / NT > 0 ? TILE * GR / NT : 1;
-  constexpr int ROWS = FEW ? 32 : NW * 32;
-  constexpr int AHEAD = FEW ? 8 : 16;     // tiles whose sites are looked at together
-  __shared__ KeyTile<DP> tiles[FEW ? NW : 1][2];
-  __shared__ KeyNotes key_notes[FEW ? NW : 1];
-  __shared__ int lq[4][NW];
-  __shared__ int visible[FEW ? 1 : AHEAD];
-  __shared__ float2 ml[FEW ? NW : 1][32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int part = FEW ? 0 : wave;  // of the tile's staging
-  const int stid = FEW ? lane : tid;
-  KeyTile<DP>* const mine = tiles[FEW ? wave : 0];
-  KeyNotes& notes = key_notes[FEW ? wave : 0];
+// What rows of a wave (its 64 lanes) see, and how.
+struct Seen {
+  int vmin, vmax;        // volumes
+  int whole_last, last;  // the last round that all see, that some see
+  bool plain;            // all rows are there, of one volume
+  bool bytes;            // their sites' bytes give distances to keys of rounds round << 8 on
+  int round;
+  // whether some row sees a key, and whether all do (and the bytes give the distances)
+  __device__ __forceinline__ bool some(const int4 s) const { return s.w >= 0 && s.w >= vmin && s.w <= vmax && s.x <= last; }
+  __device__ __forceinline__ bool all(const int4 s, bool bias) const {
+    return plain && s.w == vmin && s.x <= whole_last && (!bias || (bytes && (s.x >> 8) == round && in_byte(s.y) && in_byte(s.z)));
+  }
+};
+__device__ __forceinline__ Seen seen_by(const Attn8& p, const int4 at) {
+  const bool there = at.w >= 0;
+  Seen s;
+  s.vmin = wave_min(there ? at.w : INT_MAX), s.vmax = wave_max(there ? at.w : -1);
+  const int tmin = wave_min(there ? at.x : INT_MAX), tmax = wave_max(there ? at.x : INT_MIN);
+  s.plain = __all(there) && s.vmin == s.vmax;
+  s.bytes = (tmin >> 8) == (tmax >> 8) && __all(!there || (in_byte(at.y) && in_byte(at.z)));
+  s.round = tmin >> 8;
+  s.whole_last = p.causal ? max(tmin, p.prefix_last) : INT_MAX, s.last = p.causal ? max(tmax, p.prefix_last) : INT_MAX;
+  return s;
+}
 
-  // Workgroups are dealt to the eight XCDs in turn.  An XCD takes RUN neighbouring items, which read the same keys, in its L2.
+// Finite slopes past 2^94 leave a row its nearest tokens alone (negative ones its farthest), as 2^94 does, whose products
+// with 2^24 and with any distance stay finite.
+__device__ __forceinline__ float slope_of(const Attn8& p, int head) {
+  float slope = p.slopes ? p.slopes[head] : 0.0f;
+  if (fabsf(slope) < INFINITY) slope = fminf(fmaxf(slope * -LOG2E, -0x1p94f), 0x1p94f);
+  return slope;
+}
+
+struct Item {
+  int row_tile, split, kvh, b;
+};
+// Workgroups are dealt to the eight XCDs in turn.  An XCD takes RUN neighbouring items, which read the same keys, in its L2.
+__device__ __forceinline__ bool item_of(const Attn8& p, Item& i) {
   unsigned item = ((blockIdx.x >> 3) / RUN * 8 + (blockIdx.x & 7)) * RUN + (blockIdx.x >> 3) % RUN;
-  if (item >= p.items) return;
-  const int row_tile = (int)(item % p.row_tiles);
+  if (item >= p.items) return false;
+  i.row_tile = (int)(item % p.row_tiles);
   item /= p.row_tiles;
-  const int split = item % p.splits;
+  i.split = item % p.splits;
   item /= p.splits;
-  const int kvh = item % p.kv_heads, b = item / p.kv_heads;
+  i.kvh = item % p.kv_heads, i.b = item / p.kv_heads;
+  return true;
+}
 
-  const int row = row_tile * ROWS + (FEW ? 0 : wave * 32) + (lane & 31);
+__device__ __forceinline__ float inverse(float total) { return total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN; }
+
+// Few rows: 16 a workgroup, all of them in each of its waves, which take tiles in turn.  A lane of group g of 16 holds
+// keys 16 n + 4 g + {0 .. 3} of row lane & 15.  K comes straight into registers, a tile ahead.
+template <int DP, bool INT8, Cap CAP>
+__global__ void __launch_bounds__(NW * 64, 2) attention8_few_kernel(const Attn8 p) {
+  constexpr int GR = DP / 16;                    // granules of a row
+  constexpr int KG = DP > 64 ? 2 : 1;            // granules of K that a lane takes of a key (32 channels: half of one)
+  constexpr int STEPS = DP / 32;                 // of a product over the channels
+  constexpr int AHEAD = 8;                       // tiles whose sites are looked at together
+  __shared__ __attribute__((aligned(16))) uint8_t lv[NW][2][TILE * DP];
+  __shared__ KeyNotes key_notes[NW];
+  __shared__ float2 ml[NW][16];
+  static_assert(2 * TILE * DP >= 16 * DP * 4, "a wave's result fits its tiles");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g4 = lane >> 4;
+  KeyNotes& notes = key_notes[wave];
+  Item item;
+  if (!item_of(p, item)) return;
+  const int kvh = item.kvh, b = item.b;
+  const long long k_row = ((long long)(b * 2) * p.kv_heads + kvh) * p.capacity, v_row = k_row + (long long)p.kv_heads * p.capacity;
+  const uint8_t* kb = p.codes + k_row * p.head_dim;
+  const uint8_t* vb = p.codes + v_row * p.head_dim;
+  const int4* sites = p.sites + (long long)b * p.capacity;
+
+  // A tile's K, V, sites and scales.  Keys past the end repeat the last.
+  uint4 key[4][KG];
+  int4 site;
+  float ks, vs;
+  auto load_v = [&](int buf, int tile) {
+    const int k0 = tile * TILE, most_key = p.capacity - 1 - k0;
+#pragma unroll
+    for (int n = 0; n < GR; ++n) {
+      const int slot = lane + n * 64, of = slot / GR, vg = slot % GR ^ (vf_place<DP>(of, 0) >> 4) % GR;
+      // (past head_dim the row's last granule: its results are not stored)
+      send16(vb + (long long)(k0 + min(of, most_key)) * p.head_dim + min(16 * vg, p.head_dim - 16), lv[wave][buf] + n * 1024);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto load_k = [&](int tile) {
+    const int k0 = tile * TILE, most_key = p.capacity - 1 - k0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint8_t* from = kb + (long long)(k0 + min(16 * n + c, most_key)) * p.head_dim;
+#pragma unroll
+      for (int j = 0; j < KG; ++j) {
+        if constexpr (DP == 32) {
+          const uint2 w = *(const uint2*)(from + min(8 * g4, p.head_dim - 8));
+          key[n][j].x = w.x, key[n][j].y = w.y;
+        } else {
+          key[n][j] = *(const uint4*)(from + min(16 * (g4 + 4 * j), p.head_dim - 16));  // (past head_dim q is 0)
+        }
+      }
+    }
+    const int at = k0 + min(lane, most_key);
+    site = sites[at], ks = p.scales[k_row + at], vs = p.scales[v_row + at];
+  };
+  const int begin = item.split * p.tiles_per_split + wave, end = min(p.tiles, (item.split + 1) * p.tiles_per_split);
+  // the first tile is sent for before it is known whether a row sees it
+  if (begin < end) {
+    load_v(0, begin);
+    load_k(begin);
+  }
+
+  const int row = item.row_tile * 16 + c;
+  const int r = row < p.rows ? row : p.rows - 1;  // rows past the end repeat the last: not stored
+  const int token = r / p.group, head = kvh * p.group + r % p.group;
+  const uint16_t* q = p.q + b * p.q_b + token * p.q_t + head * p.q_h;
+  bf16x8 fq[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int d = DP == 32 ? 8 * g4 : 16 * (g4 + 4 * (s >> 1)) + 8 * (s & 1);
+    const uint4 w = *(const uint4*)(q + min(d, p.head_dim - 8));
+    fq[s] = __builtin_bit_cast(bf16x8, d < p.head_dim ? w : make_uint4(0, 0, 0, 0));
+  }
+  const int4 at = p.q_sites[b * p.q_sites_b + token];
+  const int own_volume = at.w >= 0 ? at.w : -2;  // -2: no key's volume
+  const int last = p.causal ? max(at.x, p.prefix_last) : INT_MAX;
+  const uint32_t at_bytes = site_bytes(at);
+  const bool bias = p.slopes != nullptr;
+  const float slope = slope_of(p, head);
+  const Seen seen = seen_by(p, at);
+
+  // the tiles to visit, as a mask over the next AHEAD of this wave's
+  int base = begin - AHEAD * NW;
+  uint32_t mask = 0;
+  auto next_tile = [&]() -> int {  // -1: no more
+    while (mask == 0) {
+      base += AHEAD * NW;
+      if (base >= end) return -1;
+      int4 s[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) {
+        const int k = min((base + n * NW) * TILE + lane, p.capacity - 1);
+        s[n] = sites[base + n * NW < end ? k : 0];
+      }
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) {
+        const int tile = base + n * NW;
+        mask |= __any(tile < end && tile * TILE + lane < p.capacity && seen.some(s[n])) ? 1u << n : 0u;
+      }
+    }
+    const int bit = __builtin_ctz(mask);
+    mask &= mask - 1;
+    return base + bit * NW;
+  };
+
+  typedef __attribute__((ext_vector_type(4))) float f32x4;
+  f32x4 o[DP / 16];
+#pragma unroll
+  for (int m = 0; m < DP / 16; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // scores are taken relative to `top`, the row's reference: set by the first tile that it sees, raised when a score
+  // exceeds it by 8 (the sums then stay below 2^8 times their number)
+  float top = 0.0f, total = 0.0f;
+  bool unset = true;
+  // keys 32 s + 4 g4 + {0 .. 3} and 16 more of 16 columns
+  const int v_key = 4 * g4 + ((lane >> 1) & 3) + 16 * ((lane >> 3) & 1);
+  const int v_off = vf_place<DP>(v_key, 0), v_byte = (lane & 1) * 8;
+
+  int tile = next_tile(), buf = 0;
+  if (tile >= 0 && tile != begin) {
+    buf = 1;
+    load_v(buf, tile);
+    load_k(tile);
+  }
+  while (tile >= 0) {
+    // what the tile's keys are to the rows: a lane a key
+    const bool held = tile * TILE + lane < p.capacity && site.w >= 0;
+    const uint64_t tokens = __ballot(held);
+    const bool whole = __all(held && seen.all(site, bias));
+    const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
+    notes.f[lane] = ks * p.factor;
+    notes.v[lane] = held ? vs : 0.0f;
+    notes.bytes[lane] = site_bytes(site);
+    const int4 of_lane = site;
+    __builtin_amdgcn_wave_barrier();
+    f32x4 z[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      z[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const uint4 w = key[n][s >> 1];
+        z[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s & 1 ? decode<INT8>(w.z, w.w) : decode<INT8>(w.x, w.y), fq[s], z[n], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // V has landed: it was sent for before this K, which is used.  The next tile's sends come after that wait.
+    const int after = next_tile();
+    if (after >= 0) {
+      load_v(buf ^ 1, after);
+      load_k(after);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    float size = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const float4 f = *(const float4*)&notes.f[16 * n + 4 * g4];
+      z[n][0] *= f.x, z[n][1] *= f.y, z[n][2] *= f.z, z[n][3] *= f.w;
+      size = fmaxf(fmaxf(fmaxf(size, fabsf(z[n][0])), fmaxf(fabsf(z[n][1]), fabsf(z[n][2]))), fabsf(z[n][3]));
+    }
+    float most = -INFINITY;
+    if (whole) {
+      with_tier<CAP>(size, [&](auto tier) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const uint4 w = *(const uint4*)&notes.bytes[16 * n + 4 * g4];
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[n][e] = score8<CAP, decltype(tier)::value>(p, z[n][e], near_part(u[e], at_bytes, slope * 0x1p24f, -top));
+            most = fmaxf(most, z[n][e]);
+          }
+        }
+      });
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at_key = 16 * n + 4 * g4 + e;
+          const int4 k = make_int4(__shfl(of_lane.x, at_key), __shfl(of_lane.y, at_key), __shfl(of_lane.z, at_key), __shfl(of_lane.w, at_key));
+          const bool in = tokens >> at_key & 1 && k.w == own_volume && k.x <= last;
+          const float x = score8<CAP, 2>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
+          z[n][e] = in ? x : -INFINITY;
+          most = fmaxf(most, z[n][e]);
+        }
+    }
+    if (__any(most > 8.0f || (unset && most > -INFINITY))) {
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const bool raise = most > 8.0f || (unset && most > -INFINITY);
+      const float up = raise ? most : 0.0f;
+      const float alpha = raise && !unset ? __builtin_amdgcn_exp2f(-up) : 1.0f;
+      if (raise) unset = false;
+      top += up;
+      total *= alpha;
+#pragma unroll
+      for (int m = 0; m < DP / 16; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[m][e] *= alpha;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[n][e] -= up;
+    }
+    // probabilities, times the value's scale, in bf16; and their product with the codes
+    auto finish = [&](auto carefully) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint32_t u[4], keep[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const float4 f4 = *(const float4*)&notes.v[32 * s + 16 * n + 4 * g4];
+          const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float y = z[2 * s + n][e], e2 = __builtin_amdgcn_exp2f(y);
+            total += e2;
+            x[e] = e2 * f[e];
+            if constexpr (carefully.value) x[e] = y == -INFINITY ? 0.0f : x[e];  // (an invisible row's scale may be anything)
+          }
+          u[2 * n] = bf16_pack(x[0], x[1]), u[2 * n + 1] = bf16_pack(x[2], x[3]);
+          // codes at places without a token may be E4M3's NaN
+          if constexpr (carefully.value) keep[n] = byte_mask((uint32_t)(tokens >> (32 * s + 16 * n + 4 * g4)));
+        }
+        const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+#pragma unroll
+        for (int m = 0; m < DP / 16; ++m) {
+          i32x2 w = read_byte_columns(lv[wave][buf] + (v_off ^ m << 4) + v_byte + 32 * s * DP);
+          if constexpr (carefully.value) w[0] &= keep[0], w[1] &= keep[1];
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode<INT8>((uint32_t)w[0], (uint32_t)w[1]), pr, o[m], 0, 0, 0);
+        }
+      }
+    };
+    if (careful)
+      finish(std::true_type());
+    else
+      finish(std::false_type());
+    tile = after, buf ^= 1;
+  }
+
+  total += __shfl_xor(total, 16);
+  total += __shfl_xor(total, 32);
+  const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
+  // join the four waves, through the tiles' memory (what was sent for and not used has to be in before)
+  sent();
+  if (g4 == 0) ml[wave][c] = make_float2(none ? -INFINITY : top, total);
+#pragma unroll
+  for (int m = 0; m < DP / 16; ++m)
+    *(float4*)((float*)lv[wave] + c * DP + 16 * m + 4 * g4) = make_float4(o[m][0], o[m][1], o[m][2], o[m][3]);
+  __syncthreads();
+  const long long rows_at = (((long long)item.split * p.batch + b) * p.kv_heads + kvh) * p.rows;
+  const int rows_here = min(16, p.rows - item.row_tile * 16);
+  for (int x = tid; x < rows_here * (DP / 4); x += NW * 64) {
+    const int i = x / (DP / 4), d = x % (DP / 4) * 4;
+    float best = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) best = fmaxf(best, ml[w][i].x);
+    float4 acc = make_float4(0, 0, 0, 0);
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float2 of = ml[w][i];
+      if (of.x == -INFINITY) continue;  // the row saw nothing there
+      const float weight = __builtin_amdgcn_exp2f(of.x - best);
+      const float4 v = *(const float4*)((const float*)lv[w] + i * DP + d);
+      acc.x = fmaf(v.x, weight, acc.x), acc.y = fmaf(v.y, weight, acc.y), acc.z = fmaf(v.z, weight, acc.z), acc.w = fmaf(v.w, weight, acc.w);
+      sum = fmaf(of.y, weight, sum);
+    }
+    const int rr = item.row_tile * 16 + i;
+    if (p.splits > 1) {
+      *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;
+      if (d == 0) p.part_ml[rows_at + rr] = make_float2(best, sum);
+    } else if (d < p.head_dim) {
+      const float inv = inverse(sum);
+      uint2 w;
+      w.x = bf16_pack(acc.x * inv, acc.y * inv), w.y = bf16_pack(acc.z * inv, acc.w * inv);
+      *(uint2*)(p.out + b * p.o_b + rr / p.group * p.o_t + (kvh * p.group + rr % p.group) * p.o_h + d) = w;
+    }
+  }
+}
+
+// Many rows: 32 a wave, 128 a workgroup, whose waves share the tiles.
+template <int DP, bool INT8, Cap CAP>
+__global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
+  constexpr int NT = NW * 64;
+  constexpr int GR = DP / 16;  // granules of a row
+  constexpr int AHEAD = 16;    // tiles whose sites are looked at together
+  __shared__ KeyTile<DP> tiles[2];
+  __shared__ KeyNotes notes;
+  __shared__ int lq[3][NW];
+  __shared__ int visible[AHEAD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  Item item;
+  if (!item_of(p, item)) return;
+  const int kvh = item.kvh, b = item.b;
+  const int row = item.row_tile * 128 + wave * 32 + (lane & 31);
   const int r = row < p.rows ? row : p.rows - 1;  // rows past the end repeat the last: not stored
   const int token = r / p.group, head = kvh * p.group + r % p.group;
   const uint16_t* q = p.q + b * p.q_b + token * p.q_t + head * p.q_h;
@@ -147,90 +524,62 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
     fq[s] = __builtin_bit_cast(bf16x8, w);
   }
   const int4 at = p.q_sites[b * p.q_sites_b + token];
-  const bool there = at.w >= 0;
-  const int own_volume = there ? at.w : -2;  // -2: no key's volume
+  const int own_volume = at.w >= 0 ? at.w : -2;                    // -2: no key's volume
   const int last = p.causal ? max(at.x, p.prefix_last) : INT_MAX;  // the last round that the row sees
   const uint32_t at_bytes = site_bytes(at);
-  // Finite slopes past 2^94 leave a row its nearest tokens alone (negative ones its farthest), as 2^94 does, whose products
-  // with 2^24 (below) and with any distance stay finite.
   const bool bias = p.slopes != nullptr;
-  float slope = bias ? p.slopes[head] : 0.0f;
-  if (fabsf(slope) < INFINITY) slope = fminf(fmaxf(slope * -LOG2E, -0x1p94f), 0x1p94f);
+  const float slope = slope_of(p, head);
 
   // what this wave's rows see, and the workgroup's
-  const int wv_min = wave_min(there ? at.w : INT_MAX), wv_max = wave_max(there ? at.w : -1);
-  const int wt_min = wave_min(there ? at.x : INT_MAX), wt_max = wave_max(there ? at.x : INT_MIN);
-  const bool w_plain = __all(there) && wv_min == wv_max;
-  const bool w_bytes = (wt_min >> 8) == (wt_max >> 8) && __all(!there || (in_byte(at.y) && in_byte(at.z)));
-  const int w_whole_last = p.causal ? max(wt_min, p.prefix_last) : INT_MAX, w_last = p.causal ? max(wt_max, p.prefix_last) : INT_MAX;
-  int gv_min = wv_min, gv_max = wv_max, g_last = w_last;
-  if constexpr (!FEW) {
-    if (lane == 0) lq[0][wave] = wv_min, lq[1][wave] = wv_max, lq[2][wave] = w_last;
-    __syncthreads();
+  const Seen seen = seen_by(p, at);
+  Seen any = seen;
+  if (lane == 0) lq[0][wave] = seen.vmin, lq[1][wave] = seen.vmax, lq[2][wave] = seen.last;
+  __syncthreads();
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      gv_min = min(gv_min, lq[0][w]);
-      gv_max = max(gv_max, lq[1][w]);
-      g_last = max(g_last, lq[2][w]);
-    }
-    gv_min = __builtin_amdgcn_readfirstlane(gv_min);
-    gv_max = __builtin_amdgcn_readfirstlane(gv_max);
-    g_last = __builtin_amdgcn_readfirstlane(g_last);
-  }
+  for (int w = 0; w < NW; ++w) any.vmin = min(any.vmin, lq[0][w]), any.vmax = max(any.vmax, lq[1][w]), any.last = max(any.last, lq[2][w]);
 
-  // The tiles to visit, as a mask over the next AHEAD of this wave's (workgroup's) tiles.
-  const int begin = split * p.tiles_per_split + (FEW ? wave : 0), end = min(p.tiles, (split + 1) * p.tiles_per_split);
-  constexpr int STRIDE = FEW ? NW : 1;
-  int base = begin - AHEAD * STRIDE;
+  // The tiles to visit, as a mask over the next AHEAD.
+  const int begin = item.split * p.tiles_per_split, end = min(p.tiles, (item.split + 1) * p.tiles_per_split);
+  int base = begin - AHEAD;
   uint32_t mask = 0;
-  auto site_at = [&](int key) { return key < p.capacity ? sites[key] : make_int4(0, 0, 0, -1); };
-  auto sees = [&](const int4 s) { return s.w >= 0 && s.w >= gv_min && s.w <= gv_max && s.x <= g_last; };
   auto next_tile = [&]() -> int {  // -1: no more
     while (mask == 0) {
-      base += AHEAD * STRIDE;
+      base += AHEAD;
       if (base >= end) return -1;
-      if constexpr (FEW) {
-        int4 s[AHEAD];
+      int4 s[AHEAD / NW];
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) s[n] = base + n * STRIDE < end ? site_at((base + n * STRIDE) * TILE + lane) : make_int4(0, 0, 0, -1);
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) mask |= __any(sees(s[n])) ? 1u << n : 0u;
-      } else {
-        int4 s[AHEAD / NW];
-#pragma unroll
-        for (int n = 0; n < AHEAD / NW; ++n) {
-          const int tile = base + wave + n * NW;
-          s[n] = tile < end ? site_at(tile * TILE + lane) : make_int4(0, 0, 0, -1);
-        }
-        __syncthreads();  // the last mask is read
-#pragma unroll
-        for (int n = 0; n < AHEAD / NW; ++n) {
-          const bool any = __any(sees(s[n]));
-          if (lane == 0) visible[wave + n * NW] = any;
-        }
-        __syncthreads();
-        mask = (uint32_t)__ballot(lane < AHEAD && visible[lane & (AHEAD - 1)]);
+      for (int n = 0; n < AHEAD / NW; ++n) {
+        const int key = (base + wave + n * NW) * TILE + lane;
+        s[n] = base + wave + n * NW < end && key < p.capacity ? sites[key] : make_int4(0, 0, 0, -1);
       }
+      __syncthreads();  // the last mask is read
+#pragma unroll
+      for (int n = 0; n < AHEAD / NW; ++n) {
+        const bool some = __any(any.some(s[n]));
+        if (lane == 0) visible[wave + n * NW] = some;
+      }
+      __syncthreads();
+      mask = (uint32_t)__ballot(lane < AHEAD && visible[lane & (AHEAD - 1)]);
     }
     const int bit = __builtin_ctz(mask);
     mask &= mask - 1;
-    return base + bit * STRIDE;
+    return base + bit;
   };
 
   // columns past head_dim stay the zeros that they are set to here
   if (p.head_dim < DP) {
-    for (int c = stid; c < TILE * GR; c += NT)
+    for (int c = tid; c < TILE * GR; c += NT)
 #pragma unroll
-      for (int n = 0; n < 2; ++n) *(uint4*)(mine[n].k + c * 16) = *(uint4*)(mine[n].v + c * 16) = make_uint4(0, 0, 0, 0);
-    if constexpr (!FEW) __syncthreads();
+      for (int n = 0; n < 2; ++n) *(uint4*)(tiles[n].k + c * 16) = *(uint4*)(tiles[n].v + c * 16) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
   }
-  // Staging, straight into LDS: granule slots stid + n NT.  Keys past the end repeat the last.
+  // Staging, straight into LDS: granule slots tid + n NT.  Keys past the end repeat the last.
   auto load_tile = [&](KeyTile<DP>& t, int tile) {
     const int k0 = tile * TILE, most_key = p.capacity - 1 - k0;
 #pragma unroll
-    for (int n = 0; n < G; ++n) {
-      const int slot = stid + n * NT, first = (n * NT + part * 64) * 16;
-      if (TILE * GR < NT && part * 64 >= TILE * GR) break;  // (32 channels in four waves: two of them)
+    for (int n = 0; n < (TILE * GR + NT - 1) / NT; ++n) {
+      const int slot = tid + n * NT, first = (n * NT + wave * 64) * 16;
+      if (n * NT + wave * 64 >= TILE * GR) break;  // (32 channels: two waves' worth)
       const int key = slot / GR, pos = slot % GR;
       const int kg = pos ^ (k8_place<DP>(key, 0) >> 4) % GR, vg = pos ^ (v8_place<DP>(key, 0) >> 4) % GR;
       const long long from = (long long)(k0 + min(key, most_key)) * p.head_dim;
@@ -238,9 +587,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
       if (16 * vg < p.head_dim) send16(vb + from + 16 * vg, t.v + first);
     }
     const int key = k0 + min(lane, most_key);
-    if (FEW || wave == 0) send16(sites + key, t.sites);
-    if (FEW || wave == 1) send4at(p.scales + k_row + key, t.ks);
-    if (FEW || wave == 2) send4at(p.scales + v_row + key, t.vs);
+    if (wave == 0) send16(sites + key, t.sites);
+    if (wave == 1) send4at(p.scales + k_row + key, t.ks);
+    if (wave == 2) send4at(p.scales + v_row + key, t.vs);
   };
 
   f32x16 o[DP / 32];
@@ -248,9 +597,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   for (int n = 0; n < DP / 32; ++n)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[n][e] = 0.0f;
-  // scores are taken relative to `top`, the row's reference: set by the first tile that it sees, raised when a score
-  // exceeds it by 8 (the sums then stay below 2^8 times their number)
-  float top = 0.0f, total = 0.0f;
+  float top = 0.0f, total = 0.0f;  // as in the kernel for few rows
   bool unset = true;
 
   // LDS places of this lane's operands
@@ -264,17 +611,17 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
 
   auto work = [&](KeyTile<DP>& t, int tile) {
     // what the tile's keys are to this wave's rows: a lane a key
-    const int4 s = t.sites[lane];
-    const bool held = tile * TILE + lane < p.capacity && s.w >= 0;
+    const int4 site = t.sites[lane];
+    const bool held = tile * TILE + lane < p.capacity && site.w >= 0;
+    const float vs = t.vs[lane];
     const uint64_t tokens = __ballot(held);
-    if (!__any(held && s.w >= wv_min && s.w <= wv_max && s.x <= w_last)) return;
-    // every row sees every key, and the bytes give the distances
-    const bool whole = w_plain && __all(held && s.w == wv_min && s.x <= w_whole_last &&
-                                        (!bias || ((s.x >> 8) == (wt_min >> 8) && in_byte(s.y) && in_byte(s.z)))) &&
-                       (!bias || w_bytes);
-    // (the waves that share a tile write the same)
+    const bool whole = __all(held && seen.all(site, bias));
+    if (!__any(held && seen.some(site))) return;
+    const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
+    // (the waves write the same)
     notes.f[lane] = t.ks[lane] * p.factor;
-    notes.bytes[lane] = site_bytes(s);
+    notes.v[lane] = held ? vs : 0.0f;
+    notes.bytes[lane] = site_bytes(site);
     __builtin_amdgcn_wave_barrier();
 
     f32x16 z[2];
@@ -289,72 +636,42 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
         z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>(w.z, w.w), fq[2 * c + 1], z[n], 0, 0, 0);
       }
     }
-    // times the key's scale; whether one of the wave's exceeds 0.35 of the cap
     float size = 0.0f;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 f4 = *(const float4*)&notes.f[32 * n + 8 * g + 4 * half];
-        const float f[4] = {f4.x, f4.y, f4.z, f4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          z[n][4 * g + e] *= f[e];
-          if constexpr (CAP != CAP_NONE) size = fmaxf(size, fabsf(z[n][4 * g + e]));
+        const float4 f = *(const float4*)&notes.f[32 * n + 8 * g + 4 * half];
+        z[n][4 * g] *= f.x, z[n][4 * g + 1] *= f.y, z[n][4 * g + 2] *= f.z, z[n][4 * g + 3] *= f.w;
+        if constexpr (CAP != CAP_NONE) {
+          size = fmaxf(fmaxf(size, fabsf(z[n][4 * g])), fabsf(z[n][4 * g + 1]));
+          size = fmaxf(fmaxf(size, fabsf(z[n][4 * g + 2])), fabsf(z[n][4 * g + 3]));
         }
       }
-    if constexpr (CAP != CAP_NONE) {
-      const bool large = __any(!(size <= 0.35f));
-      auto capped = [&](auto some_large) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float u = z[n][e], w = u * u;
-            if constexpr (CAP == CAP_NEAR) {
-              if constexpr (some_large.value)
-                z[n][e] = fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b);
-              else
-                z[n][e] = u * p.cap_b * fmaf(w, fmaf(w, TANH5, TANH3), TANH1);
-            } else {
-              float x = u * p.cap_b * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
-              if constexpr (some_large.value)
-                x = fabsf(u) <= 0.35f ? x : fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b);
-              z[n][e] = x;
-            }
-          }
-      };
-      if (large)
-        capped(std::true_type());
-      else
-        capped(std::false_type());
-    }
     float most = -INFINITY;
     if (whole) {
-      if (bias) {
+      with_tier<CAP>(size, [&](auto tier) {
+        auto scores = [&](auto biased) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint4 w = *(const uint4*)&notes.bytes[32 * n + 8 * g + 4 * half];
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            for (int g = 0; g < 4; ++g) {
+              uint4 w = make_uint4(0, 0, 0, 0);
+              if constexpr (biased.value) w = *(const uint4*)&notes.bytes[32 * n + 8 * g + 4 * half];
+              const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // dist < 2^10 as an fp16 number below the normal range is dist 2^-24: the mixed multiply-add takes it as it is
-              const uint32_t dist = __builtin_amdgcn_sad_u8(u[e], at_bytes, 0);
-              z[n][4 * g + e] += fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)dist), slope * 0x1p24f, -top);
-              most = fmaxf(most, z[n][4 * g + e]);
+              for (int e = 0; e < 4; ++e) {
+                const float part = biased.value ? near_part(u[e], at_bytes, slope * 0x1p24f, -top) : -top;
+                z[n][4 * g + e] = score8<CAP, decltype(tier)::value>(p, z[n][4 * g + e], part);
+                most = fmaxf(most, z[n][4 * g + e]);
+              }
             }
-          }
-      } else {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            z[n][e] -= top;
-            most = fmaxf(most, z[n][e]);
-          }
-      }
+        };
+        if (bias)
+          scores(std::true_type());
+        else
+          scores(std::false_type());
+      });
     } else {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -362,11 +679,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
         for (int e = 0; e < 16; ++e) {
           const int key = 32 * n + 8 * (e >> 2) + 4 * half + (e & 3);
           const int4 k = t.sites[key];
-          const uint32_t sign = 0x80000000u;
-          const uint32_t dist = far_add((uint32_t)at.x ^ sign, (uint32_t)k.x ^ sign,
-                                        far_add((uint32_t)at.y ^ sign, (uint32_t)k.y ^ sign, far_add((uint32_t)at.z ^ sign, (uint32_t)k.z ^ sign, 0)));
-          const bool seen = tokens >> key & 1 && k.w == own_volume && k.x <= last;
-          z[n][e] = seen ? z[n][e] + (bias ? fmaf((float)dist, slope, -top) : -top) : -INFINITY;
+          const bool in = tokens >> key & 1 && k.w == own_volume && k.x <= last;
+          const float x = score8<CAP, 2>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
+          z[n][e] = in ? x : -INFINITY;
           most = fmaxf(most, z[n][e]);
           if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four keys' sites in registers at a time
         }
@@ -388,111 +703,61 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[n][e] -= up;
     }
-    // probabilities; times the value's scale, in bf16: keys 16 s + 4 half + {0 .. 3, 8 .. 11} of block n
-    uint4 pr[2][2];
+    // probabilities, times the value's scale, in bf16: keys 16 s + 4 half + {0 .. 3, 8 .. 11}; and their product with the codes
+    auto finish = [&](auto carefully) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        uint32_t u[4];
+      for (int s = 0; s < 4; ++s) {
+        uint32_t u[4], keep[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const float4 f4 = *(const float4*)&t.vs[32 * n + 16 * s2 + 8 * g + 4 * half];
+          const float4 f4 = *(const float4*)&notes.v[16 * s + 8 * g + 4 * half];
           const float f[4] = {f4.x, f4.y, f4.z, f4.w};
           float x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float y = z[n][8 * s2 + 4 * g + e], e2 = __builtin_amdgcn_exp2f(y);
+            const float y = z[s >> 1][8 * (s & 1) + 4 * g + e], e2 = __builtin_amdgcn_exp2f(y);
             total += e2;
             x[e] = e2 * f[e];
-            if (!whole) x[e] = y == -INFINITY ? 0.0f : x[e];  // (an invisible row's scale may be anything)
+            if constexpr (carefully.value) x[e] = y == -INFINITY ? 0.0f : x[e];  // (an invisible row's scale may be anything)
           }
           u[2 * g] = bf16_pack(x[0], x[1]), u[2 * g + 1] = bf16_pack(x[2], x[3]);
+          // codes at places without a token may be E4M3's NaN
+          if constexpr (carefully.value) keep[g] = byte_mask((uint32_t)(tokens >> (16 * s + 8 * g + 4 * half)));
         }
-        pr[n][s2] = make_uint4(u[0], u[1], u[2], u[3]);
-      }
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        typedef __attribute__((ext_vector_type(2))) int i32x2;
-        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-        uint32_t keep[2] = {~0u, ~0u};
-        if (!whole) {  // codes at places without a token may be E4M3's NaN
-          const uint32_t bits = (uint32_t)(tokens >> (32 * n + 16 * s2 + 4 * half));
-          keep[0] = ((bits & 15) * 0x00204081u & 0x01010101u) * 255u;
-          keep[1] = ((bits >> 8 & 15) * 0x00204081u & 0x01010101u) * 255u;
-        }
+        const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
 #pragma unroll
         for (int m = 0; m < DP / 32; ++m) {
-          const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(t.v + v_off[m] + (32 * n + 16 * s2) * DP));
-          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>((uint32_t)w[0] & keep[0], (uint32_t)w[1] & keep[1]),
-                                                         __builtin_bit_cast(bf16x8, pr[n][s2]), o[m], 0, 0, 0);
+          i32x2 w = read_byte_columns(t.v + v_off[m] + 16 * s * DP);
+          if constexpr (carefully.value) w[0] &= keep[0], w[1] &= keep[1];
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>((uint32_t)w[0], (uint32_t)w[1]), pr, o[m], 0, 0, 0);
         }
       }
+    };
+    if (careful)
+      finish(std::true_type());
+    else
+      finish(std::false_type());
   };
 
   int tile = next_tile(), buf = 0;
-  if (tile >= 0) load_tile(mine[0], tile);
+  if (tile >= 0) load_tile(tiles[0], tile);
   sent();
-  if constexpr (!FEW) __syncthreads();
+  __syncthreads();
   while (tile >= 0) {
     const int after = next_tile();
-    if (after >= 0) load_tile(mine[buf ^ 1], after);
+    if (after >= 0) load_tile(tiles[buf ^ 1], after);
     __builtin_amdgcn_sched_barrier(0);
-    work(mine[buf], tile);
+    work(tiles[buf], tile);
     sent();
-    if constexpr (!FEW) __syncthreads();
+    __syncthreads();
     tile = after, buf ^= 1;
   }
 
   total += __shfl_xor(total, 32);
-  bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
-  const long long rows_at = (((long long)split * p.batch + b) * p.kv_heads + kvh) * p.rows;
-  if constexpr (FEW) {
-    // join the four waves: their results through the tiles' memory, 16 columns of every wave's at a time
-    if (half == 0) ml[wave][lane & 31] = make_float2(none ? -INFINITY : top, total);
-    float* const lo = (float*)mine;  // [row][DP]
-    static_assert(sizeof(KeyTile<DP>) * 2 >= 32 * DP * 4, "a wave's result fits its tiles");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int m = 0; m < DP / 32; ++m)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(float4*)(lo + (lane & 31) * DP + 32 * m + 8 * g + 4 * half) = make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
-    __syncthreads();
-    const int rows_here = min(32, p.rows - row_tile * 32);
-    for (int c = tid; c < rows_here * (DP / 4); c += NW * 64) {
-      const int i = c / (DP / 4), d = c % (DP / 4) * 4;
-      float best = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) best = fmaxf(best, ml[w][i].x);
-      float4 acc = make_float4(0, 0, 0, 0);
-      float sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float2 of = ml[w][i];
-        if (of.x == -INFINITY) continue;  // the row saw nothing there
-        const float weight = __builtin_amdgcn_exp2f(of.x - best);
-        const float4 v = *(const float4*)((const float*)tiles[FEW ? w : 0] + i * DP + d);
-        acc.x = fmaf(v.x, weight, acc.x), acc.y = fmaf(v.y, weight, acc.y), acc.z = fmaf(v.z, weight, acc.z), acc.w = fmaf(v.w, weight, acc.w);
-        sum = fmaf(of.y, weight, sum);
-      }
-      const int rr = row_tile * 32 + i;
-      if (p.splits > 1) {
-        *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;
-        if (d == 0) p.part_ml[rows_at + rr] = make_float2(best, sum);
-      } else if (d < p.head_dim) {
-        const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : NAN;
-        uint2 w;
-        w.x = bf16_pack(acc.x * inv, acc.y * inv), w.y = bf16_pack(acc.z * inv, acc.w * inv);
-        *(uint2*)(p.out + b * p.o_b + rr / p.group * p.o_t + (kvh * p.group + rr % p.group) * p.o_h + d) = w;
-      }
-    }
-    return;
-  }
   if (row >= p.rows) return;
   if (p.splits > 1) {
+    const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
+    const long long rows_at = (((long long)item.split * p.batch + b) * p.kv_heads + kvh) * p.rows;
 #pragma unroll
     for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
@@ -501,7 +766,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
     if (half == 0) p.part_ml[rows_at + row] = make_float2(none ? -INFINITY : top, total);
     return;
   }
-  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
+  const float inv = inverse(total);
   uint16_t* out = p.out + b * p.o_b + token * p.o_t + head * p.o_h;
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m)
@@ -558,7 +823,7 @@ __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
     const float4 o = so[n][lane];
     acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
   }
-  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : NAN;
+  const float inv = inverse(total);
   uint2 v;
   v.x = bf16_pack(acc.x * inv, acc.y * inv), v.y = bf16_pack(acc.z * inv, acc.w * inv);
   *(uint2*)(p.out + b * p.o_b + row / p.group * p.o_t + (kvh * p.group + row % p.group) * p.o_h + 4 * lane) = v;
@@ -577,11 +842,11 @@ Plan plan_for(const pd_attention8_args* a) {
   Plan n = {};
   const long long rows = (long long)a->n_q * (a->heads / c.kv_heads), heads = (long long)c.kv_heads * c.batch;
   n.few = rows <= 64;
-  n.row_tiles = (int)((rows + (n.few ? 31 : 127)) / (n.few ? 32 : 128));
+  n.row_tiles = (int)((rows + (n.few ? 15 : 127)) / (n.few ? 16 : 128));
   n.tiles = (int)(((long long)c.capacity + TILE - 1) / TILE);
   const int dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   // Splits: to fill the card, down to 8 tiles each
-  const long long whole = n.row_tiles * heads, fill = n.few ? (dp == 128 ? 256 : 512) : 512;
+  const long long whole = n.row_tiles * heads, fill = 512;
   long long splits = (fill + whole - 1) / whole;
   if (splits > n.tiles / 8) splits = n.tiles / 8;
   if (splits > MOST_SPLITS) splits = MOST_SPLITS;
@@ -631,27 +896,31 @@ pd_status check(const pd_attention8_args* a, bool pointers) {
   return PD_OK;
 }
 
-template <int DP, bool FEW, bool INT8>
-void launch(const Attn8& p, Cap cap, hipStream_t st) {
+template <int DP, bool INT8, Cap CAP>
+void launch(const Attn8& p, bool few, hipStream_t st) {
   const dim3 blocks((p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)), threads(NW * 64);
-  if (cap == CAP_NONE)
-    hipLaunchKernelGGL((attention8_kernel<DP, FEW, INT8, CAP_NONE>), blocks, threads, 0, st, p);
-  else if (cap == CAP_NEAR)
-    hipLaunchKernelGGL((attention8_kernel<DP, FEW, INT8, CAP_NEAR>), blocks, threads, 0, st, p);
+  if (few)
+    hipLaunchKernelGGL((attention8_few_kernel<DP, INT8, CAP>), blocks, threads, 0, st, p);
   else
-    hipLaunchKernelGGL((attention8_kernel<DP, FEW, INT8, CAP_FAR>), blocks, threads, 0, st, p);
+    hipLaunchKernelGGL((attention8_kernel<DP, INT8, CAP>), blocks, threads, 0, st, p);
+}
+
+template <int DP, bool INT8>
+void launch_cap(const Attn8& p, bool few, Cap cap, hipStream_t st) {
+  if (cap == CAP_NONE)
+    launch<DP, INT8, CAP_NONE>(p, few, st);
+  else if (cap == CAP_NEAR)
+    launch<DP, INT8, CAP_NEAR>(p, few, st);
+  else
+    launch<DP, INT8, CAP_FAR>(p, few, st);
 }
 
 template <int DP>
 void launch_width(const Attn8& p, const Plan& n, bool int8, Cap cap, hipStream_t st) {
-  if (n.few && int8)
-    launch<DP, true, true>(p, cap, st);
-  else if (n.few)
-    launch<DP, true, false>(p, cap, st);
-  else if (int8)
-    launch<DP, false, true>(p, cap, st);
+  if (int8)
+    launch_cap<DP, true>(p, n.few, cap, st);
   else
-    launch<DP, false, false>(p, cap, st);
+    launch_cap<DP, false>(p, n.few, cap, st);
   if (p.splits > 1)
     hipLaunchKernelGGL(attention8_join_kernel<DP>, dim3((unsigned)(p.kv_heads * p.batch) * p.rows), dim3(256), 0, st, p);
 }
@@ -683,6 +952,7 @@ extern "C" pd_status predecoder_attention8(void* hip_stream, const pd_attention8
   const float factor = cap == CAP_NONE ? a->scale * LOG2E : a->scale / most_cap;
   p.factor = fminf(fmaxf(factor, -FLT_MAX), FLT_MAX);
   p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
+  p.poly1 = p.cap_b * TANH1, p.poly3 = p.cap_b * TANH3, p.poly5 = p.cap_b * TANH5;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;
   p.o_b = a->out_batch_stride, p.o_t = a->out_token_stride, p.o_h = a->out_head_stride;
