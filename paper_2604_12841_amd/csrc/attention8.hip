@@ -31,6 +31,7 @@ using namespace pd;
 
 constexpr int TILE = 64;  // keys
 constexpr int NW = 4;     // waves of a workgroup
+constexpr int FW = 8;     // and of one with few rows
 constexpr int RUN = 4;    // neighbouring work items of one XCD
 constexpr int MOST_SPLITS = 256;
 
@@ -41,8 +42,8 @@ struct Attn8 {
   int row_tiles, splits, tiles_per_split;
   int causal, prefix_last;  // prefix - 1; INT_MIN, below every round: none
   // a score of product x and key scale s, in log2 units: s factor x, or with the cap, for u = s factor x:
-  // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for |u| <= 0.35 a polynomial
-  float factor, cap_a, cap_b, poly1, poly3, poly5;
+  // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for small |u| polynomials
+  float factor, cap_a, cap_b, poly1, poly3, poly5, mid[5];
   const uint16_t* q;
   uint16_t* out;
   long long q_b, q_t, q_h, o_b, o_t, o_h;
@@ -98,16 +99,16 @@ __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
 
 // A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u.
 // TIER: |u| is at most TIERS[TIER], or 2: anything.
-constexpr float TIERS[2] = {0.35f, 1.0f};
-// tanh u for |u| <= 1 is u (M1 + u^2 (M3 + ...)) within 2.1e-7 (fitted for the least largest error)
-constexpr float M1 = 0.9999961853f, M3 = -0.3332305849f, M5 = 0.1324913949f, M7 = -0.0508833490f, M9 = 0.0160305836f, M11 = -0.0028102861f;
+constexpr float TIERS[2] = {0.35f, 0.87f};
+// tanh u for |u| <= 0.87 is u (M1 + u^2 (M3 + ...)) within 7.9e-7 (fitted for the least largest error)
+constexpr float M1 = 0.99999005f, M3 = -0.33305562f, M5 = 0.13114086f, M7 = -0.04667219f, M9 = 0.01031595f;
 template <Cap CAP, int TIER>
 __device__ __forceinline__ float score8(const Attn8& p, float u, float t) {
   if constexpr (CAP == CAP_NONE) return u + t;
   const float w = u * u;
   if constexpr (CAP == CAP_NEAR) {
     if constexpr (TIER == 0) return fmaf(u, fmaf(w, fmaf(w, p.poly5, p.poly3), p.poly1), t);
-    if constexpr (TIER == 1) return fmaf(u * p.cap_b, fmaf(w, fmaf(w, fmaf(w, fmaf(w, fmaf(w, M11, M9), M7), M5), M3), M1), t);
+    if constexpr (TIER == 1) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, fmaf(w, p.mid[4], p.mid[3]), p.mid[2]), p.mid[1]), p.mid[0]), t);
     return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b + t);
   }
   float x = u * p.cap_b * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
@@ -213,14 +214,14 @@ __device__ __forceinline__ float inverse(float total) { return total > 0.0f ? 1.
 // Few rows: 16 a workgroup, all of them in each of its waves, which take tiles in turn.  A lane of group g of 16 holds
 // keys 16 n + 4 g + {0 .. 3} of row lane & 15.  K comes straight into registers, a tile ahead.
 template <int DP, bool INT8, Cap CAP>
-__global__ void __launch_bounds__(NW * 64, 2) attention8_few_kernel(const Attn8 p) {
+__global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 p) {
   constexpr int GR = DP / 16;                    // granules of a row
   constexpr int KG = DP > 64 ? 2 : 1;            // granules of K that a lane takes of a key (32 channels: half of one)
   constexpr int STEPS = DP / 32;                 // of a product over the channels
   constexpr int AHEAD = 8;                       // tiles whose sites are looked at together
-  __shared__ __attribute__((aligned(16))) uint8_t lv[NW][2][TILE * DP];
-  __shared__ KeyNotes key_notes[NW];
-  __shared__ float2 ml[NW][16];
+  __shared__ __attribute__((aligned(16))) uint8_t lv[FW][2][TILE * DP];
+  __shared__ KeyNotes key_notes[FW];
+  __shared__ float2 ml[FW][16];
   static_assert(2 * TILE * DP >= 16 * DP * 4, "a wave's result fits its tiles");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g4 = lane >> 4;
   KeyNotes& notes = key_notes[wave];
@@ -292,27 +293,27 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_few_kernel(const Attn8 
   const Seen seen = seen_by(p, at);
 
   // the tiles to visit, as a mask over the next AHEAD of this wave's
-  int base = begin - AHEAD * NW;
+  int base = begin - AHEAD * FW;
   uint32_t mask = 0;
   auto next_tile = [&]() -> int {  // -1: no more
     while (mask == 0) {
-      base += AHEAD * NW;
+      base += AHEAD * FW;
       if (base >= end) return -1;
       int4 s[AHEAD];
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) {
-        const int k = min((base + n * NW) * TILE + lane, p.capacity - 1);
-        s[n] = sites[base + n * NW < end ? k : 0];
+        const int k = min((base + n * FW) * TILE + lane, p.capacity - 1);
+        s[n] = sites[base + n * FW < end ? k : 0];
       }
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) {
-        const int tile = base + n * NW;
+        const int tile = base + n * FW;
         mask |= __any(tile < end && tile * TILE + lane < p.capacity && seen.some(s[n])) ? 1u << n : 0u;
       }
     }
     const int bit = __builtin_ctz(mask);
     mask &= mask - 1;
-    return base + bit * NW;
+    return base + bit * FW;
   };
 
   typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -464,15 +465,15 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_few_kernel(const Attn8 
   __syncthreads();
   const long long rows_at = (((long long)item.split * p.batch + b) * p.kv_heads + kvh) * p.rows;
   const int rows_here = min(16, p.rows - item.row_tile * 16);
-  for (int x = tid; x < rows_here * (DP / 4); x += NW * 64) {
+  for (int x = tid; x < rows_here * (DP / 4); x += FW * 64) {
     const int i = x / (DP / 4), d = x % (DP / 4) * 4;
     float best = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) best = fmaxf(best, ml[w][i].x);
+    for (int w = 0; w < FW; ++w) best = fmaxf(best, ml[w][i].x);
     float4 acc = make_float4(0, 0, 0, 0);
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
+    for (int w = 0; w < FW; ++w) {
       const float2 of = ml[w][i];
       if (of.x == -INFINITY) continue;  // the row saw nothing there
       const float weight = __builtin_amdgcn_exp2f(of.x - best);
@@ -846,7 +847,7 @@ Plan plan_for(const pd_attention8_args* a) {
   n.tiles = (int)(((long long)c.capacity + TILE - 1) / TILE);
   const int dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   // Splits: to fill the card, down to 8 tiles each
-  const long long whole = n.row_tiles * heads, fill = 512;
+  const long long whole = n.row_tiles * heads, fill = n.few ? 256 : 512;
   long long splits = (fill + whole - 1) / whole;
   if (splits > n.tiles / 8) splits = n.tiles / 8;
   if (splits > MOST_SPLITS) splits = MOST_SPLITS;
@@ -898,7 +899,7 @@ pd_status check(const pd_attention8_args* a, bool pointers) {
 
 template <int DP, bool INT8, Cap CAP>
 void launch(const Attn8& p, bool few, hipStream_t st) {
-  const dim3 blocks((p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)), threads(NW * 64);
+  const dim3 blocks((p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)), threads((few ? FW : NW) * 64);
   if (few)
     hipLaunchKernelGGL((attention8_few_kernel<DP, INT8, CAP>), blocks, threads, 0, st, p);
   else
@@ -952,6 +953,7 @@ extern "C" pd_status predecoder_attention8(void* hip_stream, const pd_attention8
   const float factor = cap == CAP_NONE ? a->scale * LOG2E : a->scale / most_cap;
   p.factor = fminf(fmaxf(factor, -FLT_MAX), FLT_MAX);
   p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
+  p.mid[0] = p.cap_b * M1, p.mid[1] = p.cap_b * M3, p.mid[2] = p.cap_b * M5, p.mid[3] = p.cap_b * M7, p.mid[4] = p.cap_b * M9;
   p.poly1 = p.cap_b * TANH1, p.poly3 = p.cap_b * TANH3, p.poly5 = p.cap_b * TANH5;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.q_b = a->q_batch_stride, p.q_t = a->q_token_stride, p.q_h = a->q_head_stride;
