@@ -316,7 +316,6 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
     return base + bit * FW;
   };
 
-  typedef __attribute__((ext_vector_type(4))) float f32x4;
   f32x4 o[DP / 16];
 #pragma unroll
   for (int m = 0; m < DP / 16; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};

@@ -88,26 +88,47 @@ struct Shape {
   static constexpr int NT = NW * 64;
 };
 
-// PAIRS: narrow rounds.  OUT: the results of a segment from the S that it starts from; otherwise its own S.
-template <int DP, bool PAIRS, bool OUT>
+// This workgroup's segment, key head and entry, and its first column of S; false: none.
+// (Workgroups are dealt to the eight XCDs in turn: the two that share a segment's queries and keys go to one, for its L2.)
+template <int DP>
+__device__ __forceinline__ bool item_of(const Linear& p, int& segment, int& kvh, int& b, int& v0) {
+  constexpr int VP = Shape<DP>::VP;
+  const int item = VP == DP ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7);
+  v0 = VP == DP ? 0 : VP * ((blockIdx.x >> 3) & 1);
+  segment = item % p.segments, kvh = item / p.segments % p.kv_heads, b = item / p.segments / p.kv_heads;
+  return item < p.batch * p.kv_heads * p.segments;
+}
+
+// Sends for W columns from `first` on of tokens at .. at + TILE - 1, straight into LDS: granule slots tid + n NT, of which
+// place() tells the turn.  Tokens past the tile's end repeat its last; columns past D are left as they are.
+template <int TILE, int W, int NT, typename F>
+__device__ __forceinline__ void send_rows(const uint16_t* rows, long long stride, uint8_t* to, int first, bool full, int D, long long at, int valid,
+                                          int tid, int wave, F&& place) {
+  constexpr int GR = W / 8;  // granules of a row
+#pragma unroll
+  for (int n = 0; n < (TILE * GR + NT - 1) / NT; ++n) {
+    if (n * NT + wave * 64 >= TILE * GR) break;
+    const int slot = tid + n * NT, key = slot / GR, c = first + (slot % GR ^ (place(key) >> 4) % GR) * 8;
+    const uint16_t* const from = rows + (at + min(key, valid - 1)) * stride + c;
+    if (full)
+      send16(from, to + (n * NT + wave * 64) * 16);
+    else if (c < D)
+      send16(from, to + (n * NT + wave * 64) * 16);
+  }
+}
+
+// Wide rounds.  OUT: the results of a segment from the S that it starts from; otherwise its own S.
+template <int DP, bool OUT>
 __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p) {
   using Sh = Shape<DP>;
   constexpr int VP = Sh::VP, TILE = Sh::TILE, KB = Sh::KB, VB = Sh::VB, NW = Sh::NW, NBW = Sh::NBW, NT = Sh::NT;
-  // parts that the columns of a block of results are dealt to waves in (narrow rounds: few rows, and many waves)
-  constexpr int MS = PAIRS ? VB : 1, MB = VB / MS;
   __shared__ __attribute__((aligned(16))) uint8_t lk[2][TILE * DP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * VP * 2];
   __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? VP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
-  __shared__ __attribute__((aligned(16))) float lt[PAIRS ? 64 : 4];   // round of a tile's token
-  __shared__ __attribute__((aligned(16))) float lw[PAIRS ? TILE : 4];   // what its key counts for after the tile
-  __shared__ float lp[PAIRS ? TILE + 1 : 1];                            // decay over that many rounds
-  __shared__ int odd_flag[2];
   __shared__ __attribute__((aligned(16))) uint8_t lo[OUT ? NW : 1][OUT ? 32 * 64 : 16];  // 32 columns of a unit's results
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  // (workgroups are dealt to the eight XCDs in turn: the two that share a segment's queries and keys go to one, for its L2)
-  const int item = VP == DP ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7), v0 = VP == DP ? 0 : VP * ((blockIdx.x >> 3) & 1);
-  if (item >= p.batch * p.kv_heads * p.segments) return;
-  const int segment = item % p.segments, kvh = item / p.segments % p.kv_heads, b = item / p.segments / p.kv_heads;
+  int segment, kvh, b, v0;
+  if (!item_of<DP>(p, segment, kvh, b, v0)) return;
   const int D = p.head_dim, len = length_of(p, b);
   const long long first = (long long)segment * p.segment_rounds * p.per_round;  // tokens of this segment
   const long long last = min((long long)len, first + (long long)p.segment_rounds * p.per_round);
@@ -136,10 +157,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
         if (dk < D && dv < D) to[dk * D + dv] = S[j][e];
       }
   };
-  // Slopes past 2^60 leave a row its own round, as 2^60 does; zero rounds stay 0.  (Taken here: with a choice between
-  // matrix instructions and the first reader of their result the compiler leaves too little time on the shorter way.)
-  const float slope = p.slopes ? fminf(fmaxf(p.slopes[kvh] * -LOG2E, -0x1p60f), 0x1p60f) : 0.0f;
-  const Fade fade = fade_of(p, kvh, PAIRS ? p.tile_rounds : 1);
+  const Fade fade = fade_of(p, kvh, 1);
 
   const uint16_t* kb = p.k + b * p.k_b + kvh * p.k_h;
   const uint16_t* vb = p.v + b * p.v_b + kvh * p.v_h;
@@ -148,49 +166,11 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
     for (int c = tid; c < 2 * TILE * (DP / 8); c += NT) *(uint4*)(lk[0] + c * 16) = make_uint4(0, 0, 0, 0);
     for (int c = tid; c < 2 * TILE * (VP / 8); c += NT) *(uint4*)(lv[0] + c * 16) = make_uint4(0, 0, 0, 0);
   }
-  if constexpr (PAIRS) {
-    for (int i = tid; i <= TILE; i += NT) lp[i] = p.slopes && i ? (float)exp(-(double)p.slopes[kvh] * i) : 1.0f;
-    for (int i = tid; i < 64; i += NT) lt[i] = (float)(i / p.per_round);
-  }
-  if (tid < 2) odd_flag[tid] = 0;
   __syncthreads();
-  // the keys' weights in a tile of so many rounds
-  auto weigh = [&](int rounds) {
-    for (int i = tid; i < TILE; i += NT) lw[i] = lp[max(rounds - 1 - (int)lt[i], 0)];
-  };
-
-  // Staging, straight into LDS: granule slots tid + n NT.  Tokens past the tile's end repeat its last.
   auto load_tile = [&](int buf, long long at, int valid) {
-    auto send = [&](auto width, const uint16_t* rows, long long stride, uint8_t* to, int first, auto place) {
-      constexpr int GR = decltype(width)::value / 8;  // granules of a row
-#pragma unroll
-      for (int n = 0; n < (TILE * GR + NT - 1) / NT; ++n) {
-        if (n * NT + wave * 64 >= TILE * GR) break;
-        const int slot = tid + n * NT, key = slot / GR, c = first + (slot % GR ^ (place(key) >> 4) % GR) * 8;
-        const uint16_t* const from = rows + (at + min(key, valid - 1)) * stride + c;
-        if (D == DP)
-          send16(from, to + (n * NT + wave * 64) * 16);
-        else if (c < D)
-          send16(from, to + (n * NT + wave * 64) * 16);
-      }
-    };
-    send(std::integral_constant<int, DP>(), kb, p.k_t, lk[buf], 0, [](int key) { return k_place<DP>(key, 0); });
-    send(std::integral_constant<int, VP>(), vb, p.v_t, lv[buf], v0, [](int key) { return v_place<VP>(key, 0); });
+    send_rows<TILE, DP, NT>(kb, p.k_t, lk[buf], 0, D == DP, D, at, valid, tid, wave, [](int key) { return k_place<DP>(key, 0); });
+    send_rows<TILE, VP, NT>(vb, p.v_t, lv[buf], v0, D == DP, D, at, valid, tid, wave, [](int key) { return v_place<VP>(key, 0); });
   };
-  // notes an infinity or a NaN in V, once this thread's granules have landed
-  auto note_odd = [&](int buf) {
-    uint32_t carry = 0;
-#pragma unroll
-    for (int n = 0; n < (TILE * (VP / 8) + NT - 1) / NT; ++n) {
-      if (n * NT + wave * 64 >= TILE * (VP / 8)) break;
-      const uint4 w = *(const uint4*)(lv[buf] + (tid + n * NT) * 16);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) carry |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
-    }
-    if (carry & 0x80008000u) odd_flag[buf] = 1;
-  };
-
   // LDS places of this lane's transposed operands: four tokens from 4 half on, and eight on from there
   const int vkey = (lane & 15) >> 2, vgran = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), vbyte = (lane & 1) * 8;
   const int k_tr[2] = {k_place<DP>(vkey + 4 * half, 4 * dkb + vgran) + vbyte, k_place<DP>(vkey + 4 * half + 8, 4 * dkb + vgran) + vbyte};
@@ -225,28 +205,9 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
           for (int j = 0; j < NBW; ++j) v[j][e] = in ? v[j][e] : 0;
         }
       }
-      if constexpr (PAIRS) {
-        const float4 w0 = *(const float4*)&lw[16 * s + 4 * half], w1 = *(const float4*)&lw[16 * s + 4 * half + 8];
-        const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-        uint32_t part[3][4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = bf16_of((uint16_t)a[2 * e]) * w[2 * e], y = bf16_of((uint16_t)a[2 * e + 1]) * w[2 * e + 1];
-          part[0][e] = bf16_pack(x, y);
-          const float x1 = x - __uint_as_float(part[0][e] << 16), y1 = y - __uint_as_float(part[0][e] & 0xffff0000u);
-          split2(x1, y1, part[1][e], part[2][e]);
-        }
-#pragma unroll
-        for (int n = 2; n >= 0; --n)
-#pragma unroll
-          for (int j = 0; j < NBW; ++j)
-            S[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, make_uint4(part[n][0], part[n][1], part[n][2], part[n][3])), __builtin_bit_cast(bf16x8, v[j]), S[j], 0, 0, 0);
-      } else {
 #pragma unroll
         for (int j = 0; j < NBW; ++j)
           S[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, v[j]), S[j], 0, 0, 0);
-      }
     }
   };
   auto share_state = [&] {
@@ -270,12 +231,12 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
   // (a division by the group: of the unit's first row, the same for all lanes, and of less than 128 by a product)
   const int group_part = 65536 / p.group + 1;
   auto token_at = [&](int unit, int lane_row, int& i, int& head) {
-    const int first = unit / MS * 32, from = first / p.group, x = first - from * p.group + lane_row, more = x * group_part >> 16;
+    const int first = unit * 32, from = first / p.group, x = first - from * p.group + lane_row, more = x * group_part >> 16;
     i = from + more, head = kvh * p.group + x - more * p.group;
   };
   auto place_of = [&](int unit, int tokens, int& row, int& i, int& head) {
-    row = unit / MS * 32 + (lane & 31);
-    token_at(unit, min(lane & 31, tokens * p.group - 1 - unit / MS * 32), i, head);
+    row = unit * 32 + (lane & 31);
+    token_at(unit, min(lane & 31, tokens * p.group - 1 - unit * 32), i, head);
   };
   auto fetch_unit = [&](long long at, int tokens, int unit) {
     int row, i, head;
@@ -287,36 +248,35 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
       next_q[s] = *(const uint4*)(q + min(16 * s + 8 * half, D - 8));
     }
   };
-  auto units_of = [&](int tokens) { return (tokens * p.group + 31) / 32 * MS; };
+  auto units_of = [&](int tokens) { return (tokens * p.group + 31) / 32; };
   auto fetch = [&](long long at, int tokens) {
     unit = wave;
     if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
   };
   // `most` of them
-  auto results = [&](int buf, long long at, int tokens, int most) {
+  auto results = [&](long long at, int tokens, int most) {
     const int rows = tokens * p.group, units = units_of(tokens);
 #pragma unroll 1
     for (int done = 0; done < most && unit < units; ++done, unit += NW) {
       int row, i, head;
       place_of(unit, tokens, row, i, head);
-      const int m0 = unit % MS * MB;
       bf16x8 fq[DP / 16];
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
       if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
       __builtin_amdgcn_sched_barrier(0);
-      f32x16 o[MB];
+      f32x16 o[VB];
 #pragma unroll
-      for (int m = 0; m < MB; ++m)
+      for (int m = 0; m < VB; ++m)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[m][e] = 0.0f;
       // (the parts of S are read a step ahead of the products that take them)
-      uint4 part[2][MB][2];
+      uint4 part[2][VB][2];
       auto read_parts = [&](int s) {
 #pragma unroll
-        for (int m = 0; m < MB; ++m)
+        for (int m = 0; m < VB; ++m)
 #pragma unroll
-          for (int n = 0; n < 2; ++n) part[s & 1][m][n] = *(const uint4*)(ls[OUT ? n : 0] + k_place<DP>(32 * (m0 + m) + (lane & 31), 2 * s + half));
+          for (int n = 0; n < 2; ++n) part[s & 1][m][n] = *(const uint4*)(ls[OUT ? n : 0] + k_place<DP>(32 * m + (lane & 31), 2 * s + half));
       };
       read_parts(0);
 #pragma unroll
@@ -326,78 +286,13 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
 #pragma unroll
         for (int n = 1; n >= 0; --n)
 #pragma unroll
-          for (int m = 0; m < MB; ++m)
+          for (int m = 0; m < VB; ++m)
             o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, part[s & 1][m][n]), fq[s], o[m], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (PAIRS) {
-        const float ti = lt[i], before = lp[(int)ti + 1];
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[m][e] *= before;
-        const bool odd = odd_flag[buf] != 0;
-#pragma unroll 1
-        for (int n = 0; n < 2; ++n) {
-          if (32 * n >= tokens) break;
-          f32x16 z;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[e] = 0.0f;
-#pragma unroll
-          for (int s = 0; s < DP / 16; ++s) {
-            const uint4 w = *(const uint4*)(lk[buf] + k_place<DP>(min(32 * n + (lane & 31), TILE - 1), 2 * s + half));
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z, 0, 0, 0);
-          }
-          uint32_t seen = 0;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 t = *(const float4*)&lt[32 * n + 8 * g + 4 * half];
-            const float tj[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float far = ti - tj[e];
-              const bool in = far >= 0.0f && 32 * n + 8 * g + 4 * half + e < tokens;
-              z[4 * g + e] = in ? z[4 * g + e] * __builtin_amdgcn_exp2f(slope * far) : 0.0f;
-              seen |= (uint32_t)in << (4 * g + e);
-            }
-          }
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (32 * n + 16 * s >= tokens) break;
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) split2(z[8 * s + 2 * e], z[8 * s + 2 * e + 1], hi[e], lo[e]);
-            const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-            const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-#pragma unroll
-            for (int m = 0; m < MB; ++m) {
-              const int step = (32 * n + 16 * s) * VP * 2;
-              s16x8 v = columns(lv[buf] + v_tr(m0 + m, 0) + step, lv[buf] + v_tr(m0 + m, 1) + step);
-              if (odd) {
-                // 0 x infinity: values that are not finite count as 0, and then make the rows that see them NaN
-                s16x8 there, ones;
-                f32x16 count;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) count[e] = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  there[e] = (v[e] & 0x7f80) == 0x7f80 ? 0x3f80 : 0;
-                  v[e] = there[e] ? 0 : v[e];
-                  ones[e] = seen >> (8 * s + e) & 1 ? 0x3f80 : 0;
-                }
-                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, there), __builtin_bit_cast(bf16x8, ones), count, 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[m][e] = count[e] != 0.0f ? NAN : o[m][e];
-              }
-              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pl, o[m], 0, 0, 0);
-              o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), ph, o[m], 0, 0, 0);
-            }
-          }
-        }
-      }
       // Lanes hold 8 bytes of a row here and there: through LDS, 32 columns at a time, they get 16 bytes each of whole pieces.
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
+      for (int m = 0; m < VB; ++m) {
         auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -409,7 +304,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          const int r = lane / 4 + 16 * n, rr = unit / MS * 32 + r, d = v0 + 32 * (m0 + m) + 8 * (lane & 3);
+          const int r = lane / 4 + 16 * n, rr = unit * 32 + r, d = v0 + 32 * m + 8 * (lane & 3);
           const uint4 w = *(const uint4*)granule(r, lane & 3);
           int ri, rh;
           token_at(unit, r, ri, rh);
@@ -420,82 +315,380 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
     }
   };
 
-  // The tiles: [at, at + valid).  Wide rounds: a tile does not cross a round's end.
-  auto tile_end = [&](long long at, long long round_end) { return (int)(min(min(at + p.tile_tokens, round_end), last) - at); };
-  long long at = first, round_end = PAIRS ? last : first + p.per_round;
+  // The tiles: [at, at + valid), which do not cross a round's end.
+  auto tile_end = [&](long long at, long long round_end) { return (int)(min(min(at + TILE, round_end), last) - at); };
+  long long at = first, round_end = first + p.per_round;
   int buf = 0, valid = 0;
   if (at < last) {
     valid = tile_end(at, round_end);
     load_tile(0, at, valid);
   }
-  if constexpr (PAIRS) {
-    weigh(min(p.tile_rounds, (valid + p.per_round - 1) / p.per_round));
-    if constexpr (OUT) {
-      if (at < last) fetch(at, valid);
-      share_state();
-    }
-  }
   sent();
-  if constexpr (PAIRS && OUT) note_odd(0);
   __syncthreads();
   long long round_at = at;
-  long long due_at = at;  // wide rounds: the tokens whose results are to come from the S in LDS
+  long long due_at = at;  // the tokens whose results are to come from the S in LDS
   int due = 0;
   while (at < last) {
     const long long next = at + valid;
-    const bool ends = PAIRS || next == round_end || next == last;
-    const bool begins = PAIRS || at == round_at;
-    long long next_end = round_end;
-    if (!PAIRS && next == round_end) next_end += p.per_round;
+    const bool ends = next == round_end || next == last;
+    const long long next_end = next == round_end ? round_end + p.per_round : round_end;
     int next_valid = 0;
     if (next < last) {
       next_valid = tile_end(next, next_end);
       load_tile(buf ^ 1, next, next_valid);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (PAIRS) {
-      const int rounds = (valid + p.per_round - 1) / p.per_round;
-      if constexpr (OUT) {
-        results(buf, at, valid, INT_MAX);
-        if (next < last) fetch(next, next_valid);
+    update(buf, valid, at == round_at, fade);
+    if constexpr (OUT) {
+      // a share of the round before's results with each tile of this one
+      const int left = (int)((min(round_end, last) - at + TILE - 1) / TILE), mine = (units_of(due) - unit + NW - 1) / NW;
+      if (mine > 0) results(due_at, due, (mine + left - 1) / left);
+      if (ends) {
+        __syncthreads();  // S of the round before is read
+        share_state();
+        due_at = round_at, due = (int)(next - round_at);
+        fetch(due_at, due);
       }
-      update(buf, valid, true, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
-      sent();
-      __syncthreads();  // S, the weights and this tile are read
-      if (next < last) {
-        if (OUT && tid == 0) odd_flag[buf] = 0;
-        if constexpr (OUT) {
-          note_odd(buf ^ 1);
-          share_state();
-        }
-        const int next_rounds = (next_valid + p.per_round - 1) / p.per_round;
-        if (next_rounds != rounds) weigh(next_rounds);
-      }
-      __syncthreads();
-    } else {
-      update(buf, valid, begins, fade);
-      if constexpr (OUT) {
-        // a share of the round before's results with each tile of this one
-        const int left = (int)((min(round_end, last) - at + p.tile_tokens - 1) / p.tile_tokens), mine = (units_of(due) - unit + NW - 1) / NW;
-        if (mine > 0) results(buf, due_at, due, (mine + left - 1) / left);
-        if (ends) {
-          __syncthreads();  // S of the round before is read
-          share_state();
-          due_at = round_at, due = (int)(next - round_at);
-          fetch(due_at, due);
-        }
-      }
-      sent();
-      __syncthreads();
     }
-    if (!PAIRS && ends) round_at = next;
+    sent();
+    __syncthreads();
+    if (ends) round_at = next;
     at = next, valid = next_valid, round_end = next_end, buf ^= 1;
   }
-  if constexpr (OUT && !PAIRS) results(buf, due_at, due, INT_MAX);
+  if constexpr (OUT) results(due_at, due, INT_MAX);
   if constexpr (!OUT)
     store_state(own);
   else if (p.segments == 1 && p.state_out)
     store_state(p.state_out + state_at);
+}
+
+// Narrow rounds: a tile holds whole rounds.  Products of 16 x 16 blocks, so that a tile's few queries keep the waves busy:
+// lane (c, g) of a block's result holds column c = lane & 15 and rows 4 g + {0 .. 3}, g = lane >> 4.
+// OUT: the results of a segment from the S that it starts from; otherwise its own S.
+template <int DP, bool OUT>
+__global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_kernel(const Linear p) {
+  constexpr int VP = Shape<DP>::VP, TILE = Shape<DP>::TILE, NT = 256, NW = 4;
+  constexpr int NK = DP / 16 > NW ? DP / 16 / NW : 1, NV = DP == 32 ? 1 : VP / 16;  // blocks of S of a wave: NK x NV
+  constexpr int STEPS = DP / 32;                                                    // of a product over the key's channels
+  constexpr int PARTS = (TILE + 31) / 32;                                           // of a tile: 32 tokens
+  __shared__ __attribute__((aligned(16))) uint8_t lk[2][TILE * DP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t lv[2][TILE * VP * 2];
+  __shared__ __attribute__((aligned(16))) uint8_t ls[OUT ? 2 : 1][OUT ? VP * DP * 2 : 16];  // S^T in two parts, rows placed as K's
+  __shared__ __attribute__((aligned(16))) uint8_t lo[OUT ? NW : 1][OUT ? 16 * 64 : 16];     // 32 columns of a unit's results
+  __shared__ __attribute__((aligned(16))) float lt[64];                                     // round of a tile's token, or NEVER
+  __shared__ __attribute__((aligned(16))) float lw[64];                                     // what its key counts for after the tile
+  __shared__ float lp[65];                                                                  // decay over that many rounds
+  __shared__ int odd_flag[2];
+  constexpr float NEVER = 1e30f;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g4 = lane >> 4;
+  int segment, kvh, b, v0;
+  if (!item_of<DP>(p, segment, kvh, b, v0)) return;
+  const int D = p.head_dim, len = length_of(p, b);
+  const long long first = (long long)segment * p.segment_rounds * p.per_round;  // tokens of this segment
+  const long long last = min((long long)len, first + (long long)p.segment_rounds * p.per_round);
+  const long long state_at = (long long)(b * p.kv_heads + kvh) * D * D;
+  float* const own = p.starts + (state_at * p.segments + (long long)segment * D * D);
+  const int dk0 = 16 * (DP == 32 ? wave & 1 : wave * NK), dv0 = DP == 32 ? 16 * (wave >> 1) : 0;  // of this wave's blocks
+
+  f32x4 S[NK][NV];
+  {
+    const float* from = !OUT ? nullptr : p.segments > 1 ? own : p.state ? p.state + state_at : nullptr;
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int dk = dk0 + 16 * i + 4 * g4 + e, dv = v0 + dv0 + 16 * j + c;
+          S[i][j][e] = from ? from[min(dk, D - 1) * D + min(dv, D - 1)] : 0.0f;
+          if (dk >= D || dv >= D) S[i][j][e] = 0.0f;
+        }
+  }
+  // Slopes past 2^60 leave a row its own round, as 2^60 does; zero rounds stay 0.
+  const float slope = p.slopes ? fminf(fmaxf(p.slopes[kvh] * -LOG2E, -0x1p60f), 0x1p60f) : 0.0f;
+  const Fade fade = fade_of(p, kvh, p.tile_rounds);
+  const uint16_t* kb = p.k + b * p.k_b + kvh * p.k_h;
+  const uint16_t* vb = p.v + b * p.v_b + kvh * p.v_h;
+  // columns past head_dim stay the zeros that they are set to here
+  if (D < DP) {
+    for (int i = tid; i < 2 * TILE * (DP / 8); i += NT) *(uint4*)(lk[0] + i * 16) = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < 2 * TILE * (VP / 8); i += NT) *(uint4*)(lv[0] + i * 16) = make_uint4(0, 0, 0, 0);
+  }
+  for (int i = tid; i <= 64; i += NT) lp[i] = p.slopes && i ? (float)exp(-(double)p.slopes[kvh] * i) : 1.0f;
+  if (tid < 2) odd_flag[tid] = 0;
+  __syncthreads();
+  auto rounds_of = [&](int tokens) { return (tokens + p.per_round - 1) / p.per_round; };
+  // the tokens' rounds and weights in a tile of so many
+  auto weigh = [&](int tokens) {
+    if (tid < 64) {
+      const int t = tid / p.per_round;
+      lt[tid] = tid < tokens ? (float)t : NEVER;
+      lw[tid] = lp[max(rounds_of(tokens) - 1 - t, 0)];
+    }
+  };
+  auto load_tile = [&](int buf, long long at, int valid) {
+    send_rows<TILE, DP, NT>(kb, p.k_t, lk[buf], 0, D == DP, D, at, valid, tid, wave, [](int key) { return k_place<DP>(key, 0); });
+    send_rows<TILE, VP, NT>(vb, p.v_t, lv[buf], v0, D == DP, D, at, valid, tid, wave, [](int key) { return v_place<VP>(key, 0); });
+  };
+  // notes an infinity or a NaN in V, once this thread's granules have landed
+  auto note_odd = [&](int buf) {
+    uint32_t carry = 0;
+#pragma unroll
+    for (int n = 0; n < (TILE * (VP / 8) + NT - 1) / NT; ++n) {
+      if (n * NT + wave * 64 >= TILE * (VP / 8)) break;
+      const uint4 w = *(const uint4*)(lv[buf] + (tid + n * NT) * 16);
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) carry |= (u[e] & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries
+    }
+    if (carry & 0x80008000u) odd_flag[buf] = 1;
+  };
+  // Transposed operands: columns 16 block + c of tokens 32 s + 4 g4 + {0 .. 3} and, elements 4 .. 7, 16 on from there.
+  const int t_row = 4 * g4 + (c >> 2), t_gran = (c >> 1) & 1, t_byte = (c & 1) * 8;
+  auto columns = [&](const uint8_t* f, int half_tile) {
+    return __builtin_shufflevector(read_columns(f), read_columns(f + half_tile), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // (places repeat every 16 rows; where a tile ends with the first 16, they stand for the others too, which count for nothing)
+  auto second = [&](int s) { return 32 * s + 16 < TILE ? 16 : 0; };
+  auto k_columns = [&](int buf, int channel, int s) {
+    return columns(lk[buf] + k_place<DP>(t_row, channel / 8 + t_gran) + t_byte + 32 * s * DP * 2, second(s) * DP * 2);
+  };
+  auto v_columns = [&](int buf, int channel, int s) {
+    return columns(lv[buf] + v_place<VP>(t_row, channel / 8 + t_gran) + t_byte + 32 * s * VP * 2, second(s) * VP * 2);
+  };
+  auto token_of = [&](int s, int e) { return 32 * s + 4 * g4 + (e & 3) + 16 * (e >> 2); };
+
+  // S = fade S + K^T V over the tile's tokens, the keys weighted
+  auto update = [&](int buf, int valid, Fade f) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i][j][e] = faded(S[i][j][e], f, 0.0f);
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s) {
+      s16x8 v[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) v[j] = v_columns(buf, dv0 + 16 * j, s);
+      const float4 w0 = *(const float4*)&lw[32 * s + 4 * g4], w1 = *(const float4*)&lw[32 * s + 4 * g4 + 16];
+      const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+      const bool cut = 32 * s + 32 > valid;
+      if (cut) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int j = 0; j < NV; ++j) v[j][e] = token_of(s, e) < valid ? v[j][e] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        s16x8 a = k_columns(buf, dk0 + 16 * i, s);
+        if (cut) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = token_of(s, e) < valid ? a[e] : 0;
+        }
+        uint32_t part[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = bf16_of((uint16_t)a[2 * e]) * w[2 * e], y = bf16_of((uint16_t)a[2 * e + 1]) * w[2 * e + 1];
+          part[0][e] = bf16_pack(x, y);
+          const float x1 = x - __uint_as_float(part[0][e] << 16), y1 = y - __uint_as_float(part[0][e] & 0xffff0000u);
+          split2(x1, y1, part[1][e], part[2][e]);
+        }
+#pragma unroll
+        for (int n = 2; n >= 0; --n)
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+            S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, make_uint4(part[n][0], part[n][1], part[n][2], part[n][3])), __builtin_bit_cast(bf16x8, v[j]), S[i][j], 0, 0, 0);
+      }
+    }
+  };
+  auto share_state = [&] {
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        uint2 hi, lo;
+        split2(S[i][j][0], S[i][j][1], hi.x, lo.x);
+        split2(S[i][j][2], S[i][j][3], hi.y, lo.y);
+        const int at = k_place<DP>(dv0 + 16 * j + c, (dk0 + 16 * i) / 8 + (g4 >> 1)) + 8 * (g4 & 1);
+        *(uint2*)(ls[0] + at) = hi;
+        *(uint2*)(ls[OUT ? 1 : 0] + at) = lo;
+      }
+  };
+
+  // The results of a tile's queries: rows token * group + head, 16 of them a unit, which the waves take in turn.  The queries of a
+  // wave's next unit are on their way while it works on one; fetch() sends for those of the tile's first.
+  uint4 next_q[STEPS];
+  const int group_part = 65536 / p.group + 1;
+  // (a division by the group: of the unit's first row, the same for all lanes, and of less than 128 by a product)
+  auto token_at = [&](int unit, int of_unit, int& i, int& head) {
+    const int from = 16 * unit / p.group, x = 16 * unit - from * p.group + of_unit, more = x * group_part >> 16;
+    i = from + more, head = kvh * p.group + x - more * p.group;
+  };
+  auto fetch_unit = [&](long long at, int tokens, int unit) {
+    int i, head;
+    token_at(unit, min(c, tokens * p.group - 1 - 16 * unit), i, head);
+    const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) next_q[s] = *(const uint4*)(q + min(32 * s + 8 * g4, D - 8));  // (past head_dim S and the keys are 0)
+  };
+  auto units_of = [&](int tokens) { return (tokens * p.group + 15) / 16; };
+  auto fetch = [&](long long at, int tokens) {
+    if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
+  };
+  auto results = [&](int buf, long long at, int tokens) {
+    const int rows = tokens * p.group, units = units_of(tokens);
+    const bool odd = __any(odd_flag[buf] != 0);
+#pragma unroll 1
+    for (int unit = wave; unit < units; unit += NW) {
+      bf16x8 fq[STEPS];
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
+      if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
+      int i, head, i_end, head_end;
+      token_at(unit, min(c, rows - 1 - 16 * unit), i, head);
+      token_at(unit, min(15, rows - 1 - 16 * unit), i_end, head_end);
+      const float ti = lt[i], before = lp[(int)ti + 1], t_end = lt[i_end];
+      f32x4 o[VP / 16];
+#pragma unroll
+      for (int m = 0; m < VP / 16; ++m) o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int n = 1; n >= 0; --n)
+#pragma unroll
+          for (int m = 0; m < VP / 16; ++m) {
+            const uint4 w = *(const uint4*)(ls[OUT ? n : 0] + k_place<DP>(16 * m + c, 4 * s + g4));
+            o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), fq[s], o[m], 0, 0, 0);
+          }
+#pragma unroll
+      for (int m = 0; m < VP / 16; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[m][e] *= before;
+#pragma unroll 1
+      for (int part = 0; part < PARTS; ++part) {
+        if (__any(lt[32 * part] > t_end)) break;  // later rounds than the unit's
+        f32x4 z[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          z[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s) {
+            const uint4 w = *(const uint4*)(lk[buf] + k_place<DP>(min(32 * part + 16 * n, TILE - 16) + c, 4 * s + g4));
+            z[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), fq[s], z[n], 0, 0, 0);
+          }
+        }
+        uint32_t hi[4], lo2[4];
+        float far[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const float4 t = *(const float4*)&lt[32 * part + 16 * n + 4 * g4];
+          far[n][0] = ti - t.x, far[n][1] = ti - t.y, far[n][2] = ti - t.z, far[n][3] = ti - t.w;
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = far[n][e] >= 0.0f ? z[n][e] * __builtin_amdgcn_exp2f(slope * far[n][e]) : 0.0f;
+          split2(x[0], x[1], hi[2 * n], lo2[2 * n]);
+          split2(x[2], x[3], hi[2 * n + 1], lo2[2 * n + 1]);
+        }
+        const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]));
+#pragma unroll
+        for (int m = 0; m < VP / 16; ++m) {
+          s16x8 v = v_columns(buf, 16 * m, part);
+          if (odd) {
+            // 0 x infinity: values that are not finite count as 0, and then make the rows that see them NaN
+            s16x8 there, ones;
+            f32x4 count = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              there[e] = (v[e] & 0x7f80) == 0x7f80 ? 0x3f80 : 0;
+              v[e] = there[e] ? 0 : v[e];
+              ones[e] = far[e >> 2][e & 3] >= 0.0f ? 0x3f80 : 0;
+            }
+            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, there), __builtin_bit_cast(bf16x8, ones), count, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[m][e] = count[e] != 0.0f ? NAN : o[m][e];
+          }
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pl, o[m], 0, 0, 0);
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), ph, o[m], 0, 0, 0);
+        }
+      }
+      // Lanes hold 8 bytes of a row here and there: through LDS, 32 columns at a time, they get 16 bytes each of whole pieces.
+#pragma unroll
+      for (int m = 0; m < VP / 32; ++m) {
+        auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          uint2 w;
+          w.x = bf16_pack(o[2 * m + n][0] * p.scale, o[2 * m + n][1] * p.scale);
+          w.y = bf16_pack(o[2 * m + n][2] * p.scale, o[2 * m + n][3] * p.scale);
+          *(uint2*)(granule(c, 2 * n + (g4 >> 1)) + 8 * (g4 & 1)) = w;
+        }
+        __builtin_amdgcn_wave_barrier();
+        const int r = lane >> 2, d = v0 + 32 * m + 8 * (lane & 3);
+        const uint4 w = *(const uint4*)granule(r, lane & 3);
+        int ri, rh;
+        token_at(unit, r, ri, rh);
+        if (16 * unit + r < rows && d < D) *(uint4*)(p.out + b * p.o_b + (at + ri) * p.o_t + rh * p.o_h + d) = w;
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  };
+
+  long long at = first;
+  auto tile_end = [&](long long from) { return (int)(min(from + p.tile_tokens, last) - from); };
+  int buf = 0, valid = 0;
+  if (at < last) {
+    valid = tile_end(at);
+    load_tile(0, at, valid);
+    if constexpr (OUT) fetch(at, valid);
+  }
+  weigh(valid);
+  if constexpr (OUT) share_state();
+  sent();
+  if constexpr (OUT) note_odd(0);
+  __syncthreads();
+  while (at < last) {
+    const long long next = at + valid;
+    int next_valid = 0;
+    if (next < last) {
+      next_valid = tile_end(next);
+      load_tile(buf ^ 1, next, next_valid);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (OUT) {
+      results(buf, at, valid);
+      if (next < last) fetch(next, next_valid);
+    }
+    const int rounds = rounds_of(valid);
+    update(buf, valid, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
+    sent();
+    __syncthreads();  // S, the weights and this tile are read
+    if (next < last) {
+      if (OUT && tid == 0) odd_flag[buf] = 0;
+      if constexpr (OUT) {
+        note_odd(buf ^ 1);
+        share_state();
+      }
+      if (next_valid != valid) weigh(next_valid);
+    }
+    __syncthreads();
+    at = next, valid = next_valid, buf ^= 1;
+  }
+  float* const to = !OUT ? own : p.segments == 1 && p.state_out ? p.state_out + state_at : nullptr;
+  if (to) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int dk = dk0 + 16 * i + 4 * g4 + e, dv = v0 + dv0 + 16 * j + c;
+          if (dk < D && dv < D) to[dk * D + dv] = S[i][j][e];
+        }
+  }
 }
 
 // The S that each segment starts from, in the place of its own, and the last one.  A thread an element of S.
@@ -659,15 +852,15 @@ void launch(const Linear& p, bool pairs, hipStream_t st) {
   const dim3 grid(Shape<DP>::VP == DP ? items : (items + 7) / 8 * 16), threads(Shape<DP>::NT);
   if (p.segments > 1) {
     if (pairs)
-      hipLaunchKernelGGL((linear_kernel<DP, true, false>), grid, threads, 0, st, p);
+      hipLaunchKernelGGL((linear_narrow_kernel<DP, false>), grid, dim3(256), 0, st, p);
     else
-      hipLaunchKernelGGL((linear_kernel<DP, false, false>), grid, threads, 0, st, p);
+      hipLaunchKernelGGL((linear_kernel<DP, false>), grid, threads, 0, st, p);
     hipLaunchKernelGGL(linear_scan_kernel, dim3(heads * ((p.head_dim * p.head_dim + 255) / 256)), dim3(256), 0, st, p);
   }
   if (pairs)
-    hipLaunchKernelGGL((linear_kernel<DP, true, true>), grid, threads, 0, st, p);
+    hipLaunchKernelGGL((linear_narrow_kernel<DP, true>), grid, dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((linear_kernel<DP, false, true>), grid, threads, 0, st, p);
+    hipLaunchKernelGGL((linear_kernel<DP, true>), grid, threads, 0, st, p);
 }
 
 }  // namespace
