@@ -227,42 +227,46 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
   // The results of the queries of tokens at .. at + tokens - 1: rows token * group + head, 32 of them a unit.  The
   // queries of a wave's next unit are on their way while it works on one; fetch() sends for those of the first.
   int unit = 0;  // this wave's next
-  uint4 next_q[DP / 16];
+  u32x4 next_q[DP / 16];
   // (a division by the group: of the unit's first row, the same for all lanes, and of less than 128 by a product)
   const int group_part = 65536 / p.group + 1;
   auto token_at = [&](int unit, int lane_row, int& i, int& head) {
     const int first = unit * 32, from = first / p.group, x = first - from * p.group + lane_row, more = x * group_part >> 16;
     i = from + more, head = kvh * p.group + x - more * p.group;
   };
-  auto place_of = [&](int unit, int tokens, int& row, int& i, int& head) {
-    row = unit * 32 + (lane & 31);
-    token_at(unit, min(lane & 31, tokens * p.group - 1 - unit * 32), i, head);
-  };
+  // (four lanes read 64 bytes of a row: 16 rows a load; single rows' lanes lie apart in the products' operands)
   auto fetch_unit = [&](long long at, int tokens, int unit) {
-    int row, i, head;
-    place_of(unit, tokens, row, i, head);
-    const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      // (past head_dim anything of the row will do: S and the keys are 0 there)
-      next_q[s] = *(const uint4*)(q + min(16 * s + 8 * half, D - 8));
+    for (int j = 0; j < 2; ++j) {
+      int i, head;
+      token_at(unit, min(16 * j + lane / 4, tokens * p.group - 1 - unit * 32), i, head);
+      const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
+#pragma unroll
+      for (int s = 0; s < DP / 32; ++s)  // (past head_dim anything of the row will do: S is 0 there)
+        next_q[2 * s + j] = *(const u32x4*)(q + min(32 * s + 8 * (lane & 3), D - 8));
     }
   };
+  auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };  // 32 rows of 64 bytes
   auto units_of = [&](int tokens) { return (tokens * p.group + 31) / 32; };
   auto fetch = [&](long long at, int tokens) {
     unit = wave;
     if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
   };
-  // `most` of them
+  // `most` of them.  (The next tile is waited for before the first result is stored: later, the wait would be for the stores too.)
   auto results = [&](long long at, int tokens, int most) {
     const int rows = tokens * p.group, units = units_of(tokens);
 #pragma unroll 1
     for (int done = 0; done < most && unit < units; ++done, unit += NW) {
-      int row, i, head;
-      place_of(unit, tokens, row, i, head);
       bf16x8 fq[DP / 16];
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
+      for (int s = 0; s < DP / 32; ++s) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *(u32x4*)granule(16 * j + lane / 4, lane & 3) = next_q[2 * s + j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fq[2 * s + j] = __builtin_bit_cast(bf16x8, *(const u32x4*)granule(lane & 31, 2 * j + half));
+        __builtin_amdgcn_wave_barrier();
+      }
       if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
       __builtin_amdgcn_sched_barrier(0);
       f32x16 o[VB];
@@ -290,10 +294,10 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
             o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, part[s & 1][m][n]), fq[s], o[m], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if (done == 0) sent();
       // Lanes hold 8 bytes of a row here and there: through LDS, 32 columns at a time, they get 16 bytes each of whole pieces.
 #pragma unroll
       for (int m = 0; m < VB; ++m) {
-        auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           uint2 w;
@@ -342,15 +346,19 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
     if constexpr (OUT) {
       // a share of the round before's results with each tile of this one
       const int left = (int)((min(round_end, last) - at + TILE - 1) / TILE), mine = (units_of(due) - unit + NW - 1) / NW;
-      if (mine > 0) results(due_at, due, (mine + left - 1) / left);
+      if (mine > 0)
+        results(due_at, due, (mine + left - 1) / left);
+      else
+        sent();
       if (ends) {
         __syncthreads();  // S of the round before is read
         share_state();
         due_at = round_at, due = (int)(next - round_at);
         fetch(due_at, due);
       }
+    } else {
+      sent();
     }
-    sent();
     __syncthreads();
     if (ends) round_at = next;
     at = next, valid = next_valid, round_end = next_end, buf ^= 1;
@@ -366,7 +374,7 @@ __global__ void __launch_bounds__(Shape<DP>::NT, 2) linear_kernel(const Linear p
 // lane (c, g) of a block's result holds column c = lane & 15 and rows 4 g + {0 .. 3}, g = lane >> 4.
 // OUT: the results of a segment from the S that it starts from; otherwise its own S.
 template <int DP, bool OUT>
-__global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_kernel(const Linear p) {
+__global__ void __launch_bounds__(256, 2) linear_narrow_kernel(const Linear p) {
   constexpr int VP = Shape<DP>::VP, TILE = Shape<DP>::TILE, NT = 256, NW = 4;
   constexpr int NK = DP / 16 > NW ? DP / 16 / NW : 1, NV = DP == 32 ? 1 : VP / 16;  // blocks of S of a wave: NK x NV
   constexpr int STEPS = DP / 32;                                                    // of a product over the key's channels
@@ -519,25 +527,28 @@ __global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_
   };
 
   // The results of a tile's queries: rows token * group + head, 16 of them a unit, which the waves take in turn.  The queries of a
-  // wave's next unit are on their way while it works on one; fetch() sends for those of the tile's first.
-  uint4 next_q[STEPS];
+  // wave's next unit are on their way while it works on one, and those of the next tile's first (fetch()) for a whole tile.
+  u32x4 first_q[STEPS], next_q[STEPS];
   const int group_part = 65536 / p.group + 1;
   // (a division by the group: of the unit's first row, the same for all lanes, and of less than 128 by a product)
   auto token_at = [&](int unit, int of_unit, int& i, int& head) {
     const int from = 16 * unit / p.group, x = 16 * unit - from * p.group + of_unit, more = x * group_part >> 16;
     i = from + more, head = kvh * p.group + x - more * p.group;
   };
-  auto fetch_unit = [&](long long at, int tokens, int unit) {
+  auto fetch_unit = [&](u32x4 (&to)[STEPS], long long at, int tokens, int unit) {
+    // (four lanes read 64 bytes of a row; a row's lanes lie apart in the products' operands)
     int i, head;
-    token_at(unit, min(c, tokens * p.group - 1 - 16 * unit), i, head);
+    token_at(unit, min(lane / 4, tokens * p.group - 1 - 16 * unit), i, head);
     const uint16_t* q = p.q + b * p.q_b + (at + i) * p.q_t + head * p.q_h;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) next_q[s] = *(const uint4*)(q + min(32 * s + 8 * g4, D - 8));  // (past head_dim S and the keys are 0)
+    for (int s = 0; s < STEPS; ++s) to[s] = *(const u32x4*)(q + min(32 * s + 8 * (lane & 3), D - 8));  // (past head_dim S and the keys are 0)
   };
+  auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };  // 16 rows of 64 bytes
   auto units_of = [&](int tokens) { return (tokens * p.group + 15) / 16; };
   auto fetch = [&](long long at, int tokens) {
-    if (wave < units_of(tokens)) fetch_unit(at, tokens, wave);
+    if (wave < units_of(tokens)) fetch_unit(first_q, at, tokens, wave);
   };
+  // (the next tile is waited for before the first result is stored: later, the wait would be for the stores too)
   auto results = [&](int buf, long long at, int tokens) {
     const int rows = tokens * p.group, units = units_of(tokens);
     const bool odd = __any(odd_flag[buf] != 0);
@@ -545,8 +556,13 @@ __global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_
     for (int unit = wave; unit < units; unit += NW) {
       bf16x8 fq[STEPS];
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) fq[s] = __builtin_bit_cast(bf16x8, next_q[s]);
-      if (unit + NW < units) fetch_unit(at, tokens, unit + NW);
+      for (int s = 0; s < STEPS; ++s) {
+        *(u32x4*)granule(lane / 4, lane & 3) = next_q[s];
+        __builtin_amdgcn_wave_barrier();
+        fq[s] = __builtin_bit_cast(bf16x8, *(const u32x4*)granule(c, g4));
+        __builtin_amdgcn_wave_barrier();
+      }
+      if (unit + NW < units) fetch_unit(next_q, at, tokens, unit + NW);
       int i, head, i_end, head_end;
       token_at(unit, min(c, rows - 1 - 16 * unit), i, head);
       token_at(unit, min(15, rows - 1 - 16 * unit), i_end, head_end);
@@ -615,10 +631,10 @@ __global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_
           o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), ph, o[m], 0, 0, 0);
         }
       }
+      if (unit == wave) sent();
       // Lanes hold 8 bytes of a row here and there: through LDS, 32 columns at a time, they get 16 bytes each of whole pieces.
 #pragma unroll
       for (int m = 0; m < VP / 32; ++m) {
-        auto granule = [&](int r, int g) { return lo[wave] + (r * 4 + (g ^ (r >> 2 & 3))) * 16; };
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           uint2 w;
@@ -656,15 +672,20 @@ __global__ void __launch_bounds__(256, DP == 128 || !OUT ? 2 : 3) linear_narrow_
     if (next < last) {
       next_valid = tile_end(next);
       load_tile(buf ^ 1, next, next_valid);
+      if constexpr (OUT) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) next_q[s] = first_q[s];
+        fetch(next, next_valid);
+      }
+    } else if (OUT) {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) next_q[s] = first_q[s];
     }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (OUT) {
-      results(buf, at, valid);
-      if (next < last) fetch(next, next_valid);
-    }
     const int rounds = rounds_of(valid);
     update(buf, valid, rounds == p.tile_rounds ? fade : fade_of(p, kvh, rounds));
-    sent();
+    if constexpr (OUT) results(buf, at, valid);
+    if (!OUT || wave >= units_of(valid)) sent();
     __syncthreads();  // S, the weights and this tile are read
     if (next < last) {
       if (OUT && tid == 0) odd_flag[buf] = 0;
