@@ -16,27 +16,36 @@ namespace {
 
 using namespace pd;
 
+// (arrays of HIP's own vectors, which are structures, would go to LDS)
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+constexpr int MANY = 4;  // rows a thread, in large writes
+
 struct Cache8 {
   int batch, kv_heads, head_dim, capacity, tokens;
   unsigned token_blocks;
   uint8_t* codes;
   float* scales;
-  int4* sites;
+  i32x4* sites;
   const long long* at;
   const void* x[2];  // k, v
   void* y[2];
   long long b_stride[2], t_stride[2], h_stride[2];
-  const int4* in_sites;
-  int4* out_sites;
+  const i32x4* in_sites;
+  i32x4* out_sites;
   long long sites_b;
 };
 
-// The place of token m: (at + m) mod capacity, m <= capacity.
-__device__ __forceinline__ int place_of(long long at, int m, int capacity) {
-  long long p = at % capacity;
-  if (p < 0) p += capacity;
-  p += m;
-  return (int)(p < capacity ? p : p - capacity);
+// at mod capacity, and the place of token m <= capacity from there on.
+__device__ __forceinline__ int start_of(long long at, int capacity) {
+  if (at >= 0 && at < capacity) return (int)at;
+  const long long p = at % capacity;
+  return (int)(p < 0 ? p + capacity : p);
+}
+__device__ __forceinline__ int place_of(int start, int m, int capacity) {
+  const unsigned p = (unsigned)start + (unsigned)m;
+  return (int)(p < (unsigned)capacity ? p : p - (unsigned)capacity);
 }
 
 // x / s to 23 bits, the last of which is set where more follow: another rounding, to fewer bits, is the only one.
@@ -61,57 +70,65 @@ __device__ __forceinline__ void load_row8(const T* p, float* v) {
   }
 }
 
-template <typename T, int LPR, bool INT8, bool WIDE>
+// N: rows a thread, loaded together.
+template <typename T, int LPR, int N, bool INT8, bool WIDE>
 __global__ void __launch_bounds__(256) cache_write_kernel(const Cache8 p) {
   constexpr int ROWS = 256 / LPR;
   const unsigned group = blockIdx.x / p.token_blocks;
-  const int m = (int)(blockIdx.x % p.token_blocks) * ROWS + threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const int m0 = (int)(blockIdx.x % p.token_blocks) * (ROWS * N) + threadIdx.x / LPR, lane = threadIdx.x % LPR;
   const int h = group % p.kv_heads, which = group / p.kv_heads % 2, b = group / p.kv_heads / 2;
-  const bool inside = m < p.tokens;
-  const int4 site = inside ? p.in_sites[b * p.sites_b + m] : make_int4(0, 0, 0, -1);
-  const bool there = site.w >= 0;
-  const bool mine = there && 8 * lane < p.head_dim;
-  float v[8] = {};
-  if (mine) load_row8<T, WIDE>((const T*)p.x[which] + b * p.b_stride[which] + m * p.t_stride[which] + h * p.h_stride[which] + 8 * lane, v);
-  float most = 0.0f;
-  bool finite = true;
+  const int d = min(8 * lane, p.head_dim - 8);  // (lanes past the row's end repeat its last values)
+  const T* x = (const T*)p.x[which] + b * p.b_stride[which] + h * p.h_stride[which] + d;
+  i32x4 site[N];
+  float v[N][8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    most = fmaxf(most, fabsf(v[e]));
-    finite = finite && fabsf(v[e]) < INFINITY;
+  for (int n = 0; n < N; ++n) {
+    const int m = min(m0 + n * ROWS, p.tokens - 1);
+    site[n] = p.in_sites[b * p.sites_b + m];
+    load_row8<T, WIDE>(x + m * p.t_stride[which], v[n]);
   }
-  if (!finite) most = INFINITY;
+  const int start = start_of(p.at[b], p.capacity);
+  const long long rows = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity;
 #pragma unroll
-  for (int n = 1; n < LPR; n <<= 1) most = fmaxf(most, __shfl_xor(most, n));
-  if (!there) return;
-  const float scale = most < INFINITY ? most / (INT8 ? 127.0f : 448.0f) : NAN;
-  const int place = place_of(p.at[b], m, p.capacity);
-  const long long row = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity + place;
-  if (lane == 0) p.scales[row] = scale;
-  if (lane == 0 && which == 0 && h == 0) p.sites[(long long)b * p.capacity + place] = site;
-  if (!mine) return;
-  uint2 w = make_uint2(0, 0);
-  if (scale > 0.0f) {
-    // (rows of tiny values are lifted, so that the rest of a division is a number of the range)
-    const float lift = scale < 0x1p-60f ? 0x1p64f : 1.0f, s = scale * lift, r = 1.0f / s;
-    float c[8];
+  for (int n = 0; n < N; ++n) {
+    const int m = m0 + n * ROWS;
+    const bool there = m < p.tokens && site[n].w >= 0;
+    float most = 0.0f;
+    bool finite = true;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = quotient_odd(v[e] * lift, s, r);
-    // (a scale of few bits, below the normal range, may be too small for its row)
+    for (int e = 0; e < 8; ++e) {
+      most = fmaxf(most, fabsf(v[n][e]));
+      finite = finite && fabsf(v[n][e]) < INFINITY;
+    }
+    if (!finite) most = INFINITY;
+#pragma unroll
+    for (int k = 1; k < LPR; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
+    if (!there) continue;
     const float q = INT8 ? 127.0f : 448.0f;
+    const float scale = most < INFINITY ? most / q : NAN;
+    const int place = place_of(start, m, p.capacity);
+    if (lane == 0) p.scales[rows + place] = scale;
+    if (lane == 0 && which == 0 && h == 0) p.sites[(long long)b * p.capacity + place] = site[n];
+    uint2 w = make_uint2(0, 0);
+    if (scale > 0.0f) {
+      // (rows of tiny values are lifted, so that the rest of a division is a number of the range)
+      const float lift = scale < 0x1p-60f ? 0x1p64f : 1.0f, s = scale * lift, r = 1.0f / s;
+      float c[8];
+      // (a scale of few bits, below the normal range, may be too small for its row)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = fminf(fmaxf(c[e], -q), q);
-    if constexpr (INT8)
-      w = make_uint2(int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7]));
-    else
-      w = make_uint2(e4m3_pack4_within(c[0], c[1], c[2], c[3]), e4m3_pack4_within(c[4], c[5], c[6], c[7]));
+      for (int e = 0; e < 8; ++e) c[e] = fminf(fmaxf(quotient_odd(v[n][e] * lift, s, r), -q), q);
+      if constexpr (INT8)
+        w = make_uint2(int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7]));
+      else
+        w = make_uint2(e4m3_pack4_within(c[0], c[1], c[2], c[3]), e4m3_pack4_within(c[4], c[5], c[6], c[7]));
+    }
+    if (8 * lane < p.head_dim) *(uint2*)(p.codes + (rows + place) * p.head_dim + d) = w;
   }
-  *(uint2*)(p.codes + row * p.head_dim + 8 * lane) = w;
 }
 
 // The values of eight codes.
 template <bool INT8>
-__device__ __forceinline__ void decode8(const uint2 w, float* v) {
+__device__ __forceinline__ void decode8(const u32x2 w, float* v) {
   const uint32_t u[2] = {w.x, w.y};
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
@@ -132,19 +149,20 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const Cache8 p) {
   const int m = (int)(blockIdx.x % p.token_blocks) * ROWS + threadIdx.x / LPR, lane = threadIdx.x % LPR;
   const int h = group % p.kv_heads, which = group / p.kv_heads % 2, b = group / p.kv_heads / 2;
   if (m >= p.tokens) return;
-  const int place = place_of(p.at[b], m, p.capacity);
-  const int4 site = p.sites[(long long)b * p.capacity + place];
+  const int d = min(8 * lane, p.head_dim - 8);  // (lanes past the row's end repeat its last values)
+  const int place = place_of(start_of(p.at[b], p.capacity), m, p.capacity);
+  const long long row = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity + place;
+  const i32x4 site = p.sites[(long long)b * p.capacity + place];
+  const u32x2 w = *(const u32x2*)(p.codes + row * p.head_dim + d);
+  const float scale = p.scales[row];
   if (lane == 0 && which == 0 && h == 0 && p.out_sites) p.out_sites[b * p.sites_b + m] = site;
   if (8 * lane >= p.head_dim) return;
-  float v[8] = {};
-  if (site.w >= 0) {
-    const long long row = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity + place;
-    const float scale = p.scales[row];
-    decode8<INT8>(*(const uint2*)(p.codes + row * p.head_dim + 8 * lane), v);
+  float v[8];
+  decode8<INT8>(w, v);
+  // (without a token codes and scale may be anything)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= scale;
-  }
-  T* y = (T*)p.y[which] + b * p.b_stride[which] + m * p.t_stride[which] + h * p.h_stride[which] + 8 * lane;
+  for (int e = 0; e < 8; ++e) v[e] = site.w >= 0 ? v[e] * scale : 0.0f;
+  T* y = (T*)p.y[which] + b * p.b_stride[which] + m * p.t_stride[which] + h * p.h_stride[which] + d;
   if constexpr (WIDE) {
     store8(y, v);
   } else {
@@ -154,13 +172,16 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const Cache8 p) {
 }
 
 template <typename T, bool INT8, bool WIDE>
-void launch(const Cache8& p, bool write, long long groups, hipStream_t st) {
+void launch(const Cache8& p, bool write, bool many, long long groups, hipStream_t st) {
   auto go = [&](auto lanes) {
     constexpr int LPR = decltype(lanes)::value;
-    if (write)
-      hipLaunchKernelGGL((cache_write_kernel<T, LPR, INT8, WIDE>), dim3((unsigned)(groups * p.token_blocks)), dim3(256), 0, st, p);
+    const dim3 blocks((unsigned)(groups * p.token_blocks));
+    if (write && many)
+      hipLaunchKernelGGL((cache_write_kernel<T, LPR, MANY, INT8, WIDE>), blocks, dim3(256), 0, st, p);
+    else if (write)
+      hipLaunchKernelGGL((cache_write_kernel<T, LPR, 1, INT8, WIDE>), blocks, dim3(256), 0, st, p);
     else
-      hipLaunchKernelGGL((cache_read_kernel<T, LPR, INT8, WIDE>), dim3((unsigned)(groups * p.token_blocks)), dim3(256), 0, st, p);
+      hipLaunchKernelGGL((cache_read_kernel<T, LPR, INT8, WIDE>), blocks, dim3(256), 0, st, p);
   };
   if (p.head_dim <= 32)
     go(std::integral_constant<int, 4>());
@@ -178,8 +199,13 @@ pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
   if (a->tokens < 0 || a->tokens > c.capacity) return PD_ERR_INVALID_ARG;
   if (a->dtype != PD_DTYPE_BF16 && a->dtype != PD_DTYPE_FP32) return PD_ERR_INVALID_ARG;
   if (!c.batch || !c.kv_heads || !a->tokens) return PD_OK;
-  const int lanes = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : 16, rows = 256 / lanes;
-  const long long groups = 2ll * c.batch * c.kv_heads, blocks = (a->tokens + rows - 1) / rows;
+  const int lanes = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : 16;
+  const long long groups = 2ll * c.batch * c.kv_heads;
+  // A write takes several rows a thread where the card is full all the same (16 streams of 9800 tokens, 4 x 64 bf16: 64 us
+  // against 76 with one; 64 of 196, 8 x 64: 14.5 against 13.0).  A read does not gain (170 us against 190: 16 of 9800, 4 x 128 fp32).
+  const bool many = write && groups * a->tokens * lanes >= 256ll * 2048 * MANY;
+  const int rows = 256 / lanes * (many ? MANY : 1);
+  const long long blocks = ((long long)a->tokens + rows - 1) / rows;
   if (groups * blocks >= 1ll << 24) return PD_ERR_UNSUPPORTED;  // threads below 2^32
   if (check_cache(c, true) != PD_OK || !a->at || (uintptr_t)a->at % 8 || !a->k || !a->v || (write && !a->sites)) return PD_ERR_INVALID_ARG;
   const int elem = a->dtype == PD_DTYPE_BF16 ? 2 : 4;
@@ -193,11 +219,11 @@ pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
   Cache8 p;
   p.batch = c.batch, p.kv_heads = c.kv_heads, p.head_dim = c.head_dim, p.capacity = c.capacity, p.tokens = a->tokens;
   p.token_blocks = (unsigned)blocks;
-  p.codes = (uint8_t*)c.codes, p.scales = c.scales, p.sites = (int4*)c.sites, p.at = (const long long*)a->at;
+  p.codes = (uint8_t*)c.codes, p.scales = c.scales, p.sites = (i32x4*)c.sites, p.at = (const long long*)a->at;
   p.x[0] = p.y[0] = a->k, p.x[1] = p.y[1] = a->v;
   p.b_stride[0] = a->k_batch_stride, p.t_stride[0] = a->k_token_stride, p.h_stride[0] = a->k_head_stride;
   p.b_stride[1] = a->v_batch_stride, p.t_stride[1] = a->v_token_stride, p.h_stride[1] = a->v_head_stride;
-  p.in_sites = (const int4*)a->sites, p.out_sites = (int4*)a->sites, p.sites_b = a->sites_batch_stride;
+  p.in_sites = (const i32x4*)a->sites, p.out_sites = (i32x4*)a->sites, p.sites_b = a->sites_batch_stride;
   bool wide = true;
   for (int n = 0; n < 2; ++n)
     wide = wide && (uintptr_t)p.x[n] % 16 == 0 && p.b_stride[n] * elem % 16 == 0 && p.t_stride[n] * elem % 16 == 0 && p.h_stride[n] * elem % 16 == 0;
@@ -205,9 +231,9 @@ pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
   auto go = [&](auto type, auto int8) {
     using T = decltype(type);
     if (wide)
-      launch<T, decltype(int8)::value, true>(p, write, groups, st);
+      launch<T, decltype(int8)::value, true>(p, write, many, groups, st);
     else
-      launch<T, decltype(int8)::value, false>(p, write, groups, st);
+      launch<T, decltype(int8)::value, false>(p, write, many, groups, st);
   };
   const bool int8 = c.codes_type == PD_CODES_INT8, bf16 = a->dtype == PD_DTYPE_BF16;
   if (bf16 && int8)
