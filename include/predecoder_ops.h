@@ -234,7 +234,7 @@ typedef struct pd_cache {
 } pd_cache;
 
 /* Token m of entry b is at place (at[b] + m) mod capacity (at may be any number,
- * negative ones too); tokens <= capacity, so that no place comes twice.
+ * negative ones too); tokens <= capacity, so that no place comes twice (at most 2^30).
  *
  * Write: k and v [batch][tokens][kv_heads][head_dim] into the cache, with their
  * sites.  scale = max |x| / 448 (E4M3) or / 127 (int8) in fp32, codes x / scale
@@ -268,7 +268,7 @@ pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args);
  * queries that see nothing), of q over the tokens of a cache: keys and values are
  * code scale, not rounded in between.  Scores, maximum and sum are fp32; a
  * probability times a value's scale is rounded to bf16 (2^-8) for the product with the
- * values' codes.  A visible row with scale NaN makes the result NaN; what invisible places
+ * values' codes, or for up to 64 rows (n_q heads / kv_heads) kept to 16 bits.  A visible row with scale NaN makes the result NaN; what invisible places
  * hold does not reach it (but E4M3's NaN codes, which predecoder_cache_write never
  * writes, may stand only where there is no token).
  * q and out as there: bf16, all rows 16-byte aligned; heads a multiple of

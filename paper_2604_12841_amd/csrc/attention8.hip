@@ -302,13 +302,11 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
       int4 s[AHEAD];
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) {
-        const int k = min((base + n * FW) * TILE + lane, p.capacity - 1);
-        s[n] = sites[base + n * FW < end ? k : 0];
+        s[n] = sites[min(min(base + n * FW, end - 1) * TILE + lane, p.capacity - 1)];
       }
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) {
-        const int tile = base + n * FW;
-        mask |= __any(tile < end && tile * TILE + lane < p.capacity && seen.some(s[n])) ? 1u << n : 0u;
+        mask |= base + n * FW < end && __any(seen.some(s[n])) ? 1u << n : 0u;
       }
     }
     const int bit = __builtin_ctz(mask);
@@ -415,11 +413,11 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[n][e] -= up;
     }
-    // probabilities, times the value's scale, in bf16; and their product with the codes
+    // probabilities, times the value's scale, in two bf16 parts (16 bits: matrix units have the time); and their product with the codes
     auto finish = [&](auto carefully) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        uint32_t u[4], keep[2];
+        uint32_t hi[4], lo[4], keep[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           const float4 f4 = *(const float4*)&notes.v[32 * s + 16 * n + 4 * g4];
@@ -432,16 +430,20 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
             x[e] = e2 * f[e];
             if constexpr (carefully.value) x[e] = y == -INFINITY ? 0.0f : x[e];  // (an invisible row's scale may be anything)
           }
-          u[2 * n] = bf16_pack(x[0], x[1]), u[2 * n + 1] = bf16_pack(x[2], x[3]);
+          split2(x[0], x[1], hi[2 * n], lo[2 * n]);
+          split2(x[2], x[3], hi[2 * n + 1], lo[2 * n + 1]);
           // codes at places without a token may be E4M3's NaN
           if constexpr (carefully.value) keep[n] = byte_mask((uint32_t)(tokens >> (32 * s + 16 * n + 4 * g4)));
         }
-        const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+        const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
         for (int m = 0; m < DP / 16; ++m) {
           i32x2 w = read_byte_columns(lv[wave][buf] + (v_off ^ m << 4) + v_byte + 32 * s * DP);
           if constexpr (carefully.value) w[0] &= keep[0], w[1] &= keep[1];
-          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode<INT8>((uint32_t)w[0], (uint32_t)w[1]), pr, o[m], 0, 0, 0);
+          const bf16x8 v = decode<INT8>((uint32_t)w[0], (uint32_t)w[1]);
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl, o[m], 0, 0, 0);
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph, o[m], 0, 0, 0);
         }
       }
     };

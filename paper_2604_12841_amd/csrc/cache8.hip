@@ -206,7 +206,8 @@ pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
   const bool many = write && groups * a->tokens * lanes >= 256ll * 2048 * MANY;
   const int rows = 256 / lanes * (many ? MANY : 1);
   const long long blocks = ((long long)a->tokens + rows - 1) / rows;
-  if (groups * blocks >= 1ll << 24) return PD_ERR_UNSUPPORTED;  // threads below 2^32
+  // (threads below 2^32, tokens and a block's more in 31 bits)
+  if (groups * blocks >= 1ll << 24 || a->tokens > 1 << 30) return PD_ERR_UNSUPPORTED;
   if (check_cache(c, true) != PD_OK || !a->at || (uintptr_t)a->at % 8 || !a->k || !a->v || (write && !a->sites)) return PD_ERR_INVALID_ARG;
   const int elem = a->dtype == PD_DTYPE_BF16 ? 2 : 4;
   if ((uintptr_t)a->k % elem || (uintptr_t)a->v % elem || (uintptr_t)a->sites % 16) return PD_ERR_INVALID_ARG;

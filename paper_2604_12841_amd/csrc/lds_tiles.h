@@ -1,9 +1,12 @@
 // lds_tiles.h -- tiles of tokens' rows in LDS: loads from memory straight into
-// them, where a row's granules lie, and reads of transposed operands.
+// them, where a row's granules lie, reads of transposed operands; and values in
+// two bf16 parts.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "activation.h"
 
 namespace pd {
 
@@ -53,6 +56,12 @@ template <int DP>
 __device__ __forceinline__ int v_place(int key, int g) {
   const int turn = DP == 128 ? (key & 3) << 2 : DP == 64 ? ((key >> 1) & 1) << 2 : 0;
   return key * (DP * 2) + ((g ^ turn) << 4);
+}
+
+// Two values in two bf16 parts, to 16 bits: hi + lo.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = bf16_pack(a, b);
+  lo = bf16_pack(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
 }
 
 // Four rows of 16 columns, 8 bytes a lane of each 16 lanes (row (lane & 15) >> 2, columns 4 (lane & 3) on): a lane gets its column's four rows.

@@ -70,12 +70,7 @@ __device__ __forceinline__ Fade fade_of(const Linear& p, int kvh, int rounds) {
 }
 __device__ __forceinline__ float faded(float s, Fade f, float add) { return fmaf(s, f.hi, fmaf(s, f.lo, add)); }
 
-// Splits v into bf16 parts: v = hi + lo to 16 bits.
 __device__ __forceinline__ float bf16_of(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = bf16_pack(a, b);
-  lo = bf16_pack(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
-}
 
 // A workgroup holds all rows of S (the key's channels, padded to DP) and VP of its columns (the value's channels).
 template <int DP>

@@ -475,6 +475,7 @@ def attention8(q, cache, out, q_sites, scale=None, cap=0.0, slopes=None, causal=
 
 def _linear_args(q, k, v, out, slopes, per_round, lengths, state, state_out, scale):
     _need(q.dim() == 4 and k.dim() == 4, "q and k must be [batch][tokens][heads][head_dim]")
+    _need(per_round < 1 << 31, "per_round must be below 2^31")
     shape, dev = q.shape, _index(q, "q")
     B, n, H, D = shape
     Hk = k.shape[2]
