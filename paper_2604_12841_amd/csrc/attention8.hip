@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
     }
     const int rr = item.row_tile * 16 + i;
     if (p.splits > 1) {
-      *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;
+      if (best != -INFINITY) *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;  // (the join leaves out splits of weight 0)
       if (d == 0) p.part_ml[rows_at + rr] = make_float2(best, sum);
     } else if (d < p.head_dim) {
       const float inv = inverse(sum);
@@ -510,6 +510,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   if (!item_of(p, item)) return;
   const int kvh = item.kvh, b = item.b;
   const int row = item.row_tile * 128 + wave * 32 + (lane & 31);
+  const bool idle = item.row_tile * 128 + wave * 32 >= p.rows;  // a wave without rows only sends for its part of the tiles
   const int r = row < p.rows ? row : p.rows - 1;  // rows past the end repeat the last: not stored
   const int token = r / p.group, head = kvh * p.group + r % p.group;
   const uint16_t* q = p.q + b * p.q_b + token * p.q_t + head * p.q_h;
@@ -618,7 +619,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
     const float vs = t.vs[lane];
     const uint64_t tokens = __ballot(held);
     const bool whole = __all(held && seen.all(site, bias));
-    if (!__any(held && seen.some(site))) return;
+    if (idle || !__any(held && seen.some(site))) return;
     const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
     // (the waves write the same)
     notes.f[lane] = t.ks[lane] * p.factor;
@@ -760,11 +761,13 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   if (p.splits > 1) {
     const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
     const long long rows_at = (((long long)item.split * p.batch + b) * p.kv_heads + kvh) * p.rows;
+    if (!none) {  // (the join leaves out splits of weight 0)
 #pragma unroll
-    for (int m = 0; m < DP / 32; ++m)
+      for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(float4*)(p.part_o + (rows_at + row) * DP + 32 * m + 8 * g + 4 * half) = make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
+        for (int g = 0; g < 4; ++g)
+          *(float4*)(p.part_o + (rows_at + row) * DP + 32 * m + 8 * g + 4 * half) = make_float4(o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]);
+    }
     if (half == 0) p.part_ml[rows_at + row] = make_float2(none ? -INFINITY : top, total);
     return;
   }
@@ -815,7 +818,7 @@ __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
 #pragma unroll 4
   for (int s = g; s < p.splits; s += GROUPS) {
     const float a = weight[s];
-    const float4 o = *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    const float4 o = a == 0.0f ? make_float4(0, 0, 0, 0) : *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
     acc.x = fmaf(o.x, a, acc.x), acc.y = fmaf(o.y, a, acc.y), acc.z = fmaf(o.z, a, acc.z), acc.w = fmaf(o.w, a, acc.w);
   }
   so[g][lane] = acc;
