@@ -177,3 +177,14 @@ def test_refusals():
     q = torch.zeros(2, 3, 3, 64, device="cuda", dtype=torch.bfloat16)
     with pytest.raises(pdx.PredecoderError):
         pdx.attention8(q, cache, torch.empty_like(q), sites)
+
+
+def test_many_rows_in_splits():
+    """Rows enough for the join that takes a row in a few threads."""
+    g = tc.gen(12)
+    B, capacity, n, H, Hk, D = 1, 2500, 300, 8, 2, 48
+    k_sites = places_of(g, B, capacity, 1, 30, 0.05)
+    k_sites[:, 1400:, 3] = -1
+    cache = mc.filled_cache(g, B, capacity, Hk, D, "int8", k_sites)
+    q = tc.normal(g, B, n, H, D).to(torch.bfloat16)
+    check(q, cache, places_of(g, B, n, 1, 30, 0.1), causal=True, cap=15.0)
