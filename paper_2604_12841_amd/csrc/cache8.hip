@@ -3,7 +3,7 @@
 //
 // A row is the keys or the values of one token and head: its scale is
 // max |x| / Q, its codes x / scale rounded to the format (Q its largest value).
-// Eight values a lane; as many lanes as hold a row (a power of two) find its
+// A write takes 16 values a lane, a read 8; as many lanes as hold a row (a power of two) find its
 // largest value among themselves.  A wave takes neighbouring tokens of one head,
 // whose rows lie one behind the other in the cache, so it writes whole lines.
 #include <hip/hip_runtime.h>
@@ -19,8 +19,9 @@ using namespace pd;
 // (arrays of HIP's own vectors, which are structures, would go to LDS)
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int MANY = 4;  // rows a thread, in large writes
+constexpr int MANY = 2;  // rows a thread, in large writes (16 streams of 9800 tokens, 4 x 64 bf16: 58 us, with four 60, with one 76)
 
 struct Cache8 {
   int batch, kv_heads, head_dim, capacity, tokens;
@@ -61,13 +62,23 @@ __device__ __forceinline__ float quotient_odd(float x, float s, float r) {
 }
 
 template <typename T, bool WIDE>
-__device__ __forceinline__ void load_row8(const T* p, float* v) {
+__device__ __forceinline__ void load_row16(const T* p, float* v) {
   if constexpr (WIDE) {
     load8(p, v);
+    load8(p + 8, v + 8);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = load1(p + e);
+    for (int e = 0; e < 16; ++e) v[e] = load1(p + e);
   }
+}
+
+// most / q, rounded to nearest: with 1 / q rounded, one correction makes it so where the rest is a number of the range.
+template <bool INT8>
+__device__ __forceinline__ float scale_of(float most) {
+  constexpr float q = INT8 ? 127.0f : 448.0f, part = 1.0f / q;
+  if (!(most > 0x1p-80f)) return most / q;
+  const float s = most * part;
+  return fmaf(fmaf(-s, q, most), part, s);
 }
 
 // N: rows a thread, loaded together.
@@ -77,15 +88,15 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const Cache8 p) {
   const unsigned group = blockIdx.x / p.token_blocks;
   const int m0 = (int)(blockIdx.x % p.token_blocks) * (ROWS * N) + threadIdx.x / LPR, lane = threadIdx.x % LPR;
   const int h = group % p.kv_heads, which = group / p.kv_heads % 2, b = group / p.kv_heads / 2;
-  const int d = min(8 * lane, p.head_dim - 8);  // (lanes past the row's end repeat its last values)
+  const int d = min(16 * lane, p.head_dim - 16);  // (lanes past the row's end repeat its last values)
   const T* x = (const T*)p.x[which] + b * p.b_stride[which] + h * p.h_stride[which] + d;
   i32x4 site[N];
-  float v[N][8];
+  float v[N][16];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int m = min(m0 + n * ROWS, p.tokens - 1);
     site[n] = p.in_sites[b * p.sites_b + m];
-    load_row8<T, WIDE>(x + m * p.t_stride[which], v[n]);
+    load_row16<T, WIDE>(x + m * p.t_stride[which], v[n]);
   }
   const int start = start_of(p.at[b], p.capacity);
   const long long rows = ((long long)(b * 2 + which) * p.kv_heads + h) * p.capacity;
@@ -96,7 +107,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const Cache8 p) {
     float most = 0.0f;
     bool finite = true;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 16; ++e) {
       most = fmaxf(most, fabsf(v[n][e]));
       finite = finite && fabsf(v[n][e]) < INFINITY;
     }
@@ -105,24 +116,24 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const Cache8 p) {
     for (int k = 1; k < LPR; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
     if (!there) continue;
     const float q = INT8 ? 127.0f : 448.0f;
-    const float scale = most < INFINITY ? most / q : NAN;
+    const float scale = most < INFINITY ? scale_of<INT8>(most) : NAN;
     const int place = place_of(start, m, p.capacity);
     if (lane == 0) p.scales[rows + place] = scale;
     if (lane == 0 && which == 0 && h == 0) p.sites[(long long)b * p.capacity + place] = site[n];
-    uint2 w = make_uint2(0, 0);
+    u32x4 w = {0, 0, 0, 0};
     if (scale > 0.0f) {
       // (rows of tiny values are lifted, so that the rest of a division is a number of the range)
       const float lift = scale < 0x1p-60f ? 0x1p64f : 1.0f, s = scale * lift, r = 1.0f / s;
-      float c[8];
-      // (a scale of few bits, below the normal range, may be too small for its row)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = fminf(fmaxf(quotient_odd(v[n][e] * lift, s, r), -q), q);
-      if constexpr (INT8)
-        w = make_uint2(int8_pack4(c[0], c[1], c[2], c[3]), int8_pack4(c[4], c[5], c[6], c[7]));
-      else
-        w = make_uint2(e4m3_pack4_within(c[0], c[1], c[2], c[3]), e4m3_pack4_within(c[4], c[5], c[6], c[7]));
+      for (int g = 0; g < 4; ++g) {
+        float c[4];
+        // (a scale of few bits, below the normal range, may be too small for its row)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = fminf(fmaxf(quotient_odd(v[n][4 * g + e] * lift, s, r), -q), q);
+        w[g] = INT8 ? int8_pack4(c[0], c[1], c[2], c[3]) : e4m3_pack4_within(c[0], c[1], c[2], c[3]);
+      }
     }
-    if (8 * lane < p.head_dim) *(uint2*)(p.codes + (rows + place) * p.head_dim + d) = w;
+    if (16 * lane < p.head_dim) *(u32x4*)(p.codes + (rows + place) * p.head_dim + d) = w;
   }
 }
 
@@ -177,9 +188,9 @@ void launch(const Cache8& p, bool write, bool many, long long groups, hipStream_
     constexpr int LPR = decltype(lanes)::value;
     const dim3 blocks((unsigned)(groups * p.token_blocks));
     if (write && many)
-      hipLaunchKernelGGL((cache_write_kernel<T, LPR, MANY, INT8, WIDE>), blocks, dim3(256), 0, st, p);
+      hipLaunchKernelGGL((cache_write_kernel<T, LPR / 2, MANY, INT8, WIDE>), blocks, dim3(256), 0, st, p);
     else if (write)
-      hipLaunchKernelGGL((cache_write_kernel<T, LPR, 1, INT8, WIDE>), blocks, dim3(256), 0, st, p);
+      hipLaunchKernelGGL((cache_write_kernel<T, LPR / 2, 1, INT8, WIDE>), blocks, dim3(256), 0, st, p);
     else
       hipLaunchKernelGGL((cache_read_kernel<T, LPR, INT8, WIDE>), blocks, dim3(256), 0, st, p);
   };
@@ -199,11 +210,11 @@ pd_status run(void* hip_stream, const pd_cache_args* a, bool write) {
   if (a->tokens < 0 || a->tokens > c.capacity) return PD_ERR_INVALID_ARG;
   if (a->dtype != PD_DTYPE_BF16 && a->dtype != PD_DTYPE_FP32) return PD_ERR_INVALID_ARG;
   if (!c.batch || !c.kv_heads || !a->tokens) return PD_OK;
-  const int lanes = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : 16;
+  // lanes of a row: 8 values each, a write's 16
+  const int lanes = (c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : 16) / (write ? 2 : 1);
   const long long groups = 2ll * c.batch * c.kv_heads;
-  // A write takes several rows a thread where the card is full all the same (16 streams of 9800 tokens, 4 x 64 bf16: 64 us
-  // against 76 with one; 64 of 196, 8 x 64: 14.5 against 13.0).  A read does not gain (170 us against 190: 16 of 9800, 4 x 128 fp32).
-  const bool many = write && groups * a->tokens * lanes >= 256ll * 2048 * MANY;
+  // A write takes several rows a thread where the card is full all the same.
+  const bool many = write && groups * a->tokens * lanes >= 256ll * 1024 * MANY;
   const int rows = 256 / lanes * (many ? MANY : 1);
   const long long blocks = ((long long)a->tokens + rows - 1) / rows;
   // (threads below 2^32, tokens and a block's more in 31 bits)
