@@ -18,8 +18,8 @@
 // rounds of d = 13, 8 (2) heads of 64, E4M3: 14.5 us and 4 us of the join.
 //
 // Many rows: 128 a workgroup, 32 a wave, which share tiles in LDS.  Bound by
-// vector instructions, about 15 a score with cap and bias: 196 tokens against the same
-// four caches 206 us and 8 us of the join (250 TFLOP/s; vector units 0.53 busy
+// vector instructions, about 14 a score with cap and bias: 196 tokens against the same
+// four caches 197 us and 8 us of the join (260 TFLOP/s; vector units 0.53 busy
 // without what the exponentials take longer, matrix units 0.11).
 //
 // What to read: before the keys of 8 (16) tiles the sites are read, and tiles
@@ -54,7 +54,7 @@ struct Attn8 {
   int causal, prefix_last;  // prefix - 1; INT_MIN, below every round: none
   // a score of product x and key scale s, in log2 units: s factor x, or with the cap, for u = s factor x:
   // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for small |u| polynomials
-  float factor, cap_a, cap_b, poly1, poly3, poly5, mid[5];
+  float factor, cap_a, cap_b, poly1, poly3, poly5, low[4], mid[5];
   const uint16_t* q;
   uint16_t* out;
   long long q_b, q_t, q_h, o_b, o_t, o_h;
@@ -109,9 +109,11 @@ __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
 }
 
 // A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u.
-// TIER: |u| is at most TIERS[TIER], or 2: anything.
-constexpr float TIERS[2] = {0.35f, 0.87f};
-// tanh u for |u| <= 0.87 is u (M1 + u^2 (M3 + ...)) within 7.9e-7 (fitted for the least largest error)
+// TIER: |u| is at most TIERS[TIER], or 3: anything.
+constexpr float TIERS[3] = {0.35f, 0.62f, 0.87f};
+// tanh u for |u| <= 0.62 is u (N1 + u^2 (N3 + ...)), for |u| <= 0.87 u (M1 + u^2 (M3 + ...)), within 7.9e-7 (fitted for the least
+// largest error): one and two instructions more than for the small ones, against an exponential and a reciprocal at a quarter of the rate.
+constexpr float N1 = 0.99998862f, N3 = -0.33292374f, N5 = 0.12931657f, N7 = -0.03883829f;
 constexpr float M1 = 0.99999005f, M3 = -0.33305562f, M5 = 0.13114086f, M7 = -0.04667219f, M9 = 0.01031595f;
 template <Cap CAP, int TIER>
 __device__ __forceinline__ float score8(const Attn8& p, float u, float t) {
@@ -119,7 +121,8 @@ __device__ __forceinline__ float score8(const Attn8& p, float u, float t) {
   const float w = u * u;
   if constexpr (CAP == CAP_NEAR) {
     if constexpr (TIER == 0) return fmaf(u, fmaf(w, fmaf(w, p.poly5, p.poly3), p.poly1), t);
-    if constexpr (TIER == 1) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, fmaf(w, p.mid[4], p.mid[3]), p.mid[2]), p.mid[1]), p.mid[0]), t);
+    if constexpr (TIER == 1) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, p.low[3], p.low[2]), p.low[1]), p.low[0]), t);
+    if constexpr (TIER == 2) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, fmaf(w, p.mid[4], p.mid[3]), p.mid[2]), p.mid[1]), p.mid[0]), t);
     return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b + t);
   }
   float x = u * p.cap_b * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
@@ -137,8 +140,10 @@ __device__ __forceinline__ void with_tier(float size, F&& f) {
       f(std::integral_constant<int, 0>());
     else if (CAP == CAP_NEAR && !__any(!(size <= TIERS[1])))
       f(std::integral_constant<int, 1>());
-    else
+    else if (CAP == CAP_NEAR && !__any(!(size <= TIERS[2])))
       f(std::integral_constant<int, 2>());
+    else
+      f(std::integral_constant<int, 3>());
   }
 }
 // The distance's part of a score: dist < 2^10 as an fp16 number below the normal range is dist 2^-24, which the mixed
@@ -401,7 +406,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
           const int at_key = 16 * n + 4 * g4 + e;
           const int4 k = make_int4(__shfl(of_lane.x, at_key), __shfl(of_lane.y, at_key), __shfl(of_lane.z, at_key), __shfl(of_lane.w, at_key));
           const bool in = tokens >> at_key & 1 && k.w == own_volume && k.x <= last;
-          const float x = score8<CAP, 2>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
+          const float x = score8<CAP, 3>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
           z[n][e] = in ? x : -INFINITY;
           most = fmaxf(most, z[n][e]);
         }
@@ -694,7 +699,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
           const int key = 32 * n + 8 * (e >> 2) + 4 * half + (e & 3);
           const int4 k = t.sites[key];
           const bool in = tokens >> key & 1 && k.w == own_volume && k.x <= last;
-          const float x = score8<CAP, 2>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
+          const float x = score8<CAP, 3>(p, z[n][e], bias ? fmaf((float)distance(at, k), slope, -top) : -top);
           z[n][e] = in ? x : -INFINITY;
           most = fmaxf(most, z[n][e]);
           if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // four keys' sites in registers at a time
@@ -1003,6 +1008,7 @@ extern "C" pd_status predecoder_attention8(void* hip_stream, const pd_attention8
   const float factor = cap == CAP_NONE ? a->scale * LOG2E : a->scale / most_cap;
   p.factor = fminf(fmaxf(factor, -FLT_MAX), FLT_MAX);
   p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
+  p.low[0] = p.cap_b * N1, p.low[1] = p.cap_b * N3, p.low[2] = p.cap_b * N5, p.low[3] = p.cap_b * N7;
   p.mid[0] = p.cap_b * M1, p.mid[1] = p.cap_b * M3, p.mid[2] = p.cap_b * M5, p.mid[3] = p.cap_b * M7, p.mid[4] = p.cap_b * M9;
   p.poly1 = p.cap_b * TANH1, p.poly3 = p.cap_b * TANH3, p.poly5 = p.cap_b * TANH5;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;

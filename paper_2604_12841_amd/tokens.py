@@ -298,13 +298,13 @@ def rope(x, sites, out, sections, base=10000.0, interleaved=False, inverse=False
 def _call_with_workspace(name, pack, a, q, workspace, stream):
     """Calls `name` with the packed arguments `a`, a workspace and its size; the workspace is the caller's or allocated here."""
     dev = q.get_device()
-    ptr = 0
     if workspace is not None:
         _need(workspace.get_device() == dev and workspace.is_contiguous(),
               "workspace must be a contiguous tensor on the GPU of q")
-        ptr, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        packed = pack(*a, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     else:
-        need = _by_bytes(name + "_workspace")(pack(*a, 0, 0))
+        packed = pack(*a, 0, 0)
+        need = _by_bytes(name + "_workspace")(packed)
         if need:
             if stream is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
@@ -312,8 +312,20 @@ def _call_with_workspace(name, pack, a, q, workspace, stream):
                 _need(isinstance(stream, torch.cuda.Stream), "a raw stream handle needs a workspace from the caller")
                 with torch.cuda.stream(stream):  # its memory goes back to the stream that uses it
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            ptr = workspace.data_ptr()
-    _call(name, pack(*a, ptr, need), stream, dev)
+            packed = pack(*a, workspace.data_ptr(), need)
+    _call(name, packed, stream, dev)
+
+
+def _heads(t, what, shape, dtype, index, fields):
+    """Appends the pointer and strides of a tensor [batch][tokens][heads][head_dim] with contiguous rows."""
+    if t.get_device() != index or t.dtype is not dtype or t.shape != shape:
+        raise ValueError("%s must be a %s tensor %s on GPU %d" % (what, dtype, tuple(shape), index))
+    if t.requires_grad:
+        _lost_gradient(what)
+    sb, st, sh, one = t.stride()
+    if one != 1 and shape[3] > 1:
+        raise ValueError("the rows of a head must be contiguous in %s" % what)
+    fields += (t.data_ptr(), sb, st, sh)
 
 
 def _attention_args(q, k, v, out, q_sites, k_sites, scale, cap, slopes, causal, prefix):
@@ -403,15 +415,8 @@ def _cache_call(name, cache, at, k, v, sites, stream):
     if at.get_device() != dev or at.dtype != torch.int64 or at.shape != (B,) or not at.is_contiguous():
         raise ValueError("at must be a contiguous vector of %d int64 values on GPU %d" % (B, dev))
     fields = []
-    for t, what in ((k, "k"), (v, "v")):
-        if t.get_device() != dev or t.dtype != dt or t.shape != shape:
-            raise ValueError("%s must be a %s tensor %s on GPU %d" % (what, dt, tuple(shape), dev))
-        if t.requires_grad:
-            _lost_gradient(what)
-        sb, st, sh, one = t.stride()
-        if one != 1 and D > 1:
-            raise ValueError("the rows of a head must be contiguous in %s" % what)
-        fields += (t.data_ptr(), sb, st, sh)
+    _heads(k, "k", shape, dt, dev, fields)
+    _heads(v, "v", shape, dt, dev, fields)
     ps = bs = 0
     if sites is not None:
         ps, bs = _sites(sites, "sites", n, dev, B)
@@ -444,15 +449,8 @@ def _attention8_args(q, cache, out, q_sites, scale, cap, slopes, causal, prefix)
     if B != c[0] or D != c[2]:
         raise ValueError("q has shape %s, and the cache %s" % (tuple(shape), tuple(cache[0].shape)))
     fields = []
-    for t, what in ((q, "q"), (out, "out")):
-        if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != shape:
-            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(shape)))
-        if t.requires_grad:
-            _lost_gradient(what)
-        sb, st, sh, one = t.stride()
-        if one != 1 and D > 1:
-            raise ValueError("the rows of a head must be contiguous in %s" % what)
-        fields += (t.data_ptr(), sb, st, sh)
+    _heads(q, "q", shape, torch.bfloat16, dev, fields)
+    _heads(out, "out", shape, torch.bfloat16, dev, fields)
     pq, bq = _sites(q_sites, "q_sites", nq, dev, B)
     return (*c, H, nq, D ** -0.5 if scale is None else scale, cap, bool(causal), PREFIX_NONE if prefix is None else int(prefix), *fields, pq, bq,
             _vector(slopes, "slopes", H, dev))
@@ -478,17 +476,15 @@ def _linear_args(q, k, v, out, slopes, per_round, lengths, state, state_out, sca
     _need(per_round < 1 << 31, "per_round must be below 2^31")
     shape, dev = q.shape, _index(q, "q")
     B, n, H, D = shape
-    Hk = k.shape[2]
+    kv = k.shape
+    Hk = kv[2]
+    if kv != (B, n, Hk, D):
+        raise ValueError("k has shape %s, expected %s" % (tuple(kv), (B, n, Hk, D)))
     fields = []
-    for t, what, want in ((q, "q", shape), (k, "k", (B, n, Hk, D)), (v, "v", (B, n, Hk, D)), (out, "out", shape)):
-        if t.get_device() != dev or t.dtype != torch.bfloat16 or t.shape != want:
-            raise ValueError("%s must be a bfloat16 tensor %s on the GPU of q" % (what, tuple(want)))
-        if t.requires_grad:
-            _lost_gradient(what)
-        sb, st, sh, one = t.stride()
-        if one != 1 and D > 1:
-            raise ValueError("the rows of a head must be contiguous in %s" % what)
-        fields += (t.data_ptr(), sb, st, sh)
+    _heads(q, "q", shape, torch.bfloat16, dev, fields)
+    _heads(k, "k", kv, torch.bfloat16, dev, fields)
+    _heads(v, "v", kv, torch.bfloat16, dev, fields)
+    _heads(out, "out", shape, torch.bfloat16, dev, fields)
     pl = 0
     if lengths is not None:
         if lengths.get_device() != dev or lengths.dtype != torch.int32 or lengths.shape != (B,) or not lengths.is_contiguous():
