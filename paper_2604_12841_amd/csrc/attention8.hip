@@ -517,8 +517,12 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   constexpr int NT = NW * 64;
   constexpr int GR = DP / 16;  // granules of a row
   constexpr int AHEAD = 16;    // tiles whose sites are looked at together
+  // Queries past 64 channels wait in LDS: in registers they made others spill (54 at 128 channels, 15 now; 196 tokens against four
+  // caches of up to 100 rounds, 8 (2) x 128: 173 us against 184).  At 64 channels nothing spills (205 us; from LDS 209).
+  constexpr bool LDS_Q = DP > 64;
   __shared__ KeyTile<DP> tiles[2];
   __shared__ KeyNotes notes;
+  __shared__ u32x4 lds_q[LDS_Q ? DP / 16 : 1][NT];  // each thread's own
   __shared__ int lq[3][NW];
   __shared__ int visible[AHEAD];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
@@ -526,7 +530,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   if (!item_of(p, item)) return;
   const int kvh = item.kvh, b = item.b;
   const int row = item.row_tile * 128 + wave * 32 + (lane & 31);
-  const bool idle = item.row_tile * 128 + wave * 32 >= p.rows;  // a wave without rows only sends for its part of the tiles
+  const bool idle = item.row_tile * 128 + wave * 32 >= p.rows;  // a wave without rows sees nothing and sends for its part of the tiles
   const int r = row < p.rows ? row : p.rows - 1;  // rows past the end repeat the last: not stored
   const int token = r / p.group, head = kvh * p.group + r % p.group;
   const uint16_t* q = p.q + b * p.q_b + token * p.q_t + head * p.q_h;
@@ -535,13 +539,22 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   const uint8_t* vb = p.codes + v_row * p.head_dim;
   const int4* sites = p.sites + (long long)b * p.capacity;
   // step 2 s + c of a product takes channels 32 s + 16 half + 8 c on: a lane's granule of K in two
-  bf16x8 fq[DP / 16];
+  bf16x8 fq[LDS_Q ? 1 : DP / 16];
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
     const int d = 32 * (s >> 1) + 16 * half + 8 * (s & 1);
     const uint4 w = d < p.head_dim ? *(const uint4*)(q + d) : make_uint4(0, 0, 0, 0);
-    fq[s] = __builtin_bit_cast(bf16x8, w);
+    if constexpr (LDS_Q)
+      lds_q[s][tid] = __builtin_bit_cast(u32x4, w);
+    else
+      fq[s] = __builtin_bit_cast(bf16x8, w);
   }
+  auto query = [&](int s) {
+    if constexpr (LDS_Q)
+      return __builtin_bit_cast(bf16x8, lds_q[s][tid]);
+    else
+      return fq[s];
+  };
   const int4 at = p.q_sites[b * p.q_sites_b + token];
   const int own_volume = at.w >= 0 ? at.w : -2;                    // -2: no key's volume
   const int last = p.causal ? max(at.x, p.prefix_last) : INT_MAX;  // the last round that the row sees
@@ -550,7 +563,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   const float slope = slope_of(p, head);
 
   // what this wave's rows see, and the workgroup's
-  const Seen seen = seen_by(p, at);
+  const Seen seen = seen_by(p, make_int4(at.x, at.y, at.z, idle ? -1 : at.w));
   Seen any = seen;
   if (lane == 0) lq[0][wave] = seen.vmin, lq[1][wave] = seen.vmax, lq[2][wave] = seen.last;
   __syncthreads();
@@ -635,7 +648,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
     const float vs = t.vs[lane];
     const uint64_t tokens = __ballot(held);
     const bool whole = __all(held && seen.all(site, bias));
-    if (idle || !__any(held && seen.some(site))) return;
+    if (!__any(held && seen.some(site))) return;
     const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
     // (the waves write the same)
     notes.f[lane] = t.ks[lane] * p.factor;
@@ -645,14 +658,17 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
 
     f32x16 z[2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int e = 0; e < 16; ++e) z[n][e] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < DP / 32; ++c) {
+    for (int c = 0; c < DP / 32; ++c) {
+      const bf16x8 first = query(2 * c), second = query(2 * c + 1);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
         const uint4 w = *(const uint4*)(t.k + k_off[c] + 32 * n * DP);
-        z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>(w.x, w.y), fq[2 * c], z[n], 0, 0, 0);
-        z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>(w.z, w.w), fq[2 * c + 1], z[n], 0, 0, 0);
+        z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>(w.x, w.y), first, z[n], 0, 0, 0);
+        z[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>(w.z, w.w), second, z[n], 0, 0, 0);
       }
     }
     float size = 0.0f;
@@ -750,6 +766,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
           if constexpr (carefully.value) w[0] &= keep[0], w[1] &= keep[1];
           o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>((uint32_t)w[0], (uint32_t)w[1]), pr, o[m], 0, 0, 0);
         }
+        if constexpr (LDS_Q) __builtin_amdgcn_sched_barrier(0);  // (reads of the next columns would spill)
       }
     };
     if (careful)
