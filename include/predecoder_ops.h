@@ -268,9 +268,10 @@ pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args);
  * queries that see nothing), of q over the tokens of a cache: keys and values are
  * code scale, not rounded in between.  Scores, maximum and sum are fp32; a
  * probability times a value's scale is rounded to bf16 (2^-8) for the product with the
- * values' codes, or for up to 64 rows (n_q heads / kv_heads) kept to 16 bits.  A visible row with scale NaN makes the result NaN; what invisible places
- * hold does not reach it (but E4M3's NaN codes, which predecoder_cache_write never
- * writes, may stand only where there is no token).
+ * values' codes, or for up to 64 rows (n_q heads / kv_heads) kept to 16 bits.  A visible
+ * row with scale NaN makes the result NaN; what invisible places hold does not reach it
+ * (but E4M3's NaN codes, which predecoder_cache_write never writes, may stand only where
+ * there is no token).
  * q and out as there: bf16, all rows 16-byte aligned; heads a multiple of
  * cache.kv_heads, heads / kv_heads <= 64; |coordinate| < 2^29.  q_sites is needed unless n_q
  * is 0.  workspace as there.  A cap is met within 2^-20 of the score or of the cap. */
@@ -312,6 +313,8 @@ pd_status predecoder_attention8(void* hip_stream, const pd_attention8_args* args
  * entry of length 0 passes its state on.  A last round that is not whole counts
  * as a round.
  * slopes [kv_heads] (NULL: 0): the decay of a round; infinite: only its own round.
+ * A value of q, k, v or the state that is not finite makes the results that take it in
+ * infinite or NaN, all rounds' from its own on; those before it are as without it.
  * bf16 q, k, v and out; sums and states fp32 (products of bf16 parts that hold 24
  * bits of what is decayed), the weights of pairs inside a chunk and the state's part
  * of a result taken to 16 bits or more, out rounded once.

@@ -13,13 +13,13 @@
 // Few rows (up to 64): the eight waves of a workgroup take the same 16 rows and
 // every eighth tile, without a barrier; K comes straight into registers, V to
 // LDS, a tile ahead; at the end they join.  Sixteen streams of up to 65536
-// places, 8 query and 2 key heads of 128, int8: 102 us, 4.4 TB/s (the same loads
+// places, 8 query and 2 key heads of 128, int8: 88 us, 4.9 TB/s (the same loads
 // without any work on them: 84 us).  One token against four caches of up to 200
-// rounds of d = 13, 8 (2) heads of 64, E4M3: 14.5 us and 4 us of the join.
+// rounds of d = 13, 8 (2) heads of 64, E4M3: 14.6 us and 4 us of the join.
 //
 // Many rows: 128 a workgroup, 32 a wave, which share tiles in LDS.  Bound by
 // vector instructions, about 14 a score with cap and bias: 196 tokens against the same
-// four caches 197 us and 8 us of the join (260 TFLOP/s; vector units 0.53 busy
+// four caches 196 us and 8 us of the join (260 TFLOP/s; vector units 0.54 busy
 // without what the exponentials take longer, matrix units 0.11).
 //
 // What to read: before the keys of 8 (16) tiles the sites are read, and tiles

@@ -18,7 +18,7 @@
 //   out_i = w^(t_i + 1) q_i S + sum over t_j <= t_i of w^(t_i - t_j) (q_i.k_j) v_j;
 //   then S = w^R S + sum of w^(R - 1 - t_j) k_j v_j^T.  The weighted keys are split
 //   into three bf16 parts (24 bits: two would leave the state off by 2^-18 of itself), weighted pairs into
-//   two.  8 rows of up to 4097 single-token rounds, 6 heads of 64: 35 us, a chain of latencies
+//   two.  8 rows of up to 4097 single-token rounds, 6 heads of 64: 33 us, a chain of latencies
 //   for each tile (vector units 0.33, LDS 0.34 busy).
 //
 // Few entries and heads against many rounds: the rounds are cut into segments.
