@@ -852,8 +852,13 @@ pd_status check(const pd_linear_attention_args* a, bool pointers) {
   // work items, and the scan's, are counted by the launches (threads below 2^32)
   if ((__int128)a->kv_heads * a->batch >= 1ll << 17 || plan_for(a).items >= 1ll << 22) return PD_ERR_UNSUPPORTED;
   if ((__int128)a->n * (a->kv_heads ? a->heads / a->kv_heads : 1) >= 1ll << 30) return PD_ERR_UNSUPPORTED;  // rows, in 32 bits
-  if (!pointers || !a->batch || !a->heads) return PD_OK;
+  if (!pointers || !a->batch) return PD_OK;
+  if (!a->heads) return a->kv_heads && a->state_out ? PD_ERR_INVALID_ARG : PD_OK;  // (states without a query: not handed on)
   if ((uintptr_t)a->slopes % 4 || (uintptr_t)a->lengths % 4 || (uintptr_t)a->state % 16 || (uintptr_t)a->state_out % 16) return PD_ERR_INVALID_ARG;
+  if (a->state && a->state_out && a->state != a->state_out) {
+    const uintptr_t x = (uintptr_t)a->state, y = (uintptr_t)a->state_out;
+    if ((x < y ? y - x : x - y) < (size_t)a->batch * a->kv_heads * a->head_dim * a->head_dim * 4) return PD_ERR_INVALID_ARG;
+  }
   if (!a->n) return PD_OK;
   if (!a->q || !a->k || !a->v || !a->out || a->out == a->q || a->out == a->k || a->out == a->v) return PD_ERR_INVALID_ARG;
   if (!rows16(a->q, a->q_batch_stride, a->q_token_stride, a->q_head_stride) ||

@@ -399,8 +399,8 @@ def _cache_args(cache, index):
         raise ValueError("the cache must be on GPU %d" % index)
     if not (codes.is_contiguous() and scales.is_contiguous() and sites.is_contiguous()):
         raise ValueError("the cache's tensors must be contiguous")
-    if scales.requires_grad:
-        _lost_gradient("the cache's scales")
+    if codes.requires_grad or scales.requires_grad:
+        _lost_gradient("the cache's codes" if codes.requires_grad else "the cache's scales")
     return B, Hk, D, cap, _CODES[dt], codes.data_ptr(), scales.data_ptr(), sites.data_ptr()
 
 

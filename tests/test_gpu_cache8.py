@@ -181,3 +181,10 @@ def test_refusals():
         pdx.cache_read(cache, at, k, k.clone(), sites)
     with pytest.raises(ValueError):
         pdx.new_cache(1, 1, 1, 16, "fp4")
+
+
+def test_codes_that_want_a_gradient_are_refused():
+    codes, scales, sites = pdx.new_cache(2, 8, 2, 32)
+    q = torch.zeros(2, 4, 2, 32, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        pdx.attention8(q, (codes.requires_grad_(), scales, sites), torch.empty_like(q), torch.zeros(4, 4, dtype=torch.int32, device="cuda"))

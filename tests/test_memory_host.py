@@ -98,6 +98,18 @@ def test_linear_refusals(want, kw):
     assert linear(**kw) == want
 
 
+def test_linear_states_apart():
+    """state_out is state itself or lies apart from it, also where no token comes; without a query head no state is handed on."""
+    size = 2 * 2 * 64 * 64 * 4  # of the batch, key heads and head size of linear()
+    for n in (0, 1, 5):
+        for off in (64, size - 16):
+            assert linear(n=n, state=16 * P, state_out=16 * P + off) == BAD
+            assert linear(n=n, state=16 * P + off, state_out=16 * P) == BAD
+    for state in (None, 16 * P):
+        assert linear(heads=0, state=state, state_out=32 * P) == BAD
+    assert linear(heads=0, state=16 * P) == 0 and linear(heads=0, kv_heads=0, state=16 * P, state_out=16 * P) == 0
+
+
 LONG = dict(batch=1, heads=2, kv_heads=2, head_dim=64, n=100000, per_round=4, scale=0.1)
 
 
