@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
     }
     const int rr = item.row_tile * 16 + i;
     if (p.splits > 1) {
-      if (best != -INFINITY) *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;  // (the join leaves out splits of weight 0)
+      if (best != -INFINITY) *(float4*)(p.part_o + (rows_at + rr) * DP + d) = acc;  // (the join does not read it otherwise)
       if (d == 0) p.part_ml[rows_at + rr] = make_float2(best, sum);
     } else if (d < p.head_dim) {
       const float inv = inverse(sum);
@@ -794,7 +794,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   if (p.splits > 1) {
     const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
     const long long rows_at = (((long long)item.split * p.batch + b) * p.kv_heads + kvh) * p.rows;
-    if (!none) {  // (the join leaves out splits of weight 0)
+    if (!none) {  // (the join does not read it otherwise)
 #pragma unroll
       for (int m = 0; m < DP / 32; ++m)
 #pragma unroll
@@ -821,7 +821,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
 }
 
 // Joins the splits of one row: out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.  The weights first, one split a thread; then
-// DP / 4 lanes read a split's row, and the workgroup's groups of them take splits in turn.
+// DP / 4 lanes read a split's row, and the workgroup's groups of them take splits in turn.  A split in which the row saw
+// nothing (m_s = -infinity) left no result, and is not read.  Any other one is, also where its weight is 0 in fp32: what it
+// saw may be NaN, and so is the row then.
 template <int DP>
 __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
   constexpr int L = DP / 4, GROUPS = 256 / L;
@@ -839,9 +841,10 @@ __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
   if ((tid & 63) == 0) sm[tid >> 6].x = top;
   __syncthreads();
   top = fmaxf(fmaxf(sm[0].x, sm[1].x), fmaxf(sm[2].x, sm[3].x));
-  const float w = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);  // 0: the row saw nothing there
-  float total = ml.x == -INFINITY ? 0.0f : ml.y * w;
-  weight[tid] = w;
+  const bool none = ml.x == -INFINITY;
+  const float w = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+  float total = none ? 0.0f : ml.y * w;
+  weight[tid] = none ? -1.0f : w;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
   if ((tid & 63) == 0) sm[tid >> 6].y = total;
@@ -851,7 +854,7 @@ __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
 #pragma unroll 4
   for (int s = g; s < p.splits; s += GROUPS) {
     const float a = weight[s];
-    const float4 o = a == 0.0f ? make_float4(0, 0, 0, 0) : *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    const float4 o = a == -1.0f ? make_float4(0, 0, 0, 0) : *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
     acc.x = fmaf(o.x, a, acc.x), acc.y = fmaf(o.y, a, acc.y), acc.z = fmaf(o.z, a, acc.z), acc.w = fmaf(o.w, a, acc.w);
   }
   so[g][lane] = acc;
@@ -885,10 +888,11 @@ __global__ void __launch_bounds__(256) attention8_join_few_kernel(const Attn8 p)
 #pragma unroll 4
   for (int s = 0; s < p.splits; ++s) {
     const float2 ml = p.part_ml[s * step + item];
-    const float w = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);  // 0: the row saw nothing there
-    const float4 o = w == 0.0f ? make_float4(0, 0, 0, 0) : *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
+    const bool none = ml.x == -INFINITY;
+    const float w = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    const float4 o = none ? make_float4(0, 0, 0, 0) : *(const float4*)(p.part_o + (s * step + item) * DP + 4 * lane);
     acc.x = fmaf(o.x, w, acc.x), acc.y = fmaf(o.y, w, acc.y), acc.z = fmaf(o.z, w, acc.z), acc.w = fmaf(o.w, w, acc.w);
-    total = w == 0.0f ? total : fmaf(ml.y, w, total);
+    total = none ? total : fmaf(ml.y, w, total);
   }
   const int row = (int)(item % p.rows), kvh = (int)(item / p.rows % p.kv_heads), b = (int)(item / p.rows / p.kv_heads);
   const float inv = inverse(total);
