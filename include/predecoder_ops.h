@@ -274,7 +274,9 @@ pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args);
  * there is no token).
  * q and out as there: bf16, all rows 16-byte aligned; heads a multiple of
  * cache.kv_heads, heads / kv_heads <= 64; |coordinate| < 2^29.  q_sites is needed unless n_q
- * is 0.  workspace as there.  A cap is met within 2^-20 of the score or of the cap. */
+ * is 0.  workspace as there.  A cap is met within 2^-20 of the score or of the cap.
+ * PD_ERR_UNSUPPORTED where rows (n_q heads / kv_heads) reach 2^30 or the launch 2^32 threads (512 for
+ * each 16 rows of a key head up to 64 rows, 256 for each 128 above, times the splits). */
 typedef struct pd_attention8_args {
   pd_cache cache;
   int32_t heads, n_q;

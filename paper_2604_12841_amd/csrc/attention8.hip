@@ -901,6 +901,9 @@ __global__ void __launch_bounds__(256) attention8_join_few_kernel(const Attn8 p)
   *(uint2*)(p.out + b * p.o_b + row / p.group * p.o_t + (kvh * p.group + row % p.group) * p.o_h + 4 * lane) = v;
 }
 
+// Threads of a workgroup.
+constexpr int threads_of(bool few) { return (few ? FW : NW) * 64; }
+
 // How a call runs.
 struct Plan {
   bool few;
@@ -951,10 +954,10 @@ pd_status check(const pd_attention8_args* a, bool pointers) {
   if (a->heads && (!c.kv_heads || a->heads % c.kv_heads)) return PD_ERR_INVALID_ARG;
   if (a->heads && a->heads / c.kv_heads > 64) return PD_ERR_UNSUPPORTED;
   if (a->heads && c.batch && a->n_q) {
-    // rows are counted in 32 bits, work items and rows of all heads by the launches (threads below 2^32)
+    // rows are counted in 32 bits, work items and rows of all heads by the launches (threads below 2^32, a join's 256 a row)
     if ((long long)a->n_q * (a->heads / c.kv_heads) >= 1ll << 30) return PD_ERR_UNSUPPORTED;
     const Plan n = plan_for(a);
-    if (n.items > (1ll << 24) - 8 * RUN || (n.splits > 1 && (__int128)a->n_q * a->heads * c.batch >= 1ll << 24)) return PD_ERR_UNSUPPORTED;
+    if (n.items > (1ll << 32) / threads_of(n.few) - 8 * RUN || (n.splits > 1 && (__int128)a->n_q * a->heads * c.batch >= 1ll << 24)) return PD_ERR_UNSUPPORTED;
   }
   if (!pointers || !c.batch || !a->heads || !a->n_q) return PD_OK;
   if (!a->q || !a->out || !a->q_sites || a->out == a->q) return PD_ERR_INVALID_ARG;
@@ -972,7 +975,7 @@ pd_status check(const pd_attention8_args* a, bool pointers) {
 
 template <int DP, bool INT8, Cap CAP>
 void launch(const Attn8& p, bool few, hipStream_t st) {
-  const dim3 blocks((p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)), threads((few ? FW : NW) * 64);
+  const dim3 blocks((p.items + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)), threads(threads_of(few));
   if (few)
     hipLaunchKernelGGL((attention8_few_kernel<DP, INT8, CAP>), blocks, threads, 0, st, p);
   else
