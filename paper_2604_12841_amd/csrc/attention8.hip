@@ -210,6 +210,12 @@ __device__ __forceinline__ float slope_of(const Attn8& p, int head) {
   return slope;
 }
 
+// A key's scale times p.factor: finite for finite scales, so that scores of zero stay zero.
+__device__ __forceinline__ float factor_of(const Attn8& p, float scale) {
+  const float f = scale * p.factor;
+  return fabsf(f) == INFINITY && fabsf(scale) < INFINITY ? copysignf(FLT_MAX, f) : f;
+}
+
 struct Item {
   int row_tile, split, kvh, b;
 };
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
     const uint64_t tokens = __ballot(held);
     const bool whole = __all(held && seen.all(site, bias));
     const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
-    notes.f[lane] = ks * p.factor;
+    notes.f[lane] = factor_of(p, ks);
     notes.v[lane] = held ? vs : 0.0f;
     notes.bytes[lane] = site_bytes(site);
     const int4 of_lane = site;
@@ -651,7 +657,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
     if (!__any(held && seen.some(site))) return;
     const bool careful = !whole && (tokens != ~0ull || __any(held && !(fabsf(vs) < INFINITY)));
     // (the waves write the same)
-    notes.f[lane] = t.ks[lane] * p.factor;
+    notes.f[lane] = factor_of(p, t.ks[lane]);
     notes.v[lane] = held ? vs : 0.0f;
     notes.bytes[lane] = site_bytes(site);
     __builtin_amdgcn_wave_barrier();

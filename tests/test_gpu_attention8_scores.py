@@ -131,3 +131,21 @@ def test_rows_of_rounds_on_both_sides_of_a_border():
         q = (3.0 * tc.normal(g, 1, m, 4, 64)).to(torch.bfloat16)
         at = torch.arange(m, device="cuda") * 180 // m
         check(q, cache, q_sites[:, at].contiguous(), cap=30.0, slopes=torch.tensor([0.5, 0.1, 0.01, -0.05], device="cuda"), causal=True)
+
+
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("n", [1, 70])
+def test_scores_of_zero_under_the_smallest_caps(codes, n):
+    """Keys up to 3e38 with queries of zeros: the key's scale over the cap leaves fp32's range, the scores are 0, and every value counts the same."""
+    g = tc.gen(53)
+    cache = mc.filled_cache(g, 1, 200, 1, 64, codes, torch.zeros(1, 200, 4, dtype=torch.int32, device="cuda"))
+    cache[1][:, 0] = 3e38 / mc.QMAX[CODES[codes]]
+    q_sites = torch.zeros(1, n, 4, dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, n, 2, 64, dtype=torch.bfloat16, device="cuda")
+    v = mc.by_token(cache)[1][0].mean(0)
+    for cap, scale in ((1e-5, 0.125), (0.0, 1e6)):
+        out = torch.empty_like(q)
+        pdx.attention8(q, cache, out, q_sites, cap=cap, scale=scale)
+        torch.cuda.synchronize()
+        moved = mc.by_token(cache)[1][0].abs().mean(0)
+        assert torch.all((out.double() - v).abs() <= U16 * v.abs() + (U16 + 260 * U32) * 1.01 * moved)
