@@ -53,8 +53,9 @@ struct Attn8 {
   int row_tiles, splits, tiles_per_split;
   int causal, prefix_last;  // prefix - 1; INT_MIN, below every round: none
   // a score of product x and key scale s, in log2 units: s factor x, or with the cap, for u = s factor x:
-  // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for small |u| polynomials
-  float factor, cap_a, cap_b, poly1, poly3, poly5, low[4], mid[5];
+  // cap_b + cap_a / (1 + 2^(2 log2(e) u)), and for small |u| polynomials.  (CAP_FAR: u = unit s factor x, factor as without a cap:
+  // scale / cap, times a key's scale, would lose its last bits below fp32's range.)
+  float factor, unit, cap_a, cap_b, poly1, poly3, poly5, low[4], mid[5];
   const uint16_t* q;
   uint16_t* out;
   long long q_b, q_t, q_h, o_b, o_t, o_h;
@@ -108,8 +109,8 @@ __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
 }
 
-// A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u.
-// TIER: |u| is at most TIERS[TIER], or 3: anything.
+// A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u
+// (CAP_FAR: u before the cap, cap_b tanh(unit u)).  TIER: |u| (unit |u|) is at most TIERS[TIER], or 3: anything.
 constexpr float TIERS[3] = {0.35f, 0.62f, 0.87f};
 // tanh u for |u| <= 0.62 is u (N1 + u^2 (N3 + ...)), for |u| <= 0.87 u (M1 + u^2 (M3 + ...)), within 7.9e-7 (fitted for the least
 // largest error): one and two instructions more than for the small ones, against an exponential and a reciprocal at a quarter of the rate.
@@ -118,21 +119,22 @@ constexpr float M1 = 0.99999005f, M3 = -0.33305562f, M5 = 0.13114086f, M7 = -0.0
 template <Cap CAP, int TIER>
 __device__ __forceinline__ float score8(const Attn8& p, float u, float t) {
   if constexpr (CAP == CAP_NONE) return u + t;
-  const float w = u * u;
+  const float y = CAP == CAP_FAR ? u * p.unit : u, w = y * y;
   if constexpr (CAP == CAP_NEAR) {
     if constexpr (TIER == 0) return fmaf(u, fmaf(w, fmaf(w, p.poly5, p.poly3), p.poly1), t);
     if constexpr (TIER == 1) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, p.low[3], p.low[2]), p.low[1]), p.low[0]), t);
     if constexpr (TIER == 2) return fmaf(u, fmaf(w, fmaf(w, fmaf(w, fmaf(w, p.mid[4], p.mid[3]), p.mid[2]), p.mid[1]), p.mid[0]), t);
     return fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b + t);
   }
-  float x = u * p.cap_b * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
+  float x = u * fmaf(w, fmaf(w, fmaf(w, TANH7R, TANH5R), TANH3R), 1.0f);
   if constexpr (TIER > 0)
-    x = fabsf(u) <= 0.35f ? x : fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * LOG2E))), p.cap_b);
+    x = fabsf(y) <= 0.35f ? x : fmaf(p.cap_a, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * (2.0f * LOG2E))), p.cap_b);
   return x + t;
 }
 // Calls f with the tier of a wave's largest |u|.
 template <Cap CAP, typename F>
-__device__ __forceinline__ void with_tier(float size, F&& f) {
+__device__ __forceinline__ void with_tier(const Attn8& p, float size, F&& f) {
+  if constexpr (CAP == CAP_FAR) size *= p.unit;
   if constexpr (CAP == CAP_NONE) {
     f(std::integral_constant<int, 0>());
   } else {
@@ -392,7 +394,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
     }
     float most = -INFINITY;
     if (whole) {
-      with_tier<CAP>(size, [&](auto tier) {
+      with_tier<CAP>(p, size, [&](auto tier) {
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const uint4 w = *(const uint4*)&notes.bytes[16 * n + 4 * g4];
@@ -691,7 +693,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
       }
     float most = -INFINITY;
     if (whole) {
-      with_tier<CAP>(size, [&](auto tier) {
+      with_tier<CAP>(p, size, [&](auto tier) {
         auto scores = [&](auto biased) {
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -1035,9 +1037,9 @@ extern "C" pd_status predecoder_attention8(void* hip_stream, const pd_attention8
   // (caps past 2^126, whose double would leave the range, differ from it for scores that are themselves of such size alone)
   const float most_cap = fminf(a->cap, 0x1p126f);
   // kept finite, so that scores of zero stay zero
-  const float factor = cap == CAP_NONE ? a->scale * LOG2E : a->scale / most_cap;
+  const float factor = cap == CAP_NEAR ? a->scale / most_cap : a->scale * LOG2E;
   p.factor = fminf(fmaxf(factor, -FLT_MAX), FLT_MAX);
-  p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E;
+  p.cap_a = -2.0f * most_cap * LOG2E, p.cap_b = most_cap * LOG2E, p.unit = cap == CAP_FAR ? 1.0f / p.cap_b : 0.0f;
   p.low[0] = p.cap_b * N1, p.low[1] = p.cap_b * N3, p.low[2] = p.cap_b * N5, p.low[3] = p.cap_b * N7;
   p.mid[0] = p.cap_b * M1, p.mid[1] = p.cap_b * M3, p.mid[2] = p.cap_b * M5, p.mid[3] = p.cap_b * M7, p.mid[4] = p.cap_b * M9;
   p.poly1 = p.cap_b * TANH1, p.poly3 = p.cap_b * TANH3, p.poly5 = p.cap_b * TANH5;

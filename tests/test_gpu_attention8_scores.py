@@ -149,3 +149,23 @@ def test_scores_of_zero_under_the_smallest_caps(codes, n):
         torch.cuda.synchronize()
         moved = mc.by_token(cache)[1][0].abs().mean(0)
         assert torch.all((out.double() - v).abs() <= U16 * v.abs() + (U16 + 260 * U32) * 1.01 * moved)
+
+
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("n", [1, 70])
+def test_scores_under_the_largest_caps(codes, n):
+    """Caps that no score comes near change nothing, whatever the keys' scales."""
+    g = tc.gen(54)
+    cache = mc.filled_cache(g, 1, 300, 2, 64, codes, torch.zeros(1, 300, 4, dtype=torch.int32, device="cuda"))
+    cache[1][:, 0] *= 1e-5
+    q = (2e5 * tc.normal(g, 1, n, 2, 64)).to(torch.bfloat16)
+    q_sites = torch.zeros(1, n, 4, dtype=torch.int32, device="cuda")
+    for cap in (1e30, 1e38, 3.4e38):
+        out = torch.empty_like(q)
+        pdx.attention8(q, cache, out, q_sites, cap=cap)
+        torch.cuda.synchronize()
+        # (such a cap is its own limit: tanh u = u)
+        want, moved, score = tc.attention64(q, *mc.by_token(cache), q_sites, cache[2], 0.125, 0.0, None, False, -(1 << 31))
+        z = (q.double().abs().amax() * mc.by_token(cache)[0].abs().amax()) * 64 * 0.125
+        bound = tc.attention_tolerance(want, moved, score + (2.0 ** -20 + 4 * U32) * float(z))
+        assert torch.all((out.double() - want).abs() <= bound)
