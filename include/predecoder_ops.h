@@ -321,8 +321,9 @@ pd_status predecoder_attention8(void* hip_stream, const pd_attention8_args* args
  * bits of what is decayed), the weights of pairs inside a chunk and the state's part
  * of a result taken to 16 bits or more, out rounded once.
  * head_dim: a multiple of 8, at most 128; all rows 16-byte aligned; heads a multiple of
- * kv_heads, heads / kv_heads <= 64.  out overlaps no input, its rows not each other.
- * workspace as for attention. */
+ * kv_heads, heads / kv_heads <= 64; n heads / kv_heads < 2^30; batch kv_heads < 2^24, and
+ * about 2^23 for more than 64 channels and n != 1.  out overlaps no input, its rows not
+ * each other.  workspace as for attention. */
 typedef struct pd_linear_attention_args {
   int32_t batch, heads, kv_heads, head_dim;
   int32_t n, per_round; /* per_round >= 1 */

@@ -849,8 +849,10 @@ pd_status check(const pd_linear_attention_args* a, bool pointers) {
   if (a->heads && (!a->kv_heads || a->heads % a->kv_heads)) return PD_ERR_INVALID_ARG;
   if (a->head_dim % 8 || a->head_dim > 128) return PD_ERR_UNSUPPORTED;
   if (a->heads && a->heads / a->kv_heads > 64) return PD_ERR_UNSUPPORTED;
-  // work items, and the scan's, are counted by the launches (threads below 2^32)
-  if ((__int128)a->kv_heads * a->batch >= 1ll << 17 || plan_for(a).items >= 1ll << 22) return PD_ERR_UNSUPPORTED;
+  // threads of a launch below 2^32: 256 for each work item (twice as many where two workgroups share it) or, of the recurrent form, key head.  (The
+  // scan's, up to 64 workgroups a key head, are fewer: segments are made of up to 1024 key heads.)
+  if ((__int128)a->kv_heads * a->batch >= 1ll << 24) return PD_ERR_UNSUPPORTED;
+  if (a->n != 1 && (plan_for(a).items + 7) * (a->head_dim > 64 ? 2 : 1) >= 1ll << 24) return PD_ERR_UNSUPPORTED;
   if ((__int128)a->n * (a->kv_heads ? a->heads / a->kv_heads : 1) >= 1ll << 30) return PD_ERR_UNSUPPORTED;  // rows, in 32 bits
   if (!pointers || !a->batch) return PD_OK;
   if (!a->heads) return a->kv_heads && a->state_out ? PD_ERR_INVALID_ARG : PD_OK;  // (states without a query: not handed on)

@@ -114,3 +114,23 @@ def test_what_is_not_finite_reaches_later_segments_alone(per_round, D):
         if x is v:
             columns = [c for c in range(D) if c != 5]
             assert torch.equal(out[..., columns], clean[..., columns]) and torch.equal(state[..., columns], last[..., columns])
+
+
+@pytest.mark.parametrize("n,per_round,D", [(1, 1, 8), (1, 1, 72), (3, 1, 8), (3, 40, 8), (3, 1, 72), (3, 40, 72)])
+def test_many_entries(n, per_round, D):
+    """131200 entries' heads: each as in a call of fewer."""
+    B, Hk, part = 16400, 8, 4100
+    g = tc.gen(n + D)
+    x = tc.normal(g, B, n, 2 * Hk, D).to(torch.bfloat16)
+    q, k = x[:, :, :Hk], x[:, :, Hk:]
+    state = tc.normal(g, B, Hk, D, D) if D == 8 else None
+    slopes = torch.linspace(0.0, 1.0, Hk, device="cuda")
+    out, want = torch.empty(B, n, Hk, D, device="cuda", dtype=torch.bfloat16), torch.empty(B, n, Hk, D, device="cuda", dtype=torch.bfloat16)
+    last, want_last = (None, None) if state is None else (torch.empty_like(state), torch.empty_like(state))
+    pdx.linear_attention(q, k, k, out, slopes=slopes, per_round=per_round, state=state, state_out=last)
+    for b in range(0, B, part):
+        s = slice(b, b + part)
+        pdx.linear_attention(q[s], k[s], k[s], want[s], slopes=slopes, per_round=per_round, state=None if state is None else state[s],
+                             state_out=None if state is None else want_last[s])
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and (state is None or torch.equal(last, want_last))

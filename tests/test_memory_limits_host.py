@@ -3,7 +3,7 @@ import pytest
 
 import paper_2604_12841_amd as pdx
 from paper_2604_12841_amd import tokens
-from test_memory_host import CACHE, LONG, attention8
+from test_memory_host import CACHE, LONG, attention8, linear
 
 BIG = 2147483647
 
@@ -36,3 +36,11 @@ def test_workspaces_at_the_end_of_the_sizes():
     for kw in (dict(n=BIG // 2, per_round=BIG), dict(n=1, per_round=BIG), dict(n=0), dict(batch=65535), dict(n=BIG), dict(n=1 << 29, heads=4), dict(batch=BIG, n=1),
                dict(head_dim=12), dict(per_round=0), dict(n=1 << 28, batch=4000)):
         assert work_linear(**kw) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(batch=BIG, n=1), dict(batch=1 << 23, n=1), dict(batch=1 << 23, n=2), dict(batch=BIG, heads=BIG, kv_heads=BIG, n=1),
+                                dict(batch=1 << 22, n=3, head_dim=128), dict(batch=BIG, heads=BIG, kv_heads=BIG, n=0)])
+def test_linear_launches_stay_below_2_32_threads(kw):
+    """256 threads for each key head of an entry, of more than 64 channels and several tokens twice as many."""
+    size = {n + "_batch_stride": 1 << 20 for n in ("q", "k", "v", "out")}
+    assert linear(**(size | dict(heads=2, kv_heads=2) | kw)) == pdx.PD_ERR_UNSUPPORTED
