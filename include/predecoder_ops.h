@@ -267,11 +267,10 @@ pd_status predecoder_cache_read(void* hip_stream, const pd_cache_args* args);
  * What predecoder_attention computes (there: scores, cap, slopes, masks, prefix,
  * queries that see nothing), of q over the tokens of a cache: keys and values are
  * code scale, not rounded in between.  Scores, maximum and sum are fp32; a
- * probability times a value's scale is rounded to bf16 (2^-8) for the product with the
- * values' codes, or for up to 64 rows (n_q heads / kv_heads) kept to 16 bits.  A visible
- * row with scale NaN makes the result NaN; what invisible places hold does not reach it
- * (but E4M3's NaN codes, which predecoder_cache_write never writes, may stand only where
- * there is no token).
+ * probability times a value's scale is kept to 16 bits (2^-16) for the product with the
+ * values' codes.  A visible row with scale NaN makes the result NaN; what invisible places
+ * hold does not reach it (but E4M3's NaN codes, which predecoder_cache_write never writes,
+ * may stand only where there is no token).
  * q and out as there: bf16, all rows 16-byte aligned; heads a multiple of
  * cache.kv_heads, heads / kv_heads <= 64; |coordinate| < 2^29.  q_sites is needed unless n_q
  * is 0.  workspace as there.  A cap is met within 2^-20 of the score or of the cap.

@@ -746,11 +746,13 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[n][e] -= up;
     }
-    // probabilities, times the value's scale, in bf16: keys 16 s + 4 half + {0 .. 3, 8 .. 11}; and their product with the codes
+    // probabilities, times the value's scale, in two bf16 parts, keys 16 s + 4 half + {0 .. 3, 8 .. 11}; and their product with the codes.  (In one part
+    // the result's error against 64 bits was half as large again as its own rounding's, 0.0024 against 0.0016; the second part costs 228 us against 205,
+    // 196 tokens against four caches of up to 200 rounds of d = 13, 8 (2) x 64 E4M3.)
     auto finish = [&](auto carefully) {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        uint32_t u[4], keep[2];
+        uint32_t u[4], ul[4], keep[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const float4 f4 = *(const float4*)&notes.v[16 * s + 8 * g + 4 * half];
@@ -763,16 +765,20 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
             x[e] = e2 * f[e];
             if constexpr (carefully.value) x[e] = y == -INFINITY ? 0.0f : x[e];  // (an invisible row's scale may be anything)
           }
-          u[2 * g] = bf16_pack(x[0], x[1]), u[2 * g + 1] = bf16_pack(x[2], x[3]);
+          split2(x[0], x[1], u[2 * g], ul[2 * g]);
+          split2(x[2], x[3], u[2 * g + 1], ul[2 * g + 1]);
           // codes at places without a token may be E4M3's NaN
           if constexpr (carefully.value) keep[g] = byte_mask((uint32_t)(tokens >> (16 * s + 8 * g + 4 * half)));
         }
-        const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+        const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+        const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(ul[0], ul[1], ul[2], ul[3]));
 #pragma unroll
         for (int m = 0; m < DP / 32; ++m) {
           i32x2 w = read_byte_columns(t.v + v_off[m] + 16 * s * DP);
           if constexpr (carefully.value) w[0] &= keep[0], w[1] &= keep[1];
-          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode<INT8>((uint32_t)w[0], (uint32_t)w[1]), pr, o[m], 0, 0, 0);
+          const bf16x8 v = decode<INT8>((uint32_t)w[0], (uint32_t)w[1]);
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pl, o[m], 0, 0, 0);
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, ph, o[m], 0, 0, 0);
         }
         if constexpr (LDS_Q) __builtin_amdgcn_sched_barrier(0);  // (reads of the next columns would spill)
       }

@@ -89,6 +89,15 @@ def test_without_a_cap(codes, D):
         hold(codes, 70, D, 0.0, reach, U16)
 
 
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("D", [32, 48, 64, 128])
+@pytest.mark.parametrize("n", [65, 130])
+def test_many_rows_keep_as_many_bits_as_few(codes, D, n):
+    """16 bits of a probability times its value's scale, whatever the number of rows."""
+    for cap, reach in ((0.0, 0.3), (0.0, 7.0), (20.0, 5.0), (20.0, 15.0), (80.0, 100.0)):
+        hold(codes, n, D, cap, reach, 2.0 ** -16)
+
+
 def ring(codes, g, d, kept, last, H, Hk, D):
     """A full ring of `kept` rounds up to round `last`, and its last round's sites."""
     grid = (d + 1) ** 2
