@@ -15,12 +15,19 @@
 // LDS, a tile ahead; at the end they join.  Sixteen streams of up to 65536
 // places, 8 query and 2 key heads of 128, int8: 88 us, 4.9 TB/s (the same loads
 // without any work on them: 84 us).  One token against four caches of up to 200
-// rounds of d = 13, 8 (2) heads of 64, E4M3: 14.6 us and 4 us of the join.
+// rounds of d = 13, 8 (2) heads of 64, E4M3: 14.2 us and 4 us of the join.
 //
 // Many rows: 128 a workgroup, 32 a wave, which share tiles in LDS.  Bound by
-// vector instructions, about 14 a score with cap and bias: 196 tokens against the same
-// four caches 196 us and 8 us of the join (260 TFLOP/s; vector units 0.54 busy
-// without what the exponentials take longer, matrix units 0.11).
+// vector instructions, about 20 a score with cap and bias, and by latencies that 1.5
+// waves a SIMD leave open: 196 tokens against the same four caches 221 us and 8 us of
+// the join (230 TFLOP/s; vector units 0.54 busy without what the exponentials take
+// longer, matrix units 0.15, waves wait 0.37 of their cycles).
+//
+// With a bias, distances come from the last byte of rounds, rows and columns where a
+// tile's keys and the queries are of one block of 256 rounds (t >> 8).  Tiles of
+// other blocks take the general form, score by score: the same call with rounds 156
+// to 355, 100 of them in another block than the queries, takes 448 us against 228, one
+// token 22.5 against 18.6.
 //
 // What to read: before the keys of 8 (16) tiles the sites are read, and tiles
 // that no row sees are skipped.
@@ -112,8 +119,9 @@ __device__ __forceinline__ bf16x8 decode(uint32_t a, uint32_t b) {
 // A score in log2 units, t added, from u = x f (x the product, f the key's scale times p.factor): u without a cap, with it cap_b tanh u
 // (CAP_FAR: u before the cap, cap_b tanh(unit u)).  TIER: |u| (unit |u|) is at most TIERS[TIER], or 3: anything.
 constexpr float TIERS[3] = {0.35f, 0.62f, 0.87f};
-// tanh u for |u| <= 0.62 is u (N1 + u^2 (N3 + ...)), for |u| <= 0.87 u (M1 + u^2 (M3 + ...)), within 7.9e-7 (fitted for the least
+// tanh u for |u| <= 0.62 is u (N1 + u^2 (N3 + ...)), for |u| <= 0.87 u (M1 + u^2 (M3 + ...)), within 8e-7 (fitted for the least
 // largest error): one and two instructions more than for the small ones, against an exponential and a reciprocal at a quarter of the rate.
+// The ranges end where the best polynomials of four and five coefficients pass 8e-7, so that a cap is met within 2^-20 of itself.
 constexpr float N1 = 0.99998862f, N3 = -0.33292374f, N5 = 0.12931657f, N7 = -0.03883829f;
 constexpr float M1 = 0.99999005f, M3 = -0.33305562f, M5 = 0.13114086f, M7 = -0.04667219f, M9 = 0.01031595f;
 template <Cap CAP, int TIER>
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[n][e] -= up;
     }
-    // probabilities, times the value's scale, in two bf16 parts (16 bits: matrix units have the time); and their product with the codes
+    // probabilities, times the value's scale, in two bf16 parts (16 bits: as in the kernel for many rows); and their product with the codes
     auto finish = [&](auto carefully) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -481,7 +489,7 @@ __global__ void __launch_bounds__(FW * 64, 2) attention8_few_kernel(const Attn8 
   total += __shfl_xor(total, 16);
   total += __shfl_xor(total, 32);
   const bool none = unset && total == 0.0f;  // saw nothing (without a reference, but NaN scores: not nothing)
-  // join the four waves, through the tiles' memory (what was sent for and not used has to be in before)
+  // join the eight waves, through the tiles' memory (what was sent for and not used has to be in before)
   sent();
   if (g4 == 0) ml[wave][c] = make_float2(none ? -INFINITY : top, total);
 #pragma unroll
@@ -525,8 +533,8 @@ __global__ void __launch_bounds__(NW * 64, 2) attention8_kernel(const Attn8 p) {
   constexpr int NT = NW * 64;
   constexpr int GR = DP / 16;  // granules of a row
   constexpr int AHEAD = 16;    // tiles whose sites are looked at together
-  // Queries past 64 channels wait in LDS: in registers they made others spill (54 at 128 channels, 15 now; 196 tokens against four
-  // caches of up to 100 rounds, 8 (2) x 128: 173 us against 184).  At 64 channels nothing spills (205 us; from LDS 209).
+  // Queries past 64 channels wait in LDS: in registers they made others spill (62 at 128 channels, 22 now; 196 tokens against four
+  // caches of up to 100 rounds, 8 (2) x 128: 194 us against 200).  At 64 channels they cost nothing (228 us; from LDS 232).
   constexpr bool LDS_Q = DP > 64;
   __shared__ KeyTile<DP> tiles[2];
   __shared__ KeyNotes notes;
@@ -884,7 +892,7 @@ __global__ void __launch_bounds__(256) attention8_join_kernel(const Attn8 p) {
   *(uint2*)(p.out + b * p.o_b + row / p.group * p.o_t + (kvh * p.group + row % p.group) * p.o_h + 4 * lane) = v;
 }
 
-// The same for up to FEW_SPLITS splits of MANY_ROWS rows or more: a thread joins four columns of a row (6272 rows of 10 splits: 7.8 us, above 11;
+// The same for up to FEW_SPLITS splits of MANY_ROWS rows or more: a thread joins four columns of a row (6272 rows of 10 splits: 7.6 us, above 11;
 // 32 rows of 31: 15 us, above 4).
 constexpr int FEW_SPLITS = 32, MANY_ROWS = 2048;
 template <int DP>
@@ -930,13 +938,13 @@ Plan plan_for(const pd_attention8_args* a) {
   const pd_cache& c = a->cache;
   Plan n = {};
   const long long rows = (long long)a->n_q * (a->heads / c.kv_heads), heads = (long long)c.kv_heads * c.batch;
-  // (8 (2) heads of 64 against four caches of up to 200 rounds: 36 rows 45 us for few, 44 for many; 64 rows 36 and 46; 132 rows 80 both)
+  // (8 (2) heads of 64 against four caches of up to 200 rounds: 36 rows 46 us for few, 45 for many; 64 rows 34 and 47; 132 rows 81 and 80)
   n.few = rows <= 64;
   n.row_tiles = (int)((rows + (n.few ? 15 : 127)) / (n.few ? 16 : 128));
   n.tiles = (int)(((long long)c.capacity + TILE - 1) / TILE);
   const int dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   // Splits: to fill the card (256 workgroups of eight waves, 512 of four), down to 8 tiles each.  (Two or three times as many cost more than
-  // they even out: the token above 18 to 19 us against 14, the round 212 to 240 against 206.)
+  // they even out: the token above 25 and 28 us against 19, the round 232 and 235 against 228.)
   const long long whole = n.row_tiles * heads, fill = n.few ? 256 : 512;
   long long splits = (fill + whole - 1) / whole;
   if (splits > n.tiles / 8) splits = n.tiles / 8;
